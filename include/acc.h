@@ -48,6 +48,7 @@ extern "C" {
 #define ACC_ECUDA 4       /* a CUDA runtime call or kernel launch reported an error */
 #define ACC_ETOOBIG 5     /* size beyond the fixed capacity of acc_sumsq_static    */
 #define ACC_ETIMEOUT 6    /* device side: a bounded wait on an asynchronous copy gave up (acc_device_status) */
+#define ACC_EINDEX 7      /* device side: a token id beyond the embedding's rows (acc_device_status)          */
 
 #define ACC_MATRIX 0
 #define ACC_VECTOR 1
@@ -243,6 +244,76 @@ int acc_powersgd_step_sgd(acc_ctx* ctx, const float* grads, float* err, float* q
 int acc_topk_step_sgd(acc_ctx* ctx, const float* grads, float* err, const uint8_t* level, float* vals,
                       int32_t* idx, int32_t* counts, float* out, float* delta, float* params, float* mom,
                       const float* hyper, void* stream);
+
+/* ---- AdamW (no counterpart in the paper, whose runs use the Nesterov update above) ------------------------------
+ * The update of adaptive moments with decoupled weight decay, on every element of every layer in one launch:
+ *   t = *step + 1;  g = f * d  with f = *grad_scale, 1 when grad_scale is NULL;
+ *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   x <- x - lr weight_decay x - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps);  *step <- t.
+ * hyper is a DEVICE array of five doubles {lr, beta1, beta2, eps, weight_decay} and step one DEVICE int64 (0 before the
+ * first call): the kernel reads both and counts the step itself, so a captured graph follows a schedule when the caller
+ * rewrites the doubles.  The coefficients are worked out in fp64, the elements in fp32.  Padding between layers is left
+ * alone.  When f is NaN or infinite the call changes nothing, the step count included (a gradient that overflowed);
+ * without grad_scale, elements of d that are not finite go through the formulas.  eps = 0 divides 0 by 0 wherever no
+ * gradient has arrived yet.  params_bf16, when not NULL, receives the new parameters rounded to nearest bf16.
+ * flags: 0 or ACC_ADAMW_NO_VECTOR_DECAY (VECTOR layers -- biases, norm weights -- take no weight decay).
+ *
+ * acc_adamw holds m and v as floats [worker_stride].
+ * acc_adamw_8bit holds m and r = sqrt(v) as e4m3 bytes [worker_stride], times a power of two (an e8m0 byte,
+ * 2^(byte - 127)) for each block of ACC_ADAMW_BLOCK elements of a layer: layer l's blocks are
+ * block0[l] .. block0[l] + ceil(rows*cols / ACC_ADAMW_BLOCK) - 1 of the n_blocks scales (acc_adamw_layout).  All bytes
+ * 0 is the state before the first step.  The update uses the unrounded new m and v.  They are then rounded: a block's
+ * scale puts its largest magnitude into [128, 256), and each magnitude goes up or down to a neighbouring code with the
+ * probabilities that keep its mean, by 16 bits of a hash of (seed, t, element) -- a step moves r by less than half a
+ * step of the grid, so rounding to nearest would freeze it --; a positive r never becomes 0.  Same inputs, same bits.
+ * A block whose new m (r) holds a NaN or an infinity gets the scale 255: all of its m (r) read as NaN from then on.
+ *
+ * acc_clip_factor: *factor = min(1, max_norm / norm) with norm = sqrt(sum_l norm2_layers[l]) (fp64, fixed order), NaN
+ * when norm is not finite; *norm = norm when not NULL.  acc_layer_norms(d) -> acc_clip_factor -> acc_adamw(grad_scale)
+ * clips by the global norm.  max_norm >= 0 and not NaN, otherwise ACC_EINVAL.
+ * Device pointers: d (read), params, m, v [worker_stride] floats; m_code, r_code [worker_stride] bytes, 16-byte aligned;
+ * m_scale, r_scale [n_blocks] bytes (no alignment); params_bf16 [worker_stride] 16-bit words; norm2_layers [L] doubles;
+ * factor, grad_scale one float; norm one double.  Calls on one context share its count of finished blocks: order them
+ * on one stream, as everything else on it.                                                                  */
+#define ACC_ADAMW_BLOCK 256
+#define ACC_ADAMW_NO_VECTOR_DECAY 1
+int acc_adamw_layout(const acc_ctx* ctx, int64_t* block0 /*[L]*/, int64_t* n_blocks);
+int acc_adamw(acc_ctx* ctx, const float* d, float* params, float* m, float* v, int64_t* step, const double* hyper,
+              const float* grad_scale, uint16_t* params_bf16, int32_t flags, void* stream);
+int acc_adamw_8bit(acc_ctx* ctx, const float* d, float* params, uint8_t* m_code, uint8_t* r_code, uint8_t* m_scale,
+                   uint8_t* r_scale, int64_t* step, const double* hyper, const float* grad_scale,
+                   uint16_t* params_bf16, uint32_t seed, int32_t flags, void* stream);
+int acc_clip_factor(acc_ctx* ctx, const double* norm2_layers, double max_norm, float* factor, double* norm,
+                    void* stream);
+
+/* ---- Embedding of a MATRIX layer (no counterpart in the paper: its language model's row-sparse encoder gradient is
+ * where such a layer's step begins) ----------------------------------------------------------------------------
+ * Tokens are row numbers, int32 or int64 (token_type ACC_I32 / ACC_I64).  A negative token pads the batch: its row is
+ * zeros and its gradient is not read.  A token >= rows is treated the same way and stores ACC_EINDEX in the status word
+ * (acc_device_status); nothing is read or written out of bounds.
+ *
+ * acc_embedding_lookup:  out[i] = scale * row tokens[i] of the layer in params, i < n, in fp32, rounded once to out_type
+ *   (ACC_F32 / ACC_BF16).  params [worker_stride] floats (read), tokens [n], out [n][cols] (written).
+ * acc_embedding_grad, for each of the W workers w:
+ *   G_w[row] = scale * sum over i with tokens[w][i] == row of dy[w][i]   (fp32 sums in an order that depends on the tokens
+ *   alone: bit-reproducible), G_w being the layer in worker w's slice of grads [W][worker_stride].  accumulate = 0: every
+ *   other row of G_w becomes zero, nothing outside the layer is touched.  accumulate != 0: the sums are added to what G_w
+ *   holds (weights shared with another layer, micro-batches) and rows without a token are not touched.
+ *   tokens [W][n], dy [W][n][cols] of dy_type (read).  workspace: acc_embedding_workspace_bytes(n) bytes of DEVICE memory,
+ *   256-byte aligned, caller-owned, for one call at a time; its contents before and after do not matter.
+ * n = 0 is allowed (tokens, out and dy may then be NULL).  n (lookup) and W * n (gradient) are at most
+ * ACC_EMBEDDING_MAX_TOKENS, otherwise ACC_EINVAL, as for a VECTOR layer or an unknown type.                    */
+#define ACC_F32 0
+#define ACC_BF16 1
+#define ACC_I32 0
+#define ACC_I64 1
+#define ACC_EMBEDDING_MAX_TOKENS (1 << 28)
+int acc_embedding_lookup(acc_ctx* ctx, int32_t layer, const float* params, const void* tokens, int32_t token_type,
+                         int64_t n, float scale, void* out, int32_t out_type, void* stream);
+int acc_embedding_workspace_bytes(const acc_ctx* ctx, int32_t layer, int64_t n, size_t* bytes);
+int acc_embedding_grad(acc_ctx* ctx, int32_t layer, const void* tokens, int32_t token_type, int64_t n, float scale,
+                       const void* dy, int32_t dy_type, float* grads, int32_t accumulate, void* workspace,
+                       size_t workspace_bytes, void* stream);
 
 /* ---- Batch-size mode (Section 4.2: "For batch size we use the same algorithm", switching between B_low and
  * B_high at the granularity of the whole model; Section 5.1: the learning rate scales in the same ratio;

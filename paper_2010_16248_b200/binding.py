@@ -22,8 +22,15 @@ ACC_FLAG_LAZY_RESIDUAL = 1
 ACC_FLAG_PIPELINE_ALWAYS = 2
 ACC_FLAG_PIPELINE_NEVER = 4
 ACC_FLAG_SHARE_SMS = 8
+ACC_ADAMW_BLOCK = 256
+ACC_ADAMW_NO_VECTOR_DECAY = 1
+ACC_EINDEX = 7
 POWERSGD, TOPK = 0, 1
 ACC_TOPK_PATH_DENSE, ACC_TOPK_PATH_LIST, ACC_TOPK_PATH_LIST_PREDICTED, ACC_TOPK_PATH_STAGED, ACC_TOPK_PATH_ZERO_FILL = range(5)
+
+
+_TOKEN_TYPES = {torch.int32: 0, torch.int64: 1}   # ACC_I32, ACC_I64
+_VALUE_TYPES = {torch.float32: 0, torch.bfloat16: 1}  # ACC_F32, ACC_BF16
 
 
 class AccError(RuntimeError):
@@ -53,7 +60,8 @@ EXPORTS = ["acc_workspace_bytes", "acc_create", "acc_destroy", "acc_factor_layou
            "acc_exchange_layout", "acc_powersgd_phase1", "acc_powersgd_phase2", "acc_powersgd_phase3",
            "acc_topk_compress", "acc_topk_decompress", "acc_topk_flush",
            "acc_upload_grads", "acc_download_out", "acc_selftest_wait_timeout", "acc_reset_device_status",
-           "acc_layer_msdr", "acc_detect_regime_lr"]
+           "acc_layer_msdr", "acc_detect_regime_lr", "acc_adamw_layout", "acc_adamw", "acc_adamw_8bit", "acc_clip_factor",
+           "acc_embedding_lookup", "acc_embedding_workspace_bytes", "acc_embedding_grad"]
 
 _lib = None
 
@@ -116,6 +124,13 @@ def lib() -> C.CDLL:
     L.acc_selftest_wait_timeout.argtypes = [vp, vp]
     L.acc_reset_device_status.argtypes = [vp, vp]
     L.acc_download_out.argtypes = [vp, vp, vp, vp]
+    L.acc_adamw_layout.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
+    L.acc_adamw.argtypes = [vp] * 9 + [i32, vp]
+    L.acc_adamw_8bit.argtypes = [vp] * 11 + [C.c_uint32, i32, vp]
+    L.acc_clip_factor.argtypes = [vp, vp, C.c_double, vp, vp, vp]
+    L.acc_embedding_lookup.argtypes = [vp, i32, vp, vp, i32, i64, f32, vp, i32, vp]
+    L.acc_embedding_workspace_bytes.argtypes = [vp, i32, i64, C.POINTER(C.c_size_t)]
+    L.acc_embedding_grad.argtypes = [vp, i32, vp, i32, i64, f32, vp, i32, vp, i32, vp, C.c_size_t, vp]
     for name in EXPORTS:
         if name not in ("acc_floats_sent", "acc_last_launch_count", "acc_strerror", "acc_profile_kernel_count",
                         "acc_profile_kernel_name"):
@@ -241,6 +256,9 @@ class Context:
         x1, x2, vf = C.c_int64(), C.c_int64(), C.c_int64()
         L.acc_exchange_layout(self._h, C.byref(x1), C.byref(x2), C.byref(vf))
         self.x1_floats, self.x2_floats, self.vec_floats = int(x1.value), int(x2.value), int(vf.value)
+        b0, nb = (C.c_int64 * n)(), C.c_int64()
+        L.acc_adamw_layout(self._h, b0, C.byref(nb))
+        self.adamw_block0, self.adamw_blocks = np.array(b0[:], np.int64), int(nb.value)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -259,7 +277,12 @@ class Context:
 
     def _call(self, name, *items, stream=None):
         """Checks and marshals the tensor arguments, then calls entry point ``name`` on this context."""
-        self._check(getattr(lib(), name)(self._h, *_marshal(self.device, *items), _stream(stream)), name)
+        args = _marshal(self.device, *items)
+        if self.device.index is not None and self.device.index != torch.cuda.current_device():
+            with torch.cuda.device(self.device):  # kernels launch on the current device
+                self._check(getattr(lib(), name)(self._h, *args, _stream(stream)), name)
+            return
+        self._check(getattr(lib(), name)(self._h, *args, _stream(stream)), name)
 
     # --- argument checks: every device buffer must hold what the context's layout will index -----------------
     def _f(self, t, n, what):
@@ -364,6 +387,65 @@ class Context:
         self._call("acc_topk_step_sgd", *self._topk_args(grads, err, level, vals, idx, counts),
                    self._f(out, self.stride, "out"), self._f(delta, self.stride, "delta"),
                    *self._tail(params, mom, hyper), stream=stream)
+
+    def _adamw_args(self, d, params, states, step, hyper, grad_scale, params_bf16):
+        return (self._f(d, self.stride, "d"), self._f(params, self.stride, "params"), *states,
+                _Arg(step, torch.int64, 1, "step"), self._d(hyper, 5, "hyper"), self._f(grad_scale, 1, "grad_scale"),
+                _Arg(params_bf16, torch.bfloat16, self.stride, "params_bf16"))
+
+    def acc_adamw(self, d, params, m, v, step, hyper, grad_scale=None, params_bf16=None, flags=0, stream=None):
+        self._call("acc_adamw", *self._adamw_args(d, params, (self._f(m, self.stride, "m"), self._f(v, self.stride, "v")),
+                                                  step, hyper, grad_scale, params_bf16), int(flags), stream=stream)
+
+    def acc_adamw_8bit(self, d, params, m_code, r_code, m_scale, r_scale, step, hyper, seed=0, grad_scale=None,
+                       params_bf16=None, flags=0, stream=None):
+        """The states are ``torch.float8_e4m3fn`` codes and ``torch.float8_e8m0fnu`` scales (``new_adamw_8bit``)."""
+        states = (_Arg(m_code, torch.float8_e4m3fn, self.stride, "m_code"),
+                  _Arg(r_code, torch.float8_e4m3fn, self.stride, "r_code"),
+                  _Arg(m_scale, torch.float8_e8m0fnu, self.adamw_blocks, "m_scale"),
+                  _Arg(r_scale, torch.float8_e8m0fnu, self.adamw_blocks, "r_scale"))
+        self._call("acc_adamw_8bit", *self._adamw_args(d, params, states, step, hyper, grad_scale, params_bf16),
+                   int(seed) & 0xFFFFFFFF, int(flags), stream=stream)
+
+    def acc_clip_factor(self, norm2_layers, max_norm, factor, norm=None, stream=None):
+        self._call("acc_clip_factor", self._d(norm2_layers, self.n_layers, "norm2_layers"), float(max_norm),
+                   self._f(factor, 1, "factor"), self._d(norm, 1, "norm"), stream=stream)
+
+    def _embedding(self, layer, tokens, values, what):
+        """Index of the MATRIX layer, token type, number of values' rows and value type of an embedding call."""
+        layer = int(layer)
+        if not 0 <= layer < self.n_layers or self.q_row[layer] < 0:
+            raise ValueError(f"layer {layer}: expected the index of a MATRIX layer")
+        for t, dtypes, name in ((tokens, _TOKEN_TYPES, "tokens"), (values, _VALUE_TYPES, what)):
+            if not isinstance(t, torch.Tensor):
+                raise ValueError(f"{name}: expected a torch tensor")
+            if t.dtype not in dtypes:
+                raise ValueError(f"{name}: expected one of {list(dtypes)}, got {t.dtype}")
+        n, cols = tokens.numel(), int(self.table.cols[layer])
+        if values.numel() != n * cols:
+            raise ValueError(f"{what}: {values.numel()} elements, {n} tokens of {cols} columns need {n * cols}")
+        return layer, n, _TOKEN_TYPES[tokens.dtype], _VALUE_TYPES[values.dtype]
+
+    def acc_embedding_lookup(self, layer, params, tokens, out, scale=1.0, stream=None):
+        """``out[i] = scale * row tokens[i]`` of layer ``layer`` (its index) of ``params``; shapes only have to agree in
+        number: ``tokens`` of any shape (int32 / int64), ``out`` its shape times the layer's columns (float32 /
+        bfloat16)."""
+        layer, n, tt, ot = self._embedding(layer, tokens, out, "out")
+        self._call("acc_embedding_lookup", layer, self._f(params, self.extent, "params"),
+                   _Arg(tokens, tokens.dtype, n, "tokens"), tt, n, float(scale), _Arg(out, out.dtype, out.numel(), "out"),
+                   ot, stream=stream)
+
+    def acc_embedding_grad(self, layer, tokens, dy, grads, scale=1.0, accumulate=False, workspace=None, stream=None):
+        """Gradient of the lookup into layer ``layer`` of ``grads`` ``[W, stride]``: ``tokens`` ``[W, n]``, ``dy``
+        ``[W, n, cols]``; ``workspace`` from ``new_embedding_workspace(layer, n)``."""
+        layer, total, tt, vt = self._embedding(layer, tokens, dy, "dy")
+        if total % self.n_workers or (tokens.dim() > 1 and tokens.shape[0] != self.n_workers):
+            raise ValueError(f"tokens: expected [{self.n_workers}, n]")
+        n = total // self.n_workers
+        nbytes = 0 if workspace is None else workspace.numel()
+        self._call("acc_embedding_grad", layer, _Arg(tokens, tokens.dtype, total, "tokens"), tt, n, float(scale),
+                   _Arg(dy, dy.dtype, dy.numel(), "dy"), vt, self._f(grads, self._wn, "grads"), int(bool(accumulate)),
+                   _Arg(workspace, torch.uint8, 0, "workspace"), nbytes, stream=stream)
 
     def acc_batch_accumulate(self, grads, acc, delta=None, first=False, stream=None):
         self._call("acc_batch_accumulate", self._f(grads, self._wn, "grads"), self._f(acc, self._wn, "acc"),
@@ -476,6 +558,19 @@ class Context:
 
     def new_p(self):
         return torch.zeros(max(self.p_rows, 1), ACC_MAX_RANK, dtype=torch.float32, device=self.device)
+
+    def new_adamw_8bit(self):
+        """``m_code, r_code [stride], m_scale, r_scale [blocks]`` of the 8-bit AdamW states before the first step."""
+        zeros = lambda n, dtype: torch.zeros(n, dtype=torch.uint8, device=self.device).view(dtype)  # noqa: E731
+        return (zeros(self.stride, torch.float8_e4m3fn), zeros(self.stride, torch.float8_e4m3fn),
+                zeros(self.adamw_blocks, torch.float8_e8m0fnu), zeros(self.adamw_blocks, torch.float8_e8m0fnu))
+
+    def new_embedding_workspace(self, layer, n):
+        """Scratch of ``acc_embedding_grad`` for ``n`` tokens per worker; one call at a time may use it."""
+        nbytes = C.c_size_t(0)
+        self._check(lib().acc_embedding_workspace_bytes(self._h, int(layer), int(n), C.byref(nbytes)),
+                    "acc_embedding_workspace_bytes")
+        return torch.empty(int(nbytes.value), dtype=torch.uint8, device=self.device)
 
     def new_topk_buffers(self):
         W = self.n_workers

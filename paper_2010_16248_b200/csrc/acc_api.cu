@@ -61,6 +61,8 @@ static int make_plan(const acc_config* cfg, Plan& p) {
     o.q_row = o.p_row = o.mat = -1; o.seg_off = -1; o.part_base = -1; o.vec_off = -1;
     o.vec = (d.cols % 4 == 0) ? 4 : (d.cols % 2 == 0) ? 2 : 1;
     const long long size = (long long)d.rows * d.cols;
+    o.adam_block0 = p.adam_blocks;
+    p.adam_blocks += (size + ACC_ADAMW_BLOCK - 1) / ACC_ADAMW_BLOCK;
     // flat tiles
     o.tile0 = (int)p.tiles.size();
     for (long long e = 0; e < size; e += kTile) {
@@ -461,6 +463,100 @@ int acc_sgd_nesterov(acc_ctx* ctx, const float* d, float* params, float* mom, co
                                  static_cast<cudaStream_t>(stream)));
 }
 
+int acc_adamw_layout(const acc_ctx* ctx, int64_t* block0, int64_t* n_blocks) {
+  if (!ctx) return ACC_EINVAL;
+  if (block0)
+    for (int l = 0; l < ctx->cfg.n_layers; ++l) block0[l] = ctx->plan.layers[l].adam_block0;
+  if (n_blocks) *n_blocks = ctx->plan.adam_blocks;
+  return ACC_OK;
+}
+
+static int check_adamw(const acc_ctx* ctx, const float* d, const float* params, const int64_t* step, const double* hyper,
+                       const float* grad_scale, const uint16_t* params_bf16, int flags) {
+  if (!ctx || !d || !params || !step || !hyper || (flags & ~ACC_ADAMW_NO_VECTOR_DECAY)) return ACC_EINVAL;
+  if (!aligned16(d) || !aligned16(params) || !aligned16(params_bf16) || (reinterpret_cast<uintptr_t>(step) & 7u) ||
+      (reinterpret_cast<uintptr_t>(hyper) & 7u) || (reinterpret_cast<uintptr_t>(grad_scale) & 3u))
+    return ACC_EALIGN;
+  return ACC_OK;
+}
+
+int acc_adamw(acc_ctx* ctx, const float* d, float* params, float* m, float* v, int64_t* step, const double* hyper,
+              const float* grad_scale, uint16_t* params_bf16, int32_t flags, void* stream) {
+  const int st = check_adamw(ctx, d, params, step, hyper, grad_scale, params_bf16, flags);
+  if (st == ACC_EINVAL || !m || !v) return ACC_EINVAL;
+  if (st != ACC_OK || !aligned16(m) || !aligned16(v)) return ACC_EALIGN;
+  ctx->last_launches = 0;
+  return finish(launch_adamw(ctx, d, params, m, v, step, hyper, grad_scale, params_bf16, flags,
+                             static_cast<cudaStream_t>(stream)));
+}
+
+int acc_adamw_8bit(acc_ctx* ctx, const float* d, float* params, uint8_t* m_code, uint8_t* r_code, uint8_t* m_scale,
+                   uint8_t* r_scale, int64_t* step, const double* hyper, const float* grad_scale,
+                   uint16_t* params_bf16, uint32_t seed, int32_t flags, void* stream) {
+  const int st = check_adamw(ctx, d, params, step, hyper, grad_scale, params_bf16, flags);
+  if (st == ACC_EINVAL || !m_code || !r_code || !m_scale || !r_scale) return ACC_EINVAL;
+  if (st != ACC_OK || !aligned16(m_code) || !aligned16(r_code)) return ACC_EALIGN;
+  ctx->last_launches = 0;
+  return finish(launch_adamw_8bit(ctx, d, params, m_code, r_code, m_scale, r_scale, step, hyper, grad_scale,
+                                  params_bf16, seed, flags, static_cast<cudaStream_t>(stream)));
+}
+
+int acc_clip_factor(acc_ctx* ctx, const double* norm2_layers, double max_norm, float* factor, double* norm,
+                    void* stream) {
+  if (!ctx || !norm2_layers || !factor || !(max_norm >= 0.0)) return ACC_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(norm2_layers) & 7u) || (reinterpret_cast<uintptr_t>(factor) & 3u) ||
+      (reinterpret_cast<uintptr_t>(norm) & 7u))
+    return ACC_EALIGN;
+  ctx->last_launches = 0;
+  return finish(launch_clip_factor(ctx, norm2_layers, max_norm, factor, norm, static_cast<cudaStream_t>(stream)));
+}
+
+// Tokens a call may hand over: all workers' together, so that every grid and position fits 31 bits.
+static int check_embedding(const acc_ctx* ctx, int layer, int token_type, int64_t n, int value_type) {
+  if (!ctx || layer < 0 || layer >= ctx->cfg.n_layers || ctx->plan.layers[layer].kind != ACC_MATRIX) return ACC_EINVAL;
+  if (token_type != ACC_I32 && token_type != ACC_I64) return ACC_EINVAL;
+  if (value_type != ACC_F32 && value_type != ACC_BF16) return ACC_EINVAL;
+  if (n < 0 || n > ACC_EMBEDDING_MAX_TOKENS) return ACC_EINVAL;
+  return ACC_OK;
+}
+
+int acc_embedding_lookup(acc_ctx* ctx, int32_t layer, const float* params, const void* tokens, int32_t token_type,
+                         int64_t n, float scale, void* out, int32_t out_type, void* stream) {
+  const int st = check_embedding(ctx, layer, token_type, n, out_type);
+  if (st != ACC_OK) return st;
+  if (!params || (n > 0 && (!tokens || !out))) return ACC_EINVAL;
+  if (!aligned16(params) || !aligned16(out) ||
+      (reinterpret_cast<uintptr_t>(tokens) & (token_type == ACC_I64 ? 7u : 3u)))
+    return ACC_EALIGN;
+  ctx->last_launches = 0;
+  if (n == 0) return ACC_OK;
+  return finish(launch_embedding_lookup(ctx, layer, params, tokens, token_type == ACC_I64, n, scale, out,
+                                        out_type == ACC_BF16, static_cast<cudaStream_t>(stream)));
+}
+
+int acc_embedding_workspace_bytes(const acc_ctx* ctx, int32_t layer, int64_t n, size_t* bytes) {
+  if (!bytes) return ACC_EINVAL;
+  const int st = check_embedding(ctx, layer, ACC_I32, n, ACC_F32);
+  if (st != ACC_OK || n * ctx->cfg.n_workers > ACC_EMBEDDING_MAX_TOKENS) return ACC_EINVAL;
+  *bytes = embedding_workspace(ctx, layer, n);
+  return ACC_OK;
+}
+
+int acc_embedding_grad(acc_ctx* ctx, int32_t layer, const void* tokens, int32_t token_type, int64_t n, float scale,
+                       const void* dy, int32_t dy_type, float* grads, int32_t accumulate, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  const int st = check_embedding(ctx, layer, token_type, n, dy_type);
+  if (st != ACC_OK) return st;
+  if (n * ctx->cfg.n_workers > ACC_EMBEDDING_MAX_TOKENS || !grads || (n > 0 && (!tokens || !dy))) return ACC_EINVAL;
+  if (!aligned16(grads) || !aligned16(dy) || (reinterpret_cast<uintptr_t>(tokens) & (token_type == ACC_I64 ? 7u : 3u)))
+    return ACC_EALIGN;
+  if (!workspace || workspace_bytes < embedding_workspace(ctx, layer, n)) return ACC_EWORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ACC_EALIGN;
+  ctx->last_launches = 0;
+  return finish(launch_embedding_grad(ctx, layer, tokens, token_type == ACC_I64, n, scale, dy, dy_type == ACC_BF16,
+                                      grads, accumulate != 0, workspace, static_cast<cudaStream_t>(stream)));
+}
+
 int acc_batch_accumulate(acc_ctx* ctx, const float* grads, float* acc, float* delta, int32_t first, void* stream) {
   if (!ctx || !grads || !acc) return ACC_EINVAL;
   if (!aligned16(grads) || !aligned16(acc) || !aligned16(delta)) return ACC_EALIGN;
@@ -579,7 +675,10 @@ const char* acc_profile_kernel_name(int32_t i) {
       "topk_hist2_list_kernel", "topk_hist3_list_kernel", "topk_finalize_staged_kernel",
       "psgd_orthonormalise_block_kernel", "sgd_tiles_kernel", "batch_accumulate_kernel", "batch_average_kernel",
       "detect_batch_kernel", "psgd_pfold_kernel", "vec_exchange_kernel", "psgd_qmerge_kernel",
-      "topk_decompress_packed_kernel", "topk_flush_kernel", "moments_partial_kernel", "moments_final_kernel"};
+      "topk_decompress_packed_kernel", "topk_flush_kernel", "moments_partial_kernel", "moments_final_kernel",
+      "adamw_kernel", "adamw_8bit_kernel", "clip_factor_kernel",
+      "embedding_lookup_kernel", "embedding_rank_kernel", "embedding_keys_kernel", "embedding_hist_kernel",
+      "embedding_scan_kernel", "embedding_scatter_kernel", "embedding_sum_kernel", "embedding_join_kernel"};
   return (i >= 0 && i < PH_COUNT) ? names[i] : "";
 }
 
@@ -624,6 +723,7 @@ const char* acc_strerror(int status) {
     case ACC_EWORKSPACE: return "workspace missing or too small";
     case ACC_ECUDA: return "CUDA runtime or launch error";
     case ACC_ETIMEOUT: return "a bounded device-side wait gave up (asynchronous copy did not complete)";
+    case ACC_EINDEX: return "a token id beyond the embedding's rows";
     case ACC_ETOOBIG: return "size exceeds the capacity of the built-in scratch array (ACC_STATIC_NORM_MAX_ELEMS)";
     default: return "unknown status";
   }

@@ -34,6 +34,7 @@ struct DevLayer {
   int cand_cap;         // slots of that list (the list path is taken when bucket b1 fits)
   long long part_base;  // first float4 of the layer's Q partials
   int slab_rows, nslabs;  // row slabs of the Q-partial pass
+  long long adam_block0;  // first block of ACC_ADAMW_BLOCK elements of the layer among the 8-bit states' scales
   long long vec_off;      // VECTOR layers: first float of the layer inside the packed exchange region, else -1
 };
 
@@ -56,6 +57,7 @@ constexpr int kSelDense = 0, kSelList = 1, kSelListPred = 2, kSelStaged = 3, kSe
 constexpr int kListCollect = 0, kListDense = 1, kListSelect = 2, kListStaged = 3, kNumLists = 4;
 constexpr int kListCountWord = 8;  // the lists' lengths live at words 8..11 of the per-step word block
 constexpr int kTicketWord = 16;    // tile ticket of the decompress pass, same block (cleared at the start of a step)
+constexpr int kAdamTicketWord = 10; // finished-block count of the AdamW kernels, in the status block (zero between calls)
 constexpr unsigned kNoPendingTau = 0xffffffffu;  // no key is larger: nothing pending
 constexpr int kPredTileCap = 2048;  // keys one tile may hand to a predicted list (more: overflow, fall back)
 
@@ -67,6 +69,8 @@ enum Phase {
   PH_TOPK_DECOMPRESS, PH_PSGD_FLUSH, PH_TOPK_COLLECT, PH_TOPK_PICK3, PH_TOPK_TILE_COUNTS, PH_TOPK_HIST2_LIST, PH_TOPK_HIST3_LIST, PH_TOPK_FINALIZE_STAGED, PH_PSGD_ORTHO_BLOCK, PH_SGD_TILES, PH_BATCH_ACCUMULATE, PH_BATCH_AVERAGE, PH_DETECT_BATCH,
   PH_PSGD_PFOLD, PH_VEC_EXCHANGE, PH_PSGD_QMERGE, PH_TOPK_DECOMPRESS_PACKED, PH_TOPK_FLUSH,
   PH_MOMENTS_PARTIAL, PH_MOMENTS_FINAL,
+  PH_ADAMW, PH_ADAMW_8BIT, PH_CLIP_FACTOR,
+  PH_EMB_LOOKUP, PH_EMB_RANK, PH_EMB_KEYS, PH_EMB_HIST, PH_EMB_SCAN, PH_EMB_SCATTER, PH_EMB_SUM, PH_EMB_JOIN,
   PH_COUNT
 };
 
@@ -84,6 +88,7 @@ struct Plan {
   int n_mat = 0;
   int max_rows = 0;  // most rows of any MATRIX layer
   int max_cols = 0;  // most columns of any MATRIX layer
+  long long adam_blocks = 0; // blocks of ACC_ADAMW_BLOCK elements over all layers
   long long vec_floats = 0;  // packed VECTOR elements (each layer starts at a multiple of 4)
   // workspace offsets (bytes)
   size_t o_qred_items = 0;
@@ -114,7 +119,8 @@ struct acc_ctx {
   int* d_vec_tiles = nullptr;
   int* d_mat_tiles = nullptr;
   int* d_status = nullptr;           // 64 words: [0] device-side error flag (0 = none), see acc_device_status;
-                                     // [8], [9] tile ticket and finished-block count of the pipelined first PowerSGD pass
+                                     // [8], [9] tile ticket and finished-block count of the pipelined first PowerSGD pass,
+                                     // [10] finished-block count of the AdamW kernels
   float4* d_part = nullptr;
   float4* d_ppart = nullptr;         // partial rows of P, one slot per tile a row touches
   int* d_pending = nullptr;          // lazy PowerSGD: rank of the residual not yet applied to err, per layer
@@ -185,6 +191,20 @@ cudaError_t launch_batch_average(acc_ctx* ctx, const float* acc, int n_accum, fl
                                  cudaStream_t s);
 cudaError_t launch_detect_batch(acc_ctx* ctx, const double* n2_layers, double* n2_prev, float lr_curr, float lr_next,
                                 int b_low, int b_high, int32_t* batch, float* lr_scale, cudaStream_t s);
+
+cudaError_t launch_adamw(acc_ctx* ctx, const float* d, float* params, float* m, float* v, int64_t* step,
+                         const double* hyper, const float* factor, uint16_t* low, int flags, cudaStream_t s);
+cudaError_t launch_adamw_8bit(acc_ctx* ctx, const float* d, float* params, uint8_t* m_code, uint8_t* r_code,
+                              uint8_t* m_scale, uint8_t* r_scale, int64_t* step, const double* hyper,
+                              const float* factor, uint16_t* low, uint32_t seed, int flags, cudaStream_t s);
+cudaError_t launch_clip_factor(acc_ctx* ctx, const double* n2_layers, double max_norm, float* factor, double* norm,
+                               cudaStream_t s);
+size_t embedding_workspace(const acc_ctx* ctx, int layer, long long n);
+cudaError_t launch_embedding_lookup(acc_ctx* ctx, int layer, const float* params, const void* tokens, bool tok64,
+                                    long long n, float scale, void* out, bool bf16, cudaStream_t s);
+cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, bool tok64, long long n, float scale,
+                                  const void* dy, bool bf16, float* grads, int accumulate, void* workspace,
+                                  cudaStream_t s);
 
 // Brackets one kernel launch with CUDA events on its stream when profiling is on; counts the launch.
 struct PhaseTimer {

@@ -1,0 +1,272 @@
+"""The embedding's lookup and gradient against the fp64 oracle, through the C-ABI.
+
+Tolerances.  Lookup: one fp32 product, rounded once more to bf16: equal to the same two roundings in torch, bit for bit.
+Gradient: u = 2^-24.  A row with k tokens is a sum of k values in fp32; it passes at most 32 additions in the first level
+and 64 in each of the levels above (ceil(log32 n) - 1 of them), at most k in all, each with an error of at most u times the
+sum of the magnitudes; the scale is one fma more (2 u of the result with accumulation: the product is exact inside).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import training_oracle as tor
+from paper_2010_16248_b200 import binding, workloads as wl
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _ctx(rows, cols, W, before=True):
+    """The embedding as the middle layer of three, so that neighbours would show a stray write."""
+    table = wl.make_table(([("v", (5,))] if before else []) + [("emb", (rows, cols)), ("after", (3, 7))])
+    return table, binding.Context(table, W), table.names.index("emb")
+
+
+def _slice(table, layer):
+    o = int(table.offset[layer])
+    return slice(o, o + int(table.rows[layer]) * int(table.cols[layer]))
+
+
+def _tokens(rng, W, n, rows, kind, dtype=torch.int64):
+    if kind == "zipf":
+        t = np.minimum((rng.pareto(0.7, (W, n)) * 2).astype(np.int64), rows - 1)
+        t = rng.permutation(rows)[t]
+    elif kind == "same":
+        t = np.full((W, n), rows - 1)
+    elif kind == "padding":
+        t = np.full((W, n), -1)
+    else:
+        t = rng.integers(0, rows, (W, n))
+        if kind == "padded":
+            t = np.where(rng.random((W, n)) < 0.3, -1 - rng.integers(0, 5, (W, n)), t)
+    return torch.from_numpy(np.asarray(t)).to(dtype).cuda()
+
+
+LOOKUPS = [(1, 1, 1), (2, 3, 5), (7, 8, 1), (50, 7, 33), (257, 64, 700), (3000, 650, 701), (41, 1030, 64), (5, 2, 0), (9, 4, 8),
+           (70000, 5, 1000)]
+
+
+@pytest.mark.parametrize("rows,cols,n", LOOKUPS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tok", [torch.int32, torch.int64])
+def test_lookup(rows, cols, n, dtype, tok):
+    rng = np.random.default_rng(rows + n)
+    table, ctx, layer = _ctx(rows, cols, 1)
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    params = torch.randn(table.stride, generator=g, device="cuda")
+    tokens = _tokens(rng, 1, n, rows, "padded", tok)[0]
+    out = torch.full((n, cols), 77.0, dtype=dtype, device="cuda")
+    ctx.acc_embedding_lookup(layer, params, tokens, out, scale=1.7)
+    emb = params[_slice(table, layer)].view(rows, cols)
+    want = (emb[tokens.clamp(min=0).long()] * np.float32(1.7)).to(dtype)
+    want[tokens < 0] = 0
+    assert torch.equal(out, want)
+    half_step = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8  # of the type; the scale itself was rounded to fp32
+    exact = tor.embedding_lookup(emb.cpu().numpy(), tokens.cpu().numpy(), float(np.float32(1.7)))
+    assert (np.abs(out.double().cpu().numpy() - exact) <= (half_step + 1.01 * U) * np.abs(exact)).all()
+    assert ctx.last_launch_count() == (1 if n else 0) and ctx.acc_device_status() == 0
+
+
+def _check_grad(table, ctx, layer, tokens, dy, grads0, grads, scale, accumulate):
+    rows, cols = int(table.rows[layer]), int(table.cols[layer])
+    sl = _slice(table, layer)
+    W, n = tokens.shape
+    levels = 0
+    c = n
+    while c > 32:
+        c = (c + 31) // 32
+        levels += 1
+    most = 32 + 64 * levels
+    for w in range(W):
+        t = tokens[w].cpu().numpy()
+        y = dy[w].float().cpu().numpy()
+        G, S, K = tor.embedding_grad(t, y, rows, float(np.float32(scale)))
+        base = grads0[w, sl].double().cpu().numpy().reshape(rows, cols) if accumulate else 0.0
+        want = base + G
+        got = grads[w, sl].double().cpu().numpy().reshape(rows, cols)
+        bound = 1.01 * U * (np.minimum(np.maximum(K - 1, 0), most)[:, None] * S + np.abs(G) + np.abs(want))
+        bad = ~(np.abs(got - want) <= bound)
+        assert not bad.any(), (w, np.argwhere(bad)[:4], got[bad][:4], want[bad][:4])
+        if accumulate:  # rows without a token keep their bits
+            still = K == 0
+            assert np.array_equal(got[still], base[still])
+        else:
+            assert np.array_equal(got[K == 0], np.zeros_like(got[K == 0]))
+    outside = torch.ones(grads.shape[1], dtype=torch.bool, device="cuda")
+    outside[sl] = False
+    assert torch.equal(grads[:, outside], grads0[:, outside])
+
+
+def _run_grad(rows, cols, W, n, kind, dtype=torch.float32, tok=torch.int64, scale=1.0, accumulate=False, seed=0):
+    rng = np.random.default_rng(seed + 31 * n + rows)
+    table, ctx, layer = _ctx(rows, cols, W)
+    g = torch.Generator(device="cuda").manual_seed(seed + n)
+    tokens = _tokens(rng, W, n, rows, kind, tok)
+    dy = torch.randn(W, n, cols, generator=g, device="cuda")
+    dy = torch.where((tokens < 0)[..., None], float("nan"), dy).to(dtype)  # what lies at padding is not read
+    grads0 = torch.randn(W, table.stride, generator=g, device="cuda")
+    grads = grads0.clone()
+    ws = ctx.new_embedding_workspace(layer, n)
+    ws.random_(0, 256, generator=g)
+    ctx.acc_embedding_grad(layer, tokens, dy, grads, scale=scale, accumulate=accumulate, workspace=ws)
+    assert ctx.acc_device_status() == 0
+    _check_grad(table, ctx, layer, tokens, dy, grads0, grads, scale, accumulate)
+    again = grads0.clone()
+    ws.random_(0, 256, generator=g)
+    ctx.acc_embedding_grad(layer, tokens, dy, again, scale=scale, accumulate=accumulate, workspace=ws)
+    assert torch.equal(grads, again)  # bit-reproducible, whatever the workspace held
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 31, 32, 33, 63, 64, 65, 255, 256, 257, 700, 1025, 2047, 2048, 2049, 4097, 5000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_lengths(n, accumulate):
+    _run_grad(50, 6, 2, n, "padded", scale=2.5, accumulate=accumulate)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 4), (2, 3), (300, 2), (257, 7), (256, 5), (255, 64), (65536, 3), (70000, 4),
+                                       (33, 650), (20, 1030), (12, 513)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [37, 2500])
+def test_grad_tables(rows, cols, dtype, n):
+    _run_grad(rows, cols, 2, n, "uniform", dtype=dtype, tok=torch.int32, accumulate=n == 37)
+
+
+@pytest.mark.parametrize("kind", ["zipf", "same", "padding"])
+@pytest.mark.parametrize("n", [40, 1500, 40000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_distributions(kind, n, accumulate):
+    _run_grad(1000, 12, 3, n, kind, dtype=torch.bfloat16, scale=0.5, accumulate=accumulate)
+
+
+def test_grad_layer_of_many_pieces_and_one_worker():
+    _run_grad(40009, 13, 1, 900, "zipf")
+
+
+def test_a_token_beyond_the_table_is_reported_and_reads_nothing():
+    table, ctx, layer = _ctx(10, 6, 2)
+    params = torch.randn(table.stride, device="cuda")
+    for tok in (torch.int32, torch.int64):
+        tokens = torch.tensor([[1, 10, 3], [2 ** 31 - 1, 0, 9]], dtype=tok, device="cuda")
+        if tok == torch.int64:
+            tokens[1, 0] = 2 ** 32 + 1  # must not be taken for row 1
+        inside = torch.tensor([[True, False, True], [False, True, True]], device="cuda")
+        out = torch.full((2, 3, 6), 5.0, device="cuda")
+        ctx.acc_embedding_lookup(layer, params, tokens, out)
+        assert ctx.acc_device_status() == binding.ACC_EINDEX
+        ctx.acc_reset_device_status()
+        want = params[_slice(table, layer)].view(10, 6)[torch.where(inside, tokens, 0).long()]
+        assert torch.equal(out, torch.where(inside[..., None], want, 0.0))
+        for n in (3, 2100):
+            pad = torch.cat([tokens, torch.full((2, n - 3), -1, dtype=tok, device="cuda")], 1).contiguous()
+            dy = torch.ones(2, n, 6, device="cuda")
+            grads = torch.zeros(2, table.stride, device="cuda")
+            ctx.acc_embedding_grad(layer, pad, dy, grads, workspace=ctx.new_embedding_workspace(layer, n))
+            assert ctx.acc_device_status() == binding.ACC_EINDEX
+            ctx.acc_reset_device_status()
+            rows = grads[:, _slice(table, layer)].view(2, 10, 6).sum(2).cpu().numpy() / 6
+            assert np.array_equal(rows, [[0, 1, 0, 1, 0, 0, 0, 0, 0, 0], [1, 0, 0, 0, 0, 0, 0, 0, 0, 1]])
+    assert ctx.acc_device_status() == 0
+
+
+def test_gradient_agrees_with_differences_of_the_lookup():
+    """d/dE <dy, lookup(E)> by central differences in fp64 over the lookup's own fp32 outputs: the lookup is linear, so the
+    difference over a step of 2^-3 is exact up to the roundings of the outputs (u times their size, over the step)."""
+    rows, cols, n = 6, 4, 9
+    table, ctx, layer = _ctx(rows, cols, 1)
+    sl = _slice(table, layer)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    params = torch.randn(table.stride, generator=g, device="cuda")
+    tokens = torch.tensor([[0, 3, 3, 5, -1, 0, 3, 2, 2]], device="cuda")
+    dy = torch.randn(1, n, cols, generator=g, device="cuda")
+    grads = torch.zeros(1, table.stride, device="cuda")
+    ctx.acc_embedding_grad(layer, tokens, dy, grads, scale=1.5, workspace=ctx.new_embedding_workspace(layer, n))
+    out = torch.empty(1, n, cols, device="cuda")
+    h = 2.0 ** -3
+    for j in range(rows * cols):
+        vals = []
+        for sign in (1, -1):
+            p = params.clone()
+            p[sl.start + j] += sign * h
+            ctx.acc_embedding_lookup(layer, p, tokens, out, scale=1.5)
+            vals.append(float((out.double() * dy.double()).sum()))
+        # 9 outputs of size < 10, each |dy| < 5, rounded parameters and products: 2 u a side
+        assert abs((vals[0] - vals[1]) / (2 * h) - float(grads[0, sl.start + j])) < 9 * 10 * 5 * 4 * U / h
+
+
+def test_streams_graphs_and_shared_buffers():
+    """Two calls in flight on two streams with their own workspaces; a captured forward and backward pass, replayed on new
+    tokens written into the same buffers."""
+    rows, cols, W, n = 500, 10, 2, 3000
+    table, ctx, layer = _ctx(rows, cols, W)
+    rng = np.random.default_rng(1)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    sets = [(_tokens(rng, W, n, rows, "zipf"), torch.randn(W, n, cols, generator=g, device="cuda")) for _ in range(2)]
+    zero = torch.zeros(W, table.stride, device="cuda")
+    want = []
+    for tokens, dy in sets:
+        out = zero.clone()
+        ctx.acc_embedding_grad(layer, tokens, dy, out, workspace=ctx.new_embedding_workspace(layer, n))
+        want.append(out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    spaces = [ctx.new_embedding_workspace(layer, n) for _ in sets]
+    outs = [zero.clone() for _ in sets]
+    torch.cuda.synchronize()
+    for s, ws, out, (tokens, dy) in zip(streams, spaces, outs, sets):
+        ctx.acc_embedding_grad(layer, tokens, dy, out, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, outs))
+    tokens, dy = sets[0][0].clone(), sets[0][1].clone()
+    out = zero.clone()
+    params = torch.randn(table.stride, generator=g, device="cuda")
+    y = torch.zeros(W, n, cols, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.acc_embedding_lookup(layer, params, tokens, y)
+        ctx.acc_embedding_grad(layer, tokens, dy, out, workspace=spaces[0])
+    for k in (1, 0):
+        tokens.copy_(sets[k][0])
+        dy.copy_(sets[k][1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[k])
+        assert torch.equal(y, params[_slice(table, layer)].view(rows, cols)[tokens])
+
+
+def test_refusals():
+    table, ctx, layer = _ctx(10, 6, 2)
+    lib = binding.lib()
+    tokens = torch.zeros(2, 4, dtype=torch.int64, device="cuda")
+    dy = torch.zeros(2, 4, 6, device="cuda")
+    grads = torch.zeros(2, table.stride, device="cuda")
+    ws = ctx.new_embedding_workspace(layer, 4)
+    with pytest.raises(binding.AccError) as e:
+        ctx.acc_embedding_grad(layer, tokens, dy, grads, workspace=None)
+    assert e.value.status == 3
+    with pytest.raises(binding.AccError) as e:
+        ctx.acc_embedding_grad(layer, tokens, dy, grads, workspace=ws[:-256])
+    assert e.value.status == 3
+    with pytest.raises(binding.AccError) as e:
+        ctx.acc_embedding_grad(layer, tokens, dy, grads, workspace=torch.zeros(ws.numel() + 256, dtype=torch.uint8, device="cuda")[16:])
+    assert e.value.status == 2
+    wide = torch.zeros(2 * 4 * 6 + 4, device="cuda")
+    with pytest.raises(binding.AccError) as e:
+        ctx.acc_embedding_grad(layer, tokens, wide[1:49].view(2, 4, 6), grads, workspace=ws)
+    assert e.value.status == 2
+    with pytest.raises(binding.AccError) as e:
+        ctx.acc_embedding_lookup(layer, grads[0], tokens, wide[1:49].view(2, 4, 6))
+    assert e.value.status == 2
+    t, d, g, w = tokens.data_ptr(), dy.data_ptr(), grads.data_ptr(), ws.data_ptr()
+    n, big = ws.numel(), 1 << 40
+    assert lib.acc_embedding_grad(ctx._h, 0, t, 1, 4, 1.0, d, 0, g, 0, w, n, None) == 1           # a VECTOR layer
+    assert lib.acc_embedding_grad(ctx._h, 3, t, 1, 4, 1.0, d, 0, g, 0, w, n, None) == 1           # no layer
+    assert lib.acc_embedding_grad(ctx._h, -1, t, 1, 4, 1.0, d, 0, g, 0, w, n, None) == 1
+    assert lib.acc_embedding_grad(ctx._h, layer, t, 2, 4, 1.0, d, 0, g, 0, w, n, None) == 1       # types
+    assert lib.acc_embedding_grad(ctx._h, layer, t, 1, 4, 1.0, d, 2, g, 0, w, n, None) == 1
+    assert lib.acc_embedding_grad(ctx._h, layer, t, 1, -1, 1.0, d, 0, g, 0, w, n, None) == 1      # lengths
+    assert lib.acc_embedding_grad(ctx._h, layer, t, 1, (1 << 27) + 1, 1.0, d, 0, g, 0, w, big, None) == 1
+    assert lib.acc_embedding_grad(ctx._h, layer, None, 1, 4, 1.0, d, 0, g, 0, w, n, None) == 1
+    assert lib.acc_embedding_grad(ctx._h, layer, t + 4, 1, 4, 1.0, d, 0, g, 0, w, n, None) == 2
+    assert lib.acc_embedding_lookup(ctx._h, layer, g, t, 1, (1 << 28) + 1, 1.0, d, 0, None) == 1
+    assert lib.acc_embedding_lookup(ctx._h, layer, None, t, 1, 4, 1.0, d, 0, None) == 1
