@@ -171,12 +171,9 @@ def acc_sumsq_static(buf: torch.Tensor, n: int, norm2: torch.Tensor, stream=None
         raise AccError(st, "acc_sumsq_static")
 
 
-class _Arg:
+def _Arg(t, dtype, min_numel, what):
     """One tensor argument of a call with what the call requires of it."""
-    __slots__ = ("t", "dtype", "min_numel", "what")
-
-    def __init__(self, t, dtype, min_numel, what):
-        self.t, self.dtype, self.min_numel, self.what = t, dtype, int(min_numel), what
+    return t, dtype, min_numel, what
 
 
 def _marshal(device, *items):
@@ -184,37 +181,51 @@ def _marshal(device, *items):
     cannot see.  First every tensor's dtype, contiguity and length -- the kernels index by the context's layout, so
     a short tensor would be an out-of-bounds device access, not an exception -- then that every tensor lives on
     the GPU the call runs on (there is no CPU path)."""
-    for a in items:
-        if not isinstance(a, _Arg) or a.t is None:
-            continue
-        t = a.t
-        if not isinstance(t, torch.Tensor):
-            raise ValueError(f"{a.what}: expected a torch tensor")
-        if t.dtype != a.dtype:
-            raise ValueError(f"{a.what}: expected dtype {a.dtype}, got {t.dtype}")
-        if not t.is_contiguous():
-            raise ValueError(f"{a.what}: expected a contiguous tensor")
-        if t.numel() < a.min_numel:
-            raise ValueError(f"{a.what}: {t.numel()} elements, the call needs at least {a.min_numel}")
+    index = None if device is None else device.index
     out = []
     for a in items:
-        if not isinstance(a, _Arg):
+        if type(a) is not tuple:
             out.append(a)
             continue
-        if a.t is None:
+        t, dtype, least, _ = a
+        if t is None:
             out.append(None)
             continue
-        if not a.t.is_cuda:
-            raise ValueError(f"{a.what}: expected a CUDA tensor (the library has no CPU path)")
-        if device is not None and device.index is not None and a.t.device.index != device.index:
-            raise ValueError(f"{a.what}: lives on {a.t.device}, the context on {device}")
-        out.append(a.t.data_ptr())
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() < least or not t.is_contiguous():
+            _refuse(device, items)
+        on = t.get_device()  # -1: not on a GPU
+        if on < 0 or (index is not None and on != index):
+            _refuse(device, items)
+        out.append(t.data_ptr())
     return out
 
 
-def _stream(stream) -> Optional[int]:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream or None
+def _refuse(device, items):
+    """Raises for the first thing that is wrong with the tensors of a call."""
+    args = [a for a in items if type(a) is tuple and a[0] is not None]
+    for t, dtype, least, what in args:
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{what}: expected a torch tensor")
+        if t.dtype != dtype:
+            raise ValueError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous tensor")
+        if t.numel() < least:
+            raise ValueError(f"{what}: {t.numel()} elements, the call needs at least {least}")
+    for t, _, _, what in args:
+        if not t.is_cuda:
+            raise ValueError(f"{what}: expected a CUDA tensor (the library has no CPU path)")
+        if device is not None and device.index is not None and t.device.index != device.index:
+            raise ValueError(f"{what}: lives on {t.device}, the context on {device}")
+    raise ValueError("a tensor argument of the call cannot be used")
+
+
+def _stream(stream, index=None) -> Optional[int]:
+    """Address of ``stream``, or of the current stream of device ``index`` (of the current device)."""
+    if stream is not None:
+        return stream.cuda_stream or None
+    # (torch.cuda.current_stream builds a Stream object, 3 us of a 10 us call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if index is None else index) or None
 
 
 class Context:
@@ -278,11 +289,14 @@ class Context:
     def _call(self, name, *items, stream=None):
         """Checks and marshals the tensor arguments, then calls entry point ``name`` on this context."""
         args = _marshal(self.device, *items)
-        if self.device.index is not None and self.device.index != torch.cuda.current_device():
-            with torch.cuda.device(self.device):  # kernels launch on the current device
-                self._check(getattr(lib(), name)(self._h, *args, _stream(stream)), name)
-            return
-        self._check(getattr(lib(), name)(self._h, *args, _stream(stream)), name)
+        index = self.device.index
+        if index is None or index == torch.cuda.current_device():
+            st = getattr(lib(), name)(self._h, *args, _stream(stream, index))
+        else:
+            with torch.cuda.device(index):  # kernels launch on the current device
+                st = getattr(lib(), name)(self._h, *args, _stream(stream, index))
+        if st != ACC_OK:
+            raise AccError(st, name)
 
     # --- argument checks: every device buffer must hold what the context's layout will index -----------------
     def _f(self, t, n, what):

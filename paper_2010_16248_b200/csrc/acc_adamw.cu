@@ -7,7 +7,7 @@
 namespace acc {
 
 // The step's coefficients, worked out once per block in fp64 from the caller's doubles and the step count.
-struct AdamCoef {
+struct AdamCoef {  // 11 words
   float f;                 // factor on the gradient
   float b1, ob1, b2, ob2;  // beta1, 1 - beta1, beta2, 1 - beta2
   float lrwd;              // lr * weight_decay
@@ -15,6 +15,7 @@ struct AdamCoef {
   float rc2;               // 1 / sqrt(1 - beta2^t)
   float eps;
   unsigned key;            // of this step's random numbers (8-bit states)
+  int skip;                // the factor is not finite: nothing changes (written by adamw_coef_kernel)
 };
 
 // b^t by squaring: t has at most 63 bits, so the relative error stays under 126 * 2^-53.
@@ -29,19 +30,21 @@ __device__ __forceinline__ double pow_int(double b, long long t) {
 
 // 32-bit integer mixing (two rounds of xor-shift and multiply, C. Wellons' constants): a bijection, so distinct elements
 // of one step draw distinct words.
-__host__ __device__ __forceinline__ unsigned mix32(unsigned x) {
+__device__ __forceinline__ unsigned mix32_open(unsigned x) {  // all but the last fold
   x ^= x >> 16;
   x *= 0x7feb352du;
   x ^= x >> 15;
-  x *= 0x846ca68bu;
+  return x * 0x846ca68bu;
+}
+__device__ __forceinline__ unsigned mix32(unsigned x) {
+  x = mix32_open(x);
   return x ^ (x >> 16);
 }
 
-// Two lanes take one power each; the result is valid for every thread after the next __syncthreads.
-__device__ __forceinline__ void adam_coef(AdamCoef* c, const double* __restrict__ hyper, const long long* step, float f,
+// Two lanes take one power each.
+__device__ __forceinline__ void adam_coef(AdamCoef* c, const double* __restrict__ hyper, long long t, float f,
                                           unsigned seed) {
   if (threadIdx.x >= 2) return;
-  const long long t = *step + 1;
   const double lr = hyper[0], b = hyper[1 + threadIdx.x];
   const double corr = 1.0 - pow_int(b, t);
   if (threadIdx.x == 0) {
@@ -59,16 +62,6 @@ __device__ __forceinline__ void adam_coef(AdamCoef* c, const double* __restrict_
   }
 }
 
-// Every block has read the step count before it arrives here, so the last one may advance it; it also leaves the ticket
-// at zero for the next call.
-__device__ __forceinline__ void adam_finish(long long* step, unsigned* ticket) {
-  __syncthreads();
-  if (threadIdx.x == 0 && atomicAdd(ticket, 1u) == gridDim.x - 1) {
-    *ticket = 0;
-    *step += 1;
-  }
-}
-
 // A factor that is not finite means that the gradient's norm was not: the call then changes nothing.
 __device__ __forceinline__ float adam_factor(const float* factor, bool& skip) {
   const float f = factor != nullptr ? __ldg(factor) : 1.f;
@@ -76,14 +69,34 @@ __device__ __forceinline__ float adam_factor(const float* factor, bool& skip) {
   return f;
 }
 
-// m, v (or r with v = r^2) in, new m, v out, in fp32; returns the new x.
-__device__ __forceinline__ float adam_update(float d, float x, float& m, float& v, float& r, const AdamCoef& c,
-                                             float lrwd) {
+// Root and quotient as one special-function instruction each (sqrt.approx: relative error 2^-23; div.approx: 2 ulp for
+// divisors in [2^-126, 2^126]): the update's own roundings are of that size, and the correctly rounded forms with their
+// range checks were a fifth of the 8-bit kernel's instructions.
+__device__ __forceinline__ float sqrt_fast(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float div_fast(float a, float b) {
+  float r;
+  asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN where either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// The update of one element: the old moments arrive as factors, beta1 m = ka a and beta2 v = kb b; m, v, r = sqrt(v) are
+// the new ones in fp32; returns the new parameter.
+__device__ __forceinline__ float adam_update(float d, float x, float a, float ka, float b, float kb, float& m, float& v,
+                                             float& r, const AdamCoef& c, float lrwd) {
   const float g = c.f * d;
-  m = fmaf(c.b1, m, c.ob1 * g);
-  v = fmaf(c.b2, v, c.ob2 * (g * g));
-  r = sqrtf(v);
-  return fmaf(-c.size, m / fmaf(r, c.rc2, c.eps), fmaf(-lrwd, x, x));
+  m = fmaf(ka, a, c.ob1 * g);
+  v = fmaf(kb, b, c.ob2 * (g * g));
+  r = sqrt_fast(v);
+  return fmaf(-c.size, div_fast(m, fmaf(r, c.rc2, c.eps)), fmaf(-lrwd, x, x));
 }
 
 __device__ __forceinline__ uint2 bf16x4(const float4 v) {
@@ -91,55 +104,125 @@ __device__ __forceinline__ uint2 bf16x4(const float4 v) {
   return make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
 }
 
-// States in 32 bits: 16 B read and 12 B written per parameter, 15 operations: bound by HBM.  A block takes `share` elements
-// of a tile, four at a time per thread.
-__global__ void __launch_bounds__(256)
-adamw_kernel(const DevLayer* __restrict__ layers, const Tile* __restrict__ tiles, int split, const float* __restrict__ d,
-             float* __restrict__ params, float* __restrict__ ms, float* __restrict__ vs, long long* step,
-             const double* __restrict__ hyper, const float* __restrict__ factor, unsigned short* __restrict__ low,
-             int flags, unsigned* ticket) {
-  __shared__ AdamCoef sc;
+// A warp takes one unit of 256 elements of a tile (a unit never spans layers, and with states in 8 bits it is a block of its
+// own scale), eight elements per lane as two vectors of four at 4 lane and 128 + 4 lane: full lines, and a block's largest
+// magnitude is one warp reduction away.  All of a warp's loads go out at once, before the coefficients are looked at.
+//
+// Coefficients.  Working them out takes fp64 powers, a quotient and a root, about 1 us.  Where all blocks are resident at
+// once (ONE), each does so itself behind its loads, and the last block to finish advances the step count.  Larger tables,
+// whose blocks follow one another on an SM and would pay that time again and again, take them from a kernel of one warp
+// launched ahead (50.1 M parameters in 8 bits: 208 us with the coefficients in every block, 142 us so); the update's blocks
+// start beside it and wait for it behind their loads (programmatic dependent launch).
+constexpr int kUnit = ACC_ADAMW_BLOCK, kUnitsPerTile = kTile / kUnit, kBlocksPerTile = kUnitsPerTile / 8;
+
+__global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* __restrict__ hyper,
+                                  const float* __restrict__ factor, unsigned seed) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   bool skip;
   const float f = adam_factor(factor, skip);
-  if (skip) return;
-  const Tile t = tiles[blockIdx.x / split];
-  const int share = kTile / split, first = (int)(blockIdx.x % split) * share;
-  if (first < t.nelem) adam_coef(&sc, hyper, step, f, 0u);
-  const DevLayer& L = layers[t.layer];
-  const long long base = L.offset + t.elem0;
-  const int end = min(first + share, t.nelem);
-  const bool decay = L.kind == ACC_MATRIX || !(flags & ACC_ADAMW_NO_VECTOR_DECAY);
+  const long long t = *step + 1;
+  adam_coef(c, hyper, t, f, seed);
+  __syncwarp();
+  if (threadIdx.x == 0) {
+    c->skip = skip;
+    if (!skip) *step = t;
+  }
+}
+
+// The block's coefficients, from `pre` or worked out here; false where nothing is to change.
+template <bool ONE>
+__device__ __forceinline__ bool adam_begin(AdamCoef& c, AdamCoef* sc, const AdamCoef* pre, const long long* step,
+                                           const double* __restrict__ hyper, const float* __restrict__ factor,
+                                           unsigned seed) {
+  if (ONE) {
+    bool skip;
+    const float f = adam_factor(factor, skip);
+    if (skip) return false;
+    adam_coef(sc, hyper, *step + 1, f, seed);
+    __syncthreads();
+    c = *sc;
+    return true;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  c = *pre;
+  return c.skip == 0;
+}
+
+// ONE: every block has read the step count before it arrives here, so the last one may advance it; it also leaves the
+// ticket at zero for the next call.
+template <bool ONE>
+__device__ __forceinline__ void adam_finish(long long* step, unsigned* ticket) {
+  if (!ONE) return;
   __syncthreads();
-  const AdamCoef c = sc;
-  const float lrwd = decay ? c.lrwd : 0.f;
-  for (int e = first + 4 * (int)threadIdx.x; e < end; e += 4 * 256) {
+  if (threadIdx.x == 0 && atomicAdd(ticket, 1u) == gridDim.x - 1) {
+    *ticket = 0;
+    *step += 1;
+  }
+}
+
+// A warp's unit: where it starts, how many elements it has (<= 0: none), which scale it holds.
+struct AdamUnit { long long base, block; int n; bool decay; };
+__device__ __forceinline__ AdamUnit adam_unit(const FlatTile* __restrict__ tiles, int flags) {
+  const FlatTile t = tiles[blockIdx.x / kBlocksPerTile];
+  const int i = (int)(blockIdx.x % kBlocksPerTile) * 8 + (int)(threadIdx.x >> 5), e = i * kUnit;
+  return AdamUnit{t.base + e, t.block0 + i, min(t.nelem - e, kUnit), t.matrix || !(flags & ACC_ADAMW_NO_VECTOR_DECAY)};
+}
+
+// States in 32 bits: 16 B read and 12 B written per parameter, some 15 operations: bound by HBM (50.1 M parameters: 213 us,
+// 6.6 TB/s; 234 us with a block per tile of 8192 elements and a loop over it, 252 us as persistent blocks).
+template <bool ONE>
+__global__ void __launch_bounds__(256)
+adamw_kernel(const FlatTile* __restrict__ tiles, const float* __restrict__ d, float* params, float* ms, float* vs,
+             const AdamCoef* pre, long long* step, const double* __restrict__ hyper, const float* __restrict__ factor,
+             unsigned short* low, int flags, unsigned* ticket) {
+  __shared__ AdamCoef sc;
+  const int lane = threadIdx.x & 31;
+  const AdamUnit u = adam_unit(tiles, flags);
+  float4 gs[2], xs[2], mv[2], vv[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int e = 128 * h + 4 * lane;
     // (layers start at multiples of four elements and the buffers end at one, so whole vectors are in bounds)
-    const float4 dv = ld_stream4(d + base + e);
-    float4 x = *reinterpret_cast<const float4*>(params + base + e);
-    float4 m = ld_stream4(ms + base + e), v = ld_stream4(vs + base + e);
+    if (e < u.n) {
+      gs[h] = ld_stream4(d + u.base + e);
+      xs[h] = *reinterpret_cast<const float4*>(params + u.base + e);
+      mv[h] = ld_stream4(ms + u.base + e);
+      vv[h] = ld_stream4(vs + u.base + e);
+    }
+  }
+  AdamCoef c;
+  if (!adam_begin<ONE>(c, &sc, pre, step, hyper, factor, 0u)) return;
+  const float lrwd = u.decay ? c.lrwd : 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int e = 128 * h + 4 * lane;
+    if (e >= u.n) continue;
+    float4 x = xs[h], m = mv[h], v = vv[h];
+    const float4 g = gs[h];
     float r;
-    x.x = adam_update(dv.x, x.x, m.x, v.x, r, c, lrwd);
-    x.y = adam_update(dv.y, x.y, m.y, v.y, r, c, lrwd);
-    x.z = adam_update(dv.z, x.z, m.z, v.z, r, c, lrwd);
-    x.w = adam_update(dv.w, x.w, m.w, v.w, r, c, lrwd);
-    if (e + 4 <= end) {
-      *reinterpret_cast<float4*>(params + base + e) = x;
-      st_stream4(ms + base + e, m);
-      st_stream4(vs + base + e, v);
-      if (low != nullptr) *reinterpret_cast<uint2*>(low + base + e) = bf16x4(x);
+    x.x = adam_update(g.x, x.x, m.x, c.b1, v.x, c.b2, m.x, v.x, r, c, lrwd);
+    x.y = adam_update(g.y, x.y, m.y, c.b1, v.y, c.b2, m.y, v.y, r, c, lrwd);
+    x.z = adam_update(g.z, x.z, m.z, c.b1, v.z, c.b2, m.z, v.z, r, c, lrwd);
+    x.w = adam_update(g.w, x.w, m.w, c.b1, v.w, c.b2, m.w, v.w, r, c, lrwd);
+    const long long at = u.base + e;
+    if (e + 4 <= u.n) {
+      *reinterpret_cast<float4*>(params + at) = x;
+      st_stream4(ms + at, m);
+      st_stream4(vs + at, v);
+      if (low != nullptr) *reinterpret_cast<uint2*>(low + at) = bf16x4(x);
     } else {
-      const float xs[3] = {x.x, x.y, x.z}, mv[3] = {m.x, m.y, m.z}, vv[3] = {v.x, v.y, v.z};
+      const float x3[3] = {x.x, x.y, x.z}, m3[3] = {m.x, m.y, m.z}, v3[3] = {v.x, v.y, v.z};
 #pragma unroll
       for (int k = 0; k < 3; ++k)
-        if (e + k < end) {
-          params[base + e + k] = xs[k];
-          ms[base + e + k] = mv[k];
-          vs[base + e + k] = vv[k];
-          if (low != nullptr) low[base + e + k] = __bfloat16_as_ushort(__float2bfloat16_rn(xs[k]));
+        if (e + k < u.n) {
+          params[at + k] = x3[k];
+          ms[at + k] = m3[k];
+          vs[at + k] = v3[k];
+          if (low != nullptr) low[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(x3[k]));
         }
     }
   }
-  adam_finish(step, ticket);
+  adam_finish<ONE>(step, ticket);
 }
 
 // ---- states in 8 bits --------------------------------------------------------------------------------------------
@@ -162,117 +245,151 @@ __device__ __forceinline__ unsigned scale_byte(unsigned top, int lowest) {
 }
 constexpr int kLowestM = 10, kLowestR = 73;
 
-// What a magnitude is multiplied by before its code is taken; 0 where every code of the block is 0.
-__device__ __forceinline__ float inverse_scale(unsigned byte) {
-  return byte == 0u || byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
+// e4m3's exponent bias is 120 below fp32's, so y 2^-120 in fp32 has y's e4m3 code in its bits 20 to 26, subnormals
+// included (fp32's own subnormals begin where e4m3's do), and what rounding cuts below: adding 20 random bits there and
+// cutting rounds up with the probability that the cut bits stand for.  This is the factor 2^(127 - byte - 120), as one
+// float where that is normal; a block of larger values takes 2^-120 first (`big`).
+__device__ __forceinline__ float code_factor(unsigned byte, bool& big) {
+  big = byte > 133u;
+  return byte == 0u || byte == 255u ? 0.f : __uint_as_float((big ? 254u - byte : 134u - byte) << 23);
 }
 
-// e4m3 magnitude of y in [0, 256), rounded up with the probability that the cut bits stand for (16 random bits).
-__device__ __forceinline__ unsigned encode(float y, unsigned rnd) {
-  if (y >= 0.015625f) return ((__float_as_uint(y) + (rnd << 4)) >> 20) - (120u << 3);
-  return (unsigned)floorf(fmaf(y, 512.f, (float)rnd * 0x1p-16f));
-}
-
-__device__ __forceinline__ float4 decode4(unsigned codes, float scale) {
+__device__ __forceinline__ void decode4(unsigned codes, float* out) {
   const __half2 lo(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffffu), __NV_E4M3));
   const __half2 hi(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> 16), __NV_E4M3));
   const float2 a = __half22float2(lo), b = __half22float2(hi);
-  return make_float4(a.x * scale, a.y * scale, b.x * scale, b.y * scale);
+  out[0] = a.x; out[1] = a.y; out[2] = b.x; out[3] = b.y;
 }
 
-// A warp takes a block of 256 elements, eight per lane as two vectors of four (lane's first element 4 lane and 128 + 4
-// lane), so that the block's largest magnitudes are one warp reduction away and every access is a full line.
-// 16.03 B per parameter, bound by HBM.
-__global__ void __launch_bounds__(256)
-adamw_8bit_kernel(const DevLayer* __restrict__ layers, const Tile* __restrict__ tiles, int split,
-                  const float* __restrict__ d, float* __restrict__ params, unsigned char* __restrict__ mc,
-                  unsigned char* __restrict__ rc, unsigned char* __restrict__ msc, unsigned char* __restrict__ rsc,
-                  long long* step, const double* __restrict__ hyper, const float* __restrict__ factor,
-                  unsigned short* __restrict__ low, unsigned seed, int flags, unsigned* ticket) {
-  __shared__ AdamCoef sc;
-  bool skip;
-  const float f = adam_factor(factor, skip);
-  if (skip) return;
-  const Tile t = tiles[blockIdx.x / split];
-  const int share = kTile / split, first = (int)(blockIdx.x % split) * share;
-  if (first < t.nelem) adam_coef(&sc, hyper, step, f, seed);
-  const DevLayer& L = layers[t.layer];
-  const long long base = L.offset + t.elem0;
-  const long long block0 = L.adam_block0 + t.elem0 / ACC_ADAMW_BLOCK;
-  const int end = min(first + share, t.nelem);
-  const bool decay = L.kind == ACC_MATRIX || !(flags & ACC_ADAMW_NO_VECTOR_DECAY);
-  __syncthreads();
-  const AdamCoef c = sc;
-  const float lrwd = decay ? c.lrwd : 0.f;
-  const int lane = threadIdx.x & 31;
-  for (int b0 = first + ACC_ADAMW_BLOCK * (int)(threadIdx.x >> 5); b0 < end; b0 += ACC_ADAMW_BLOCK * 8) {
-    const long long blk = block0 + b0 / ACC_ADAMW_BLOCK;
-    float dv[8], x[8], m[8], r[8];
-    const float sm = scale_of(msc[blk]), sr = scale_of(rsc[blk]);
+// The top bytes of four words.
+__device__ __forceinline__ unsigned top_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
+  return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// 16.03 B per parameter and 60 instructions, issued in some 60 % of the cycles: 50.1 M parameters take 132 us, 6.1 TB/s, the
+// last part of it the wait for loads at 40 warps per SM (48 registers; 142 us at 64 registers and 32 warps).
+struct Adam8Regs { float4 d[2], x[2]; unsigned m[2], r[2], ms, rs; };
+struct Adam8Args {
+  const float* d; float* params; unsigned char* mc; unsigned char* rc; unsigned char* ms; unsigned char* rs;
+  unsigned short* low;
+};
+__device__ __forceinline__ void adam8_load(Adam8Regs& q, const AdamUnit& u, int lane, const Adam8Args& p) {
+  if (u.n <= 0) return;
+  q.ms = p.ms[u.block];
+  q.rs = p.rs[u.block];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int e = b0 + 128 * h + 4 * lane;
-      float4 dd = make_float4(0.f, 0.f, 0.f, 0.f), xx = dd, mm = dd, rr = dd;
-      if (e < end) {
-        dd = ld_stream4(d + base + e);
-        xx = *reinterpret_cast<const float4*>(params + base + e);
-        mm = decode4(__ldcs(reinterpret_cast<const unsigned*>(mc + base + e)), sm);
-        rr = decode4(__ldcs(reinterpret_cast<const unsigned*>(rc + base + e)), sr);
-      }
-      dv[4 * h] = dd.x; dv[4 * h + 1] = dd.y; dv[4 * h + 2] = dd.z; dv[4 * h + 3] = dd.w;
-      x[4 * h] = xx.x; x[4 * h + 1] = xx.y; x[4 * h + 2] = xx.z; x[4 * h + 3] = xx.w;
-      m[4 * h] = mm.x; m[4 * h + 1] = mm.y; m[4 * h + 2] = mm.z; m[4 * h + 3] = mm.w;
-      r[4 * h] = rr.x; r[4 * h + 1] = rr.y; r[4 * h + 2] = rr.z; r[4 * h + 3] = rr.w;
-    }
-    unsigned topm = 0u, topr = 0u;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float v = r[k] * r[k];
-      x[k] = adam_update(dv[k], x[k], m[k], v, r[k], c, lrwd);
-      if (b0 + 128 * (k >> 2) + 4 * lane + (k & 3) < end) {
-        topm = max(topm, __float_as_uint(m[k]) & 0x7fffffffu);
-        topr = max(topr, __float_as_uint(r[k]) & 0x7fffffffu);
-      }
-    }
-    topm = __reduce_max_sync(0xffffffffu, topm);
-    topr = __reduce_max_sync(0xffffffffu, topr);
-    const unsigned bm = scale_byte(topm, kLowestM), br = scale_byte(topr, kLowestR);
-    const float im = inverse_scale(bm), ir = inverse_scale(br);
-    if (lane == 0) { msc[blk] = (unsigned char)bm; rsc[blk] = (unsigned char)br; }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int e = b0 + 128 * h + 4 * lane;
-      unsigned cm = 0u, cr = 0u;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float mk = m[4 * h + k], rk = r[4 * h + k];
-        const unsigned rnd = mix32(c.key ^ (unsigned)(base + e + k));
-        unsigned qm = 0u, qr = 0u;
-        if (bm != 255u) qm = encode(fabsf(mk) * im, rnd & 0xffffu) | (__float_as_uint(mk) >> 31 << 7);
-        if (br != 255u) qr = encode(rk * ir, rnd >> 16);
-        if (qr == 0u && rk > 0.f) qr = 1u;
-        cm |= qm << (8 * k);
-        cr |= qr << (8 * k);
-      }
-      const float4 xo = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
-      if (e + 4 <= end) {
-        *reinterpret_cast<float4*>(params + base + e) = xo;
-        __stcs(reinterpret_cast<unsigned*>(mc + base + e), cm);
-        __stcs(reinterpret_cast<unsigned*>(rc + base + e), cr);
-        if (low != nullptr) *reinterpret_cast<uint2*>(low + base + e) = bf16x4(xo);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-          if (e + k < end) {
-            params[base + e + k] = x[4 * h + k];
-            mc[base + e + k] = (unsigned char)(cm >> (8 * k));
-            rc[base + e + k] = (unsigned char)(cr >> (8 * k));
-            if (low != nullptr) low[base + e + k] = __bfloat16_as_ushort(__float2bfloat16_rn(x[4 * h + k]));
-          }
-      }
+  for (int h = 0; h < 2; ++h) {
+    const int e = 128 * h + 4 * lane;
+    q.d[h] = q.x[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+    q.m[h] = q.r[h] = 0u;
+    if (e < u.n) {
+      q.d[h] = ld_stream4(p.d + u.base + e);
+      q.x[h] = *reinterpret_cast<const float4*>(p.params + u.base + e);
+      q.m[h] = __ldcs(reinterpret_cast<const unsigned*>(p.mc + u.base + e));
+      q.r[h] = __ldcs(reinterpret_cast<const unsigned*>(p.rc + u.base + e));
     }
   }
-  adam_finish(step, ticket);
+}
+
+// FULL: the unit has all of its 256 elements.
+template <bool FULL>
+__device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u, int lane, const Adam8Args& p,
+                                           const AdamCoef& c) {
+  const float lrwd = u.decay ? c.lrwd : 0.f;
+  const float sr = scale_of(q.rs);
+  const float km = scale_of(q.ms) * c.b1, kr = sr * sr * c.b2;  // powers of two: exact
+  float m[8], r[8];
+  float topm = 0.f, topr = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float a[4], b[4];
+    decode4(q.m[h], a);
+    decode4(q.r[h], b);
+    const float dv[4] = {q.d[h].x, q.d[h].y, q.d[h].z, q.d[h].w};
+    float x[4] = {q.x[h].x, q.x[h].y, q.x[h].z, q.x[h].w};
+    const int e = 128 * h + 4 * lane;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = 4 * h + k;
+      float v;
+      x[k] = adam_update(dv[k], x[k], a[k], km, b[k] * b[k], kr, m[i], v, r[i], c, lrwd);
+      if (FULL || e + k < u.n) {
+        topm = max_nan(topm, fabsf(m[i]));
+        topr = max_nan(topr, r[i]);
+      }
+    }
+    const long long at = u.base + e;
+    const float4 xo = make_float4(x[0], x[1], x[2], x[3]);
+    if (FULL || e + 4 <= u.n) {
+      *reinterpret_cast<float4*>(p.params + at) = xo;
+      if (p.low != nullptr) *reinterpret_cast<uint2*>(p.low + at) = bf16x4(xo);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (e + k < u.n) {
+          p.params[at + k] = x[k];
+          if (p.low != nullptr) p.low[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(x[k]));
+        }
+    }
+  }
+  const unsigned bm = scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(topm)), kLowestM);
+  const unsigned br = scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(topr)), kLowestR);
+  bool bigm, bigr;
+  const float fm = code_factor(bm, bigm), fr = code_factor(br, bigr);
+  if (bigm || bigr) {  // (the whole warp; 255 comes here too, and leaves codes that its scale of NaN makes NaN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (bigm) m[i] = bm == 255u ? 0.f : m[i] * 0x1p-120f;
+      if (bigr) r[i] = br == 255u ? 0.f : r[i] * 0x1p-120f;
+    }
+  }
+  if (lane == 0) { p.ms[u.block] = (unsigned char)bm; p.rs[u.block] = (unsigned char)br; }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int e = 128 * h + 4 * lane;
+    // (units start at multiples of four elements, so the element's number is its vector's with k in the low bits)
+    const unsigned seed = c.key ^ (unsigned)(u.base + e);
+    unsigned cm[4], cr[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const unsigned w = mix32_open(seed ^ (unsigned)k), hi = w >> 16;  // random word: its halves are w ^ hi and hi
+      const unsigned tm = __float_as_uint(m[4 * h + k] * fm) + (((w ^ hi) & 0xffffu) << 4);
+      cm[k] = (tm & 0x80000000u) | ((tm << 4) & 0x7fffffffu);
+      const float rk = r[4 * h + k];
+      const float y = rk > 0.f ? fmaxf(rk * fr, 0x1p-129f) : 0.f;  // 2^-129: code 1
+      cr[k] = (__float_as_uint(y) + (hi << 4)) << 4;
+    }
+    const unsigned wm = top_bytes(cm[0], cm[1], cm[2], cm[3]), wr = top_bytes(cr[0], cr[1], cr[2], cr[3]);
+    const long long at = u.base + e;
+    if (FULL || e + 4 <= u.n) {
+      __stcs(reinterpret_cast<unsigned*>(p.mc + at), wm);
+      __stcs(reinterpret_cast<unsigned*>(p.rc + at), wr);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        if (e + k < u.n) {
+          p.mc[at + k] = (unsigned char)(wm >> (8 * k));
+          p.rc[at + k] = (unsigned char)(wr >> (8 * k));
+        }
+    }
+  }
+}
+
+template <bool ONE>
+__global__ void __launch_bounds__(256, 5)
+adamw_8bit_kernel(const FlatTile* __restrict__ tiles, const Adam8Args p, const AdamCoef* pre, long long* step,
+                  const double* __restrict__ hyper, const float* __restrict__ factor, unsigned seed, int flags,
+                  unsigned* ticket) {
+  __shared__ AdamCoef sc;
+  const int lane = threadIdx.x & 31;
+  const AdamUnit u = adam_unit(tiles, flags);
+  Adam8Regs q;
+  adam8_load(q, u, lane, p);
+  AdamCoef c;
+  if (!adam_begin<ONE>(c, &sc, pre, step, hyper, factor, seed)) return;
+  if (u.n == kUnit) adam8_unit<true>(q, u, lane, p, c);
+  else if (u.n > 0) adam8_unit<false>(q, u, lane, p, c);
+  adam_finish<ONE>(step, ticket);
 }
 
 // One block: norm = sqrt(sum of the layers' squared norms, fp64, fixed order); factor = min(1, max_norm / norm), NaN where
@@ -295,36 +412,57 @@ clip_factor_kernel(const double* __restrict__ n2_layers, int n_layers, double ma
   }
 }
 
-// Blocks per tile: small tables are cut finer, so that every SM has work.
-static int tile_split(int n_tiles, int sm_count, int most) {
-  int split = 1;
-  while (split < most && n_tiles * split < 4 * sm_count) split *= 2;
-  return split;
+// Launches an update's kernel over every tile: kernel_one where its blocks all fit at once, else the coefficients' kernel
+// and kernel_many, which starts beside it.
+template <typename... Args>
+static cudaError_t adam_launch(acc_ctx* ctx, int phase, int occupancy, void (*kernel_one)(Args...),
+                               void (*kernel_many)(Args...), int64_t* step, const double* hyper, const float* factor,
+                               unsigned seed, cudaStream_t s, Args... args) {
+  const unsigned grid = (unsigned)ctx->plan.tiles.size() * kBlocksPerTile;
+  const bool one = grid <= (unsigned)(occupancy * ctx->sm_count);
+  if (!one) {
+    PhaseTimer pt(ctx, PH_ADAMW_COEF, s);
+    adamw_coef_kernel<<<1, 32, 0, s>>>(reinterpret_cast<AdamCoef*>(ctx->d_status + kAdamCoefWord),
+                                       reinterpret_cast<long long*>(step), hyper, factor, seed);
+  }
+  PhaseTimer pt(ctx, phase, s);
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = one ? 0 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, one ? kernel_one : kernel_many, args...);
+  return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
 cudaError_t launch_adamw(acc_ctx* ctx, const float* d, float* params, float* m, float* v, int64_t* step,
                          const double* hyper, const float* factor, uint16_t* low, int flags, cudaStream_t s) {
-  const int nt = (int)ctx->plan.tiles.size(), split = tile_split(nt, ctx->sm_count, 8);
-  {
-    PhaseTimer pt(ctx, PH_ADAMW, s);
-    adamw_kernel<<<nt * split, 256, 0, s>>>(ctx->d_layers, ctx->d_tiles, split, d, params, m, v,
-                                            reinterpret_cast<long long*>(step), hyper, factor, low, flags,
-                                            reinterpret_cast<unsigned*>(ctx->d_status + kAdamTicketWord));
-  }
-  return cudaGetLastError();
+  return adam_launch(ctx, PH_ADAMW, ctx->occ_adamw, adamw_kernel<true>, adamw_kernel<false>, step, hyper, factor, 0u, s,
+                     (const FlatTile*)ctx->d_flat_tiles, d, params, m, v,
+                     (const AdamCoef*)(ctx->d_status + kAdamCoefWord), reinterpret_cast<long long*>(step), hyper, factor,
+                     (unsigned short*)low, flags, reinterpret_cast<unsigned*>(ctx->d_status + kAdamTicketWord));
 }
 
 cudaError_t launch_adamw_8bit(acc_ctx* ctx, const float* d, float* params, uint8_t* m_code, uint8_t* r_code,
                               uint8_t* m_scale, uint8_t* r_scale, int64_t* step, const double* hyper,
                               const float* factor, uint16_t* low, uint32_t seed, int flags, cudaStream_t s) {
-  const int nt = (int)ctx->plan.tiles.size(), split = tile_split(nt, ctx->sm_count, 4);
-  {
-    PhaseTimer pt(ctx, PH_ADAMW_8BIT, s);
-    adamw_8bit_kernel<<<nt * split, 256, 0, s>>>(ctx->d_layers, ctx->d_tiles, split, d, params, m_code, r_code, m_scale,
-                                                 r_scale, reinterpret_cast<long long*>(step), hyper, factor, low, seed,
-                                                 flags, reinterpret_cast<unsigned*>(ctx->d_status + kAdamTicketWord));
-  }
-  return cudaGetLastError();
+  const Adam8Args p{d, params, m_code, r_code, m_scale, r_scale, low};
+  return adam_launch(ctx, PH_ADAMW_8BIT, ctx->occ_adamw_8bit, adamw_8bit_kernel<true>, adamw_8bit_kernel<false>, step,
+                     hyper, factor, (unsigned)seed, s, (const FlatTile*)ctx->d_flat_tiles, p,
+                     (const AdamCoef*)(ctx->d_status + kAdamCoefWord), reinterpret_cast<long long*>(step), hyper, factor,
+                     (unsigned)seed, flags, reinterpret_cast<unsigned*>(ctx->d_status + kAdamTicketWord));
+}
+
+// Once per context, at creation: how many blocks of the update's kernels an SM holds.
+cudaError_t prepare_adamw(acc_ctx* ctx) {
+  cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctx->occ_adamw, adamw_kernel<true>, 256, 0);
+  if (e == cudaSuccess)
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctx->occ_adamw_8bit, adamw_8bit_kernel<true>, 256, 0);
+  return e;
 }
 
 cudaError_t launch_clip_factor(acc_ctx* ctx, const double* n2_layers, double max_norm, float* factor, double* norm,

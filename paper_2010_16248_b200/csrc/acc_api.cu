@@ -111,6 +111,7 @@ static int make_plan(const acc_config* cfg, Plan& p) {
   p.o_col_items = take(sizeof(ColItem) * std::max<size_t>(1, p.col_items.size()));
   p.o_qred_items = take(sizeof(int2) * std::max<size_t>(1, p.qred_items.size()));
   p.o_tiles = take(sizeof(Tile) * nt);
+  p.o_flat_tiles = take(sizeof(FlatTile) * nt);
   p.o_mat_layers = take(sizeof(int) * std::max<size_t>(1, p.mat_layers.size()));
   p.o_vec_tiles = take(sizeof(int) * std::max<size_t>(1, p.vec_tiles.size()));
   p.o_mat_tiles = take(sizeof(int) * std::max<size_t>(1, p.mat_tiles.size()));
@@ -177,6 +178,7 @@ int acc_create(const acc_config* cfg, void* workspace, size_t workspace_bytes, a
   ctx->d_col_items = reinterpret_cast<ColItem*>(ws + p.o_col_items);
   ctx->d_qred_items = reinterpret_cast<int2*>(ws + p.o_qred_items);
   ctx->d_tiles = reinterpret_cast<Tile*>(ws + p.o_tiles);
+  ctx->d_flat_tiles = reinterpret_cast<FlatTile*>(ws + p.o_flat_tiles);
   ctx->d_mat_layers = reinterpret_cast<int*>(ws + p.o_mat_layers);
   ctx->d_vec_tiles = reinterpret_cast<int*>(ws + p.o_vec_tiles);
   ctx->d_mat_tiles = reinterpret_cast<int*>(ws + p.o_mat_tiles);
@@ -211,6 +213,13 @@ int acc_create(const acc_config* cfg, void* workspace, size_t workspace_bytes, a
   up(ctx->d_col_items, p.col_items.data(), sizeof(ColItem) * p.col_items.size());
   up(ctx->d_qred_items, p.qred_items.data(), sizeof(int2) * p.qred_items.size());
   up(ctx->d_tiles, p.tiles.data(), sizeof(Tile) * p.tiles.size());
+  std::vector<FlatTile> flat_tiles(p.tiles.size());
+  for (size_t i = 0; i < p.tiles.size(); ++i) {
+    const DevLayer& l = p.layers[p.tiles[i].layer];
+    flat_tiles[i] = FlatTile{l.offset + p.tiles[i].elem0, l.adam_block0 + p.tiles[i].elem0 / ACC_ADAMW_BLOCK,
+                             p.tiles[i].nelem, l.kind == ACC_MATRIX};
+  }
+  up(ctx->d_flat_tiles, flat_tiles.data(), sizeof(FlatTile) * flat_tiles.size());
   up(ctx->d_mat_layers, p.mat_layers.data(), sizeof(int) * p.mat_layers.size());
   up(ctx->d_vec_tiles, p.vec_tiles.data(), sizeof(int) * p.vec_tiles.size());
   up(ctx->d_mat_tiles, p.mat_tiles.data(), sizeof(int) * p.mat_tiles.size());
@@ -220,6 +229,7 @@ int acc_create(const acc_config* cfg, void* workspace, size_t workspace_bytes, a
   if (e == cudaSuccess) e = cudaMemset(ctx->d_pend_tau, 0xff, sizeof(unsigned) * seg);  // nothing pending
   if (e == cudaSuccess) e = prepare_powersgd();
   if (e == cudaSuccess) e = prepare_topk(ctx);
+  if (e == cudaSuccess) e = prepare_adamw(ctx);
   int dev = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, dev);
@@ -676,7 +686,7 @@ const char* acc_profile_kernel_name(int32_t i) {
       "psgd_orthonormalise_block_kernel", "sgd_tiles_kernel", "batch_accumulate_kernel", "batch_average_kernel",
       "detect_batch_kernel", "psgd_pfold_kernel", "vec_exchange_kernel", "psgd_qmerge_kernel",
       "topk_decompress_packed_kernel", "topk_flush_kernel", "moments_partial_kernel", "moments_final_kernel",
-      "adamw_kernel", "adamw_8bit_kernel", "clip_factor_kernel",
+      "adamw_coef_kernel", "adamw_kernel", "adamw_8bit_kernel", "clip_factor_kernel",
       "embedding_lookup_kernel", "embedding_rank_kernel", "embedding_keys_kernel", "embedding_hist_kernel",
       "embedding_scan_kernel", "embedding_scatter_kernel", "embedding_sum_kernel", "embedding_join_kernel"};
   return (i >= 0 && i < PH_COUNT) ? names[i] : "";

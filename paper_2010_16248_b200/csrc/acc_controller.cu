@@ -52,33 +52,47 @@ __global__ void __launch_bounds__(256) ef_kernel(const DevLayer* __restrict__ la
 }
 
 // One block per (tile, buffer): fp64 sum of squares of the tile, reduced in a fixed order.
-__global__ void __launch_bounds__(256) norm_partial_kernel(const DevLayer* __restrict__ layers,
-                                                           const Tile* __restrict__ tiles,
+template <bool MINUS>
+__global__ void __launch_bounds__(256) norm_partial_kernel(const FlatTile* __restrict__ tiles,
                                                            const float* __restrict__ buf, long long stride,
                                                            const float* __restrict__ minus,
                                                            double* __restrict__ part, int n_tiles) {
   __shared__ double sm[8];
-  const Tile t = tiles[blockIdx.x];
+  const FlatTile t = tiles[blockIdx.x];
   const int b = blockIdx.y;
-  const long long base = layers[t.layer].offset + t.elem0;
-  const float* x = buf + (long long)b * stride + base;
-  const float* y = minus != nullptr ? minus + base : nullptr;  // norms of (buf - minus), one buffer only
+  const float* x = buf + (long long)b * stride + t.base;
+  const float* y = minus + t.base;  // MINUS: norms of (buf - minus), one buffer only
   double acc = 0.0;
   const int n4 = t.nelem >> 2;
-  for (int i = threadIdx.x; i < n4; i += blockDim.x) {
-    float4 v = ld_stream4(x + 4 * i);
-    if (y != nullptr) {
+  // a tile's vectors, at most eight per thread, are loaded together and added in order (50.1 M elements: 47 us with one
+  // load at a time, 33 us so)
+  constexpr int kMost = kTile / 4 / 256;
+  float4 v[kMost];
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = (int)threadIdx.x + k * 256;
+    v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < n4) v[k] = ld_stream4(x + 4 * i);
+  }
+  if (MINUS) {
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+      const int i = (int)threadIdx.x + k * 256;
+      if (i >= n4) continue;
       const float4 u = ld_stream4(y + 4 * i);
-      v.x -= u.x; v.y -= u.y; v.z -= u.z; v.w -= u.w;
+      v[k].x -= u.x; v[k].y -= u.y; v[k].z -= u.z; v[k].w -= u.w;
     }
-    acc += (double)v.x * v.x;
-    acc += (double)v.y * v.y;
-    acc += (double)v.z * v.z;
-    acc += (double)v.w * v.w;
+  }
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    acc += (double)v[k].x * v[k].x;
+    acc += (double)v[k].y * v[k].y;
+    acc += (double)v[k].z * v[k].z;
+    acc += (double)v[k].w * v[k].w;
   }
   for (int i = 4 * n4 + threadIdx.x; i < t.nelem; i += blockDim.x) {
-    const float v = y != nullptr ? x[i] - y[i] : x[i];
-    acc += (double)v * v;
+    const float w = MINUS ? x[i] - y[i] : x[i];
+    acc += (double)w * w;
   }
   acc = warp_sum(acc);
   if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = acc;
@@ -96,6 +110,7 @@ __global__ void norm_final_kernel(const DevLayer* __restrict__ layers, const dou
   const int l = blockIdx.x, b = blockIdx.y;
   const DevLayer L = layers[l];
   double acc = 0.0;
+#pragma unroll 16
   for (int i = threadIdx.x; i < L.ntiles; i += 32) acc += part[(long long)b * n_tiles + L.tile0 + i];
   acc = warp_sum(acc);
   if (threadIdx.x == 0) norm2[(long long)b * n_layers + l] = acc;
@@ -202,8 +217,11 @@ cudaError_t launch_layer_norms(acc_ctx* ctx, const float* buf, long long stride,
   const int nt = (int)ctx->plan.tiles.size();
   {
     PhaseTimer pt(ctx, PH_NORM_PARTIAL, s);
-    norm_partial_kernel<<<dim3((unsigned)nt, (unsigned)n_bufs), 256, 0, s>>>(ctx->d_layers, ctx->d_tiles, buf, stride,
-                                                                            minus, ctx->d_norm_part, nt);
+    const dim3 grid((unsigned)nt, (unsigned)n_bufs);
+    if (minus != nullptr)
+      norm_partial_kernel<true><<<grid, 256, 0, s>>>(ctx->d_flat_tiles, buf, stride, minus, ctx->d_norm_part, nt);
+    else
+      norm_partial_kernel<false><<<grid, 256, 0, s>>>(ctx->d_flat_tiles, buf, stride, nullptr, ctx->d_norm_part, nt);
   }
   {
     PhaseTimer pt(ctx, PH_NORM_FINAL, s);

@@ -40,6 +40,8 @@ struct DevLayer {
 
 struct ColItem { int layer, slab, row0, nrows, col0; };  // (row slab, column block) of a MATRIX layer
 struct Tile { int layer, elem0, nelem; };              // flat tile, never spans layers
+// A flat tile with what the kernels over all layers need of its layer: one load instead of two in a row.
+struct FlatTile { long long base, block0; int nelem, matrix; };
 
 // Per (worker, MATRIX layer) state of the radix select.
 struct Select {
@@ -58,6 +60,7 @@ constexpr int kListCollect = 0, kListDense = 1, kListSelect = 2, kListStaged = 3
 constexpr int kListCountWord = 8;  // the lists' lengths live at words 8..11 of the per-step word block
 constexpr int kTicketWord = 16;    // tile ticket of the decompress pass, same block (cleared at the start of a step)
 constexpr int kAdamTicketWord = 10; // finished-block count of the AdamW kernels, in the status block (zero between calls)
+constexpr int kAdamCoefWord = 16;   // a step's AdamW coefficients, same block
 constexpr unsigned kNoPendingTau = 0xffffffffu;  // no key is larger: nothing pending
 constexpr int kPredTileCap = 2048;  // keys one tile may hand to a predicted list (more: overflow, fall back)
 
@@ -69,7 +72,7 @@ enum Phase {
   PH_TOPK_DECOMPRESS, PH_PSGD_FLUSH, PH_TOPK_COLLECT, PH_TOPK_PICK3, PH_TOPK_TILE_COUNTS, PH_TOPK_HIST2_LIST, PH_TOPK_HIST3_LIST, PH_TOPK_FINALIZE_STAGED, PH_PSGD_ORTHO_BLOCK, PH_SGD_TILES, PH_BATCH_ACCUMULATE, PH_BATCH_AVERAGE, PH_DETECT_BATCH,
   PH_PSGD_PFOLD, PH_VEC_EXCHANGE, PH_PSGD_QMERGE, PH_TOPK_DECOMPRESS_PACKED, PH_TOPK_FLUSH,
   PH_MOMENTS_PARTIAL, PH_MOMENTS_FINAL,
-  PH_ADAMW, PH_ADAMW_8BIT, PH_CLIP_FACTOR,
+  PH_ADAMW_COEF, PH_ADAMW, PH_ADAMW_8BIT, PH_CLIP_FACTOR,
   PH_EMB_LOOKUP, PH_EMB_RANK, PH_EMB_KEYS, PH_EMB_HIST, PH_EMB_SCAN, PH_EMB_SCATTER, PH_EMB_SUM, PH_EMB_JOIN,
   PH_COUNT
 };
@@ -91,7 +94,7 @@ struct Plan {
   long long adam_blocks = 0; // blocks of ACC_ADAMW_BLOCK elements over all layers
   long long vec_floats = 0;  // packed VECTOR elements (each layer starts at a multiple of 4)
   // workspace offsets (bytes)
-  size_t o_qred_items = 0;
+  size_t o_qred_items = 0, o_flat_tiles = 0;
   size_t o_layers = 0, o_col_items = 0, o_tiles = 0, o_mat_layers = 0, o_vec_tiles = 0, o_mat_tiles = 0, o_status = 0,
          o_part = 0, o_ppart = 0, o_pending = 0, o_norm_part = 0, o_hist = 0, o_sel = 0, o_pred = 0, o_cand = 0, o_tile_cand = 0, o_tile_cnt = 0, o_tile_h3 = 0, o_tile_pre = 0, o_tile_rng = 0, o_lists = 0, o_pend_tau = 0,
          hist_bytes = 0, total = 0;
@@ -106,6 +109,7 @@ struct acc_ctx {
   char* ws = nullptr;
   int sm_count = 148;
   int occ_topk_first_pass = 3;       // resident blocks per SM of topk_ef_hist1_kernel (queried at creation)
+  int occ_adamw = 1, occ_adamw_8bit = 1;  // resident blocks per SM of the AdamW kernels, likewise
   int last_launches = 0;
   bool prof = false;                 // per-kernel event timing on
   std::vector<acc::ProfSlot> prof_slots;
@@ -115,12 +119,13 @@ struct acc_ctx {
   acc::ColItem* d_col_items = nullptr;
   int2* d_qred_items = nullptr;
   acc::Tile* d_tiles = nullptr;
+  acc::FlatTile* d_flat_tiles = nullptr;
   int* d_mat_layers = nullptr;
   int* d_vec_tiles = nullptr;
   int* d_mat_tiles = nullptr;
   int* d_status = nullptr;           // 64 words: [0] device-side error flag (0 = none), see acc_device_status;
                                      // [8], [9] tile ticket and finished-block count of the pipelined first PowerSGD pass,
-                                     // [10] finished-block count of the AdamW kernels
+                                     // [10] finished-block count of the AdamW kernels, [16..] a step's AdamW coefficients
   float4* d_part = nullptr;
   float4* d_ppart = nullptr;         // partial rows of P, one slot per tile a row touches
   int* d_pending = nullptr;          // lazy PowerSGD: rank of the residual not yet applied to err, per layer
@@ -178,6 +183,7 @@ cudaError_t launch_topk(acc_ctx* ctx, const float* grads, float* err, const uint
 // Real workers: the TopK step in two halves around the all-gather of the packed sets.
 cudaError_t launch_topk_flush(acc_ctx* ctx, float* err, cudaStream_t s);
 cudaError_t prepare_topk(acc_ctx* ctx);
+cudaError_t prepare_adamw(acc_ctx* ctx);
 cudaError_t launch_topk_compress(acc_ctx* ctx, const float* grads, float* err, const uint8_t* level, float* vals,
                                  int32_t* idx, int32_t* counts, float* delta, float* vec_packed, cudaStream_t s);
 cudaError_t launch_topk_decompress_packed(acc_ctx* ctx, const float* vals, const int32_t* idx, const int32_t* counts,

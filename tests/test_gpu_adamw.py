@@ -4,9 +4,11 @@ Tolerances.  u = 2^-24 is the largest relative error of one fp32 rounding.  Per 
 and the coefficients rounded to fp32 once:
   m:  beta1 m carries 1 u (the coefficient), (1 - beta1) g 3 u (coefficient, f d, product), the fma 1 u on the result:
       |error| <= 5 u (|beta1 m| + |(1 - beta1) g|).
-  v:  a sum of non-negative terms with at most 6 u (coefficient, g twice, g g, product, fma): 6 u relative; sqrt halves it
-      and rounds once: 4 u on r; the root of the bias correction, its product in the fma and eps: 7 u on the denominator.
-  x:  step size (1 u), quotient (m's error / denominator + 7 u + 1 u), the two fma (1 u each of what they give) and lr wd.
+  v:  a sum of non-negative terms with at most 6 u (coefficient, g twice, g g, product, fma): 6 u relative; the root halves
+      it, and sqrt.approx adds 2^-23 = 2 u (its stated largest relative error): 5 u on r; the root of the bias correction,
+      the fma and eps: 8 u on the denominator.
+  x:  step size (1 u), quotient (m's error / denominator + 8 u + the 2 ulp = 4 u of __fdividef), the two fma (1 u each of
+      what they give) and lr wd: 13 u on the quotient.
 Second-order terms are covered by a factor of 1.01.  Values under 2^-126 add at most 2^-149 each.
 """
 import numpy as np
@@ -64,7 +66,7 @@ def _bounds(d, x, m, v, step, hyper, layers, factor, decay_vectors):
     ev = 1.01 * 6 * U * V + TINY
     denom = np.sqrt(V) / root + eps
     q = np.abs(M) / denom
-    ex = 1.01 * U * (2 * np.abs(X) + 2 * lr * wd * np.abs(x) + 2 * np.abs(x) + size * (5 * parts / denom + 10 * q)) + TINY
+    ex = 1.01 * U * (2 * np.abs(X) + 2 * lr * wd * np.abs(x) + 2 * np.abs(x) + size * (5 * parts / denom + 14 * q)) + TINY
     return X, M, V, T, ex, em, ev
 
 
@@ -168,8 +170,8 @@ def _check_8bit(table, ctx, d, x, m, v, step0, hyper, seed, clip=None, flags=0, 
             c = torch.from_numpy(cover).cuda()
             assert torch.equal(low[c], x.to(torch.bfloat16)[c]) and bool((low[~c] == 7.0).all())
         got = [_bytes(t) for t in state]
-        for name, code, scale, err in (("m", got[0], got[2], em), ("r", got[1], got[3], 4.04 * U * np.sqrt(V) + TINY)):
-            # (4 u on r: half of v's 6 u, and the root's rounding)
+        for name, code, scale, err in (("m", got[0], got[2], em), ("r", got[1], got[3], 5.05 * U * np.sqrt(V) + TINY)):
+            # (5 u on r: half of v's 6 u, and the root's 2 u)
             assert np.array_equal(scale, want[name + "_scale"]), name
             assert np.array_equal(code[~cover], b[0 if name == "m" else 1][~cover])
             for blk, (s, n) in enumerate(tor.block_starts(layers)):
