@@ -445,7 +445,7 @@ class Context:
         number: ``tokens`` of any shape (int32 / int64), ``out`` its shape times the layer's columns (float32 /
         bfloat16)."""
         layer, n, tt, ot = self._embedding(layer, tokens, out, "out")
-        self._call("acc_embedding_lookup", layer, self._f(params, self.extent, "params"),
+        self._call("acc_embedding_lookup", layer, self._f(params, self.stride, "params"),
                    _Arg(tokens, tokens.dtype, n, "tokens"), tt, n, float(scale), _Arg(out, out.dtype, out.numel(), "out"),
                    ot, stream=stream)
 

@@ -1,6 +1,8 @@
 // Embedding of a MATRIX layer: the lookup of token rows, and the gradient as one sum per distinct token.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "acc_internal.cuh"
 
 namespace acc {
@@ -8,33 +10,28 @@ namespace acc {
 // VEC adjacent values of fp32 or bf16, as fp32.  VEC is the widest width at which every row of the layer starts aligned.
 template <int VEC> struct Vals { float v[VEC]; };
 
-template <int VEC> __device__ __forceinline__ Vals<VEC> load_vals(const float* p) {
-  Vals<VEC> r;
-  if constexpr (VEC == 4) {
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    r.v[0] = a.x; r.v[1] = a.y; r.v[2] = a.z; r.v[3] = a.w;
-  } else if constexpr (VEC == 2) {
-    const float2 a = *reinterpret_cast<const float2*>(p);
-    r.v[0] = a.x; r.v[1] = a.y;
-  } else {
-    r.v[0] = *p;
-  }
-  return r;
+// As loaded, and as fp32.
+template <typename T, int VEC> struct Raw;
+template <> struct Raw<float, 4> { using type = float4; };
+template <> struct Raw<float, 2> { using type = float2; };
+template <> struct Raw<float, 1> { using type = float; };
+template <> struct Raw<__nv_bfloat16, 4> { using type = uint2; };
+template <> struct Raw<__nv_bfloat16, 2> { using type = unsigned; };
+template <> struct Raw<__nv_bfloat16, 1> { using type = unsigned short; };
+template <int VEC, typename T> __device__ __forceinline__ typename Raw<T, VEC>::type load_raw(const T* p) {
+  return *reinterpret_cast<const typename Raw<T, VEC>::type*>(p);
 }
-template <int VEC> __device__ __forceinline__ Vals<VEC> load_vals(const __nv_bfloat16* p) {
-  Vals<VEC> r;
-  if constexpr (VEC == 4) {
-    const uint2 a = *reinterpret_cast<const uint2*>(p);
-    r.v[0] = __uint_as_float(a.x << 16); r.v[1] = __uint_as_float(a.x & 0xffff0000u);
-    r.v[2] = __uint_as_float(a.y << 16); r.v[3] = __uint_as_float(a.y & 0xffff0000u);
-  } else if constexpr (VEC == 2) {
-    const unsigned a = *reinterpret_cast<const unsigned*>(p);
-    r.v[0] = __uint_as_float(a << 16); r.v[1] = __uint_as_float(a & 0xffff0000u);
-  } else {
-    r.v[0] = __bfloat162float(*p);
-  }
-  return r;
+__device__ __forceinline__ Vals<4> unpack(const float4& a) { return {a.x, a.y, a.z, a.w}; }
+__device__ __forceinline__ Vals<2> unpack(const float2& a) { return {a.x, a.y}; }
+__device__ __forceinline__ Vals<1> unpack(float a) { return {a}; }
+__device__ __forceinline__ Vals<2> unpack(unsigned a) { return {__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)}; }
+__device__ __forceinline__ Vals<4> unpack(const uint2& a) {
+  const Vals<2> lo = unpack(a.x), hi = unpack(a.y);
+  return {lo.v[0], lo.v[1], hi.v[0], hi.v[1]};
 }
+__device__ __forceinline__ Vals<1> unpack(unsigned short a) { return {__uint_as_float((unsigned)a << 16)}; }
+
+template <int VEC> __device__ __forceinline__ Vals<VEC> load_vals(const float* p) { return unpack(load_raw<VEC>(p)); }
 template <int VEC> __device__ __forceinline__ void store_vals(float* p, const Vals<VEC>& r) {
   if constexpr (VEC == 4) *reinterpret_cast<float4*>(p) = make_float4(r.v[0], r.v[1], r.v[2], r.v[3]);
   else if constexpr (VEC == 2) *reinterpret_cast<float2*>(p) = make_float2(r.v[0], r.v[1]);
@@ -66,7 +63,8 @@ __device__ __forceinline__ unsigned token_row(long long tok, int rows, int* stat
   return (unsigned)tok;
 }
 
-// One warp per token:  out_i = scale * row(tok_i), rounded once; zeros where there is no row.
+// One warp per token:  out_i = scale * row(tok_i), rounded once; zeros where there is no row.  A lane's loads of a batch of
+// VEC columns go out together.  Bound by the traffic of L2 and HBM.
 template <typename Tok, typename Out, int VEC>
 __global__ void __launch_bounds__(256)
 embedding_lookup_kernel(const float* __restrict__ table, int rows, int cols, const Tok* __restrict__ tokens, long long n,
@@ -75,27 +73,30 @@ embedding_lookup_kernel(const float* __restrict__ table, int rows, int cols, con
   if (i >= n) return;
   const int lane = threadIdx.x & 31;
   const unsigned row = token_row((long long)tokens[i], rows, status);
-  const float* src = table + (long long)row * cols;
+  const bool none = row == (unsigned)rows;
+  const float* src = table + (none ? 0ll : (long long)row * cols);
   Out* dst = out + i * cols;
-  const int nv = cols / VEC;
-  if (row == (unsigned)rows) {
-    for (int j = lane; j < nv; j += 32) store_vals<VEC>(dst + (long long)j * VEC, Vals<VEC>{});
-    return;
-  }
-#pragma unroll 4
-  for (int j = lane; j < nv; j += 32) {
-    Vals<VEC> a = load_vals<VEC>(src + (long long)j * VEC);
+  constexpr int kBatch = 6;
+  for (int c0 = VEC * lane; c0 < cols; c0 += 32 * VEC * kBatch) {
+    Vals<VEC> v[kBatch];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) a.v[k] *= scale;
-    store_vals<VEC>(dst + (long long)j * VEC, a);
+    for (int k = 0; k < kBatch; ++k)
+      if (c0 + 32 * VEC * k < cols) v[k] = load_vals<VEC>(src + c0 + 32 * VEC * k);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (c0 + 32 * VEC * k >= cols) continue;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[k].v[j] = none ? 0.f : v[k].v[j] * scale;
+      store_vals<VEC>(dst + c0 + 32 * VEC * k, v[k]);
+    }
   }
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------
 // G_w[r] (+)= scale * sum over the tokens i of worker w with tok_i = r of dy_i.  The tokens of a worker are sorted by
-// (row, position); the sorted order is cut into chunks of 32 entries, whatever the rows, so that a frequent token costs no
-// more than 32 rare ones.  A row whose entries lie inside one chunk is final there; one that crosses a chunk's edge leaves
-// a partial sum in that chunk's head or tail slot, and the next level adds the slots of 32 chunks in the same way, until
+// (row, position); the sorted order is cut into chunks of 128 entries, whatever the rows, so that a frequent token costs no
+// more than as many rare ones.  A row whose entries lie inside one chunk is final there; one that crosses a chunk's edge leaves
+// a partial sum in that chunk's head or tail slot, and the next level adds the slots of 128 chunks in the same way, until
 // one chunk is left.  Every sum has one writer and a fixed order, so results do not change from run to run.
 
 struct EmbArgs {
@@ -105,52 +106,119 @@ struct EmbArgs {
   int rows, cols, n;     // n: tokens per worker
 };
 
-// Zeros of every worker's slice of the layer, cut into pieces of kZeroPiece elements.
-constexpr int kZeroPiece = 32768;
-__device__ __forceinline__ void zero_piece(float* __restrict__ grads, const EmbArgs& a, long long piece, long long pieces_per_worker) {
-  const long long w = piece / pieces_per_worker;
-  const long long e0 = (piece - w * pieces_per_worker) * kZeroPiece;
-  float* g = grads + w * a.stride + a.offset + e0;
+// The next kernel of a call may start while this one runs; it waits for it in full before it touches memory.  (Only the
+// call's first kernel is launched without that permission, so it starts behind everything queued before the call.)
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Overwriting a gradient is mostly writing zeros: pieces of kZeroPiece elements, handed to the call's kernels behind their
+// own blocks.  While the tokens are sorted whole pieces are cleared, as many as fill that time (zero_piece; a row written
+// later is then written twice); the rest are cleared beside the sums, leaving the rows out that the sums write
+// (zero_piece_around).  So the memory system never waits for the sort or the last level of sums.
+struct EmbZero {
+  float* grads;
+  int first_block;       // blocks behind this one clear pieces
+  int from;              // number of the first such block's piece
+  int pieces_per_worker;
+  unsigned* rows_taken;  // see zero_piece_around
+};
+constexpr int kZeroPiece = 16384;
+
+__device__ __forceinline__ void zero_piece(const EmbZero& z, const EmbArgs& a) {
+  const int piece = z.from + (int)blockIdx.x - z.first_block;
+  const int w = piece / z.pieces_per_worker;
+  const long long e0 = (long long)(piece - w * z.pieces_per_worker) * kZeroPiece;
+  float* g = z.grads + w * a.stride + a.offset + e0;
   const int n = (int)min((long long)kZeroPiece, a.size - e0);
   for (int i = 4 * (int)threadIdx.x; i + 4 <= n; i += 4 * (int)blockDim.x) st_stream4(g + i, make_float4(0.f, 0.f, 0.f, 0.f));
   for (int i = (n & ~3) + (int)threadIdx.x; i < n; i += blockDim.x) g[i] = 0.f;
 }
 
+// The rows of a piece that some token names: a bit each in `rows_taken` ([W][(rows + 31) / 32], set by the last pass of the
+// radix sort), or, where that is null, what a look at all of the worker's few sorted keys says.
+__device__ __forceinline__ void zero_piece_around(const EmbZero& z, const EmbArgs& a, const unsigned* __restrict__ keys) {
+  __shared__ unsigned taken[kZeroPiece / 32 + 3];  // bit r: row (row0 & ~31) + r
+  const int piece = z.from + (int)blockIdx.x - z.first_block;
+  const int w = piece / z.pieces_per_worker;
+  const unsigned e0 = (unsigned)(piece - w * z.pieces_per_worker) * kZeroPiece, cols = (unsigned)a.cols;
+  float* g = z.grads + w * a.stride + a.offset + e0;
+  const int n = (int)min((long long)kZeroPiece, a.size - e0);
+  const unsigned row0 = e0 / cols, row1 = (e0 + (unsigned)n - 1u) / cols, word0 = row0 >> 5, words = (row1 >> 5) - word0 + 1u;
+  if (z.rows_taken != nullptr) {
+    const unsigned* bits = z.rows_taken + (long long)w * ((a.rows + 31) / 32) + word0;
+    for (unsigned i = threadIdx.x; i < words; i += blockDim.x) taken[i] = bits[i];
+  } else {
+    const unsigned* kw = keys + (long long)w * a.n;
+    for (unsigned i = threadIdx.x; i < words; i += blockDim.x) taken[i] = 0u;
+    __syncthreads();
+#pragma unroll 4
+    for (int j = threadIdx.x; j < a.n; j += blockDim.x) {
+      const unsigned key = kw[j];
+      if (key >= row0 && key <= row1) atomicOr(&taken[(key >> 5) - word0], 1u << (key & 31));
+    }
+  }
+  __syncthreads();
+  auto free_row = [&](unsigned r) { return !(taken[(r >> 5) - word0] >> (r & 31) & 1u); };
+  if (a.cols < 64) {  // element by element: which row a narrow one lies in, x / cols, exact for x below 2^32 / cols
+    const unsigned magic = cols > 1u ? 0xffffffffu / cols + 1u : 0u, off0 = e0 - row0 * cols;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+      const unsigned x = (unsigned)i + off0;
+      if (free_row(row0 + (cols == 1u ? x : __umulhi(x, magic)))) g[i] = 0.f;
+    }
+    return;
+  }
+  const int lane = threadIdx.x & 31;
+  for (unsigned r = row0 + (threadIdx.x >> 5); r <= row1; r += blockDim.x >> 5) {  // a warp per row
+    if (!free_row(r)) continue;
+    const long long r0 = (long long)r * cols - e0;
+    const int lo = (int)max(r0, 0ll), hi = (int)min(r0 + cols, (long long)n);
+    const int lo4 = min((lo + 3) & ~3, hi), hi4 = max(hi & ~3, lo4);
+    if (lo + lane < lo4) g[lo + lane] = 0.f;
+    for (int i = lo4 + 4 * lane; i < hi4; i += 128) st_stream4(g + i, make_float4(0.f, 0.f, 0.f, 0.f));
+    if (hi4 + lane < hi) g[hi4 + lane] = 0.f;
+  }
+}
+
 // Up to kRankMost tokens per worker: a token's place is the number of tokens before it in (row, position) order, counted
-// against all of them in shared memory.  Quadratic, but 256 tokens per block and no pass waits for another: 700 tokens
-// take 1/3 of one radix pass's launches.  Blocks behind the counting ones write zeros meanwhile.
-constexpr int kRankMost = 2048, kRankBlock = 256;
+// against all of them in shared memory.  Quadratic, but 64 tokens per block and one launch where the radix sort takes
+// four or more.
+constexpr int kRankMost = 2048, kRankThreads = 256, kRankBlock = kRankThreads / 4;  // tokens, threads, tokens per block
 template <typename Tok>
-__global__ void __launch_bounds__(kRankBlock)
+__global__ void __launch_bounds__(kRankThreads)
 embedding_rank_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __restrict__ keys, unsigned* __restrict__ pos,
-                      int rank_blocks, int blocks_per_worker, float* __restrict__ grads, long long pieces_per_worker,
-                      int* status) {
-  if ((int)blockIdx.x >= rank_blocks) {
-    zero_piece(grads, a, (long long)blockIdx.x - rank_blocks, pieces_per_worker);
+                      int blocks_per_worker, int* status, EmbZero z) {
+  let_next_start();
+  if ((int)blockIdx.x >= z.first_block) {
+    zero_piece(z, a);
     return;
   }
   __shared__ __align__(16) unsigned sk[kRankMost];
   const int w = blockIdx.x / blocks_per_worker, first = (int)(blockIdx.x % blocks_per_worker) * kRankBlock;
   const Tok* tok = tokens + (long long)w * a.n;
   const int n4 = (a.n + 3) & ~3;
-  for (int j = threadIdx.x; j < n4; j += kRankBlock)
+  for (int j = threadIdx.x; j < n4; j += kRankThreads)
     sk[j] = j < a.n ? token_row((long long)tok[j], a.rows, status) : 0xffffffffu;
   __syncthreads();
-  const int i = first + (int)threadIdx.x;
+  // four lanes per token, each against every fourth vector of keys: those before the token's own vector count if they are
+  // smaller or equal, the others if they are smaller; equal ones before it in its own vector are added by the first lane
+  const int i = first + (int)(threadIdx.x >> 2), part = threadIdx.x & 3, own = i & ~3;
   const unsigned key = i < a.n ? sk[i] : 0u;
-  int rank = 0;
-  // tokens before this block's come first among equals, those behind it last
-  const int last = min(first + kRankBlock, n4);
-  for (int j = 0; j < first; j += 4) {
+  int rank = 0, j = 4 * part;
+#pragma unroll 4
+  for (; j < min(own, n4); j += 16) {
     const uint4 o = *reinterpret_cast<const uint4*>(sk + j);
     rank += (o.x <= key) + (o.y <= key) + (o.z <= key) + (o.w <= key);
   }
-  for (int j = first; j < last; ++j) rank += sk[j] < key || (sk[j] == key && j < i);
-  for (int j = last; j < n4; j += 4) {
+#pragma unroll 4
+  for (; j < n4; j += 16) {
     const uint4 o = *reinterpret_cast<const uint4*>(sk + j);
     rank += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
   }
-  if (i < a.n) {
+  if (part == 0 && i < a.n)
+    for (int k = own; k < i; ++k) rank += sk[k] == key;
+  rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+  rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+  if (part == 0 && i < a.n) {
     keys[(long long)w * a.n + rank] = key;
     pos[(long long)w * a.n + rank] = (unsigned)i;
   }
@@ -167,10 +235,10 @@ __device__ __forceinline__ long long sort_hist_at(int w, int digit, int tile, in
 template <typename Tok>
 __global__ void __launch_bounds__(kSortThreads)
 embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __restrict__ keys, unsigned* __restrict__ pos,
-                      unsigned* __restrict__ hist, int n_tiles, int sort_blocks, float* __restrict__ grads,
-                      long long pieces_per_worker, int* status) {
-  if ((int)blockIdx.x >= sort_blocks) {
-    zero_piece(grads, a, (long long)blockIdx.x - sort_blocks, pieces_per_worker);
+                      unsigned* __restrict__ hist, int n_tiles, int* status, EmbZero z) {
+  let_next_start();
+  if ((int)blockIdx.x >= z.first_block) {
+    zero_piece(z, a);
     return;
   }
   __shared__ unsigned h[256];
@@ -179,6 +247,10 @@ embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __res
   const int w = blockIdx.x / n_tiles, tile = blockIdx.x % n_tiles;
   const long long w0 = (long long)w * a.n;
   const int end = min((tile + 1) * kSortTile, a.n);
+  const int row_words = (a.rows + 31) / 32;
+  if (z.rows_taken != nullptr)
+    for (int i = tile * kSortThreads + (int)threadIdx.x; i < row_words; i += n_tiles * kSortThreads)
+      z.rows_taken[(long long)w * row_words + i] = 0u;
   for (int i = tile * kSortTile + (int)threadIdx.x; i < end; i += kSortThreads) {
     const unsigned key = token_row((long long)tokens[w0 + i], a.rows, status);
     keys[w0 + i] = key;
@@ -190,7 +262,15 @@ embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __res
 }
 
 __global__ void __launch_bounds__(kSortThreads)
-embedding_hist_kernel(const unsigned* __restrict__ keys, int n, int shift, unsigned* __restrict__ hist, int n_tiles) {
+embedding_hist_kernel(const unsigned* __restrict__ keys, EmbArgs a, int shift, unsigned* __restrict__ hist, int n_tiles,
+                      EmbZero z) {
+  let_next_start();
+  if ((int)blockIdx.x >= z.first_block) {
+    zero_piece(z, a);
+    return;
+  }
+  await_previous();
+  const int n = a.n;
   __shared__ unsigned h[256];
   h[threadIdx.x] = 0u;
   __syncthreads();
@@ -203,9 +283,17 @@ embedding_hist_kernel(const unsigned* __restrict__ keys, int n, int shift, unsig
   hist[sort_hist_at(w, threadIdx.x, tile, n_tiles)] = h[threadIdx.x];
 }
 
-// One block per worker: exclusive sum over (digit, tile), in place.
+// One block per worker: exclusive sum over (digit, tile), in place.  Only for more than kScanTiles tiles: fewer counts are
+// quicker summed by every block of the scatter pass (a launch costs 5 us).
+constexpr int kScanTiles = 64;
 __global__ void __launch_bounds__(1024)
-embedding_scan_kernel(unsigned* __restrict__ hist, int n_tiles) {
+embedding_scan_kernel(unsigned* __restrict__ hist, int n_tiles, EmbArgs a, EmbZero z) {
+  let_next_start();
+  if ((int)blockIdx.x >= z.first_block) {
+    zero_piece(z, a);
+    return;
+  }
+  await_previous();
   __shared__ unsigned part[32];
   unsigned* h = hist + (long long)blockIdx.x * 256 * n_tiles;
   const int total = 256 * n_tiles, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -237,11 +325,20 @@ embedding_scan_kernel(unsigned* __restrict__ hist, int n_tiles) {
 
 // Moves a tile's entries to their places.  A warp takes 256 adjacent entries, 32 at a time in order; lanes with the same
 // digit rank themselves by lane, the warp's running counts give the rank among its earlier ones.
+template <bool SCANNED>
 __global__ void __launch_bounds__(kSortThreads)
-embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ pos, int n, int shift,
+embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ pos, EmbArgs a, int shift,
                          const unsigned* __restrict__ hist, int n_tiles, unsigned* __restrict__ keys_out,
-                         unsigned* __restrict__ pos_out) {
+                         unsigned* __restrict__ pos_out, int last, EmbZero z) {
+  let_next_start();
+  if ((int)blockIdx.x >= z.first_block) {
+    zero_piece(z, a);
+    return;
+  }
+  await_previous();
+  const int n = a.n;
   __shared__ unsigned cnt[kSortWarps][256];
+  __shared__ unsigned warp_total[kSortWarps];
   const int w = blockIdx.x / n_tiles, tile = blockIdx.x % n_tiles;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long w0 = (long long)w * n;
@@ -266,7 +363,29 @@ embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __re
   }
   __syncthreads();
   {
-    unsigned run = hist[sort_hist_at(w, threadIdx.x, tile, n_tiles)];
+    unsigned run;  // where the tile's first entry with this thread's digit goes
+    if (SCANNED) {
+      run = hist[sort_hist_at(w, threadIdx.x, tile, n_tiles)];
+    } else {
+      const unsigned* h = hist + sort_hist_at(w, threadIdx.x, 0, n_tiles);
+      unsigned ahead = 0u, total = 0u;
+#pragma unroll 8
+      for (int k = 0; k < n_tiles; ++k) {
+        const unsigned c = h[k];
+        ahead += k < tile ? c : 0u;
+        total += c;
+      }
+      unsigned inc = total;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+      }
+      if (lane == 31) warp_total[warp] = inc;
+      __syncthreads();
+      run = ahead + inc - total;
+      for (int k = 0; k < warp; ++k) run += warp_total[k];
+    }
 #pragma unroll
     for (int k = 0; k < kSortWarps; ++k) {
       const unsigned c = cnt[k][threadIdx.x];
@@ -281,114 +400,210 @@ embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __re
     const long long to = w0 + cnt[warp][(key[k] >> shift) & 255u] + rank[k];
     keys_out[to] = key[k];
     pos_out[to] = pos[w0 + i0 + 32 * k];
+    if (last && z.rows_taken != nullptr && key[k] != (unsigned)a.rows) {
+      unsigned* word = z.rows_taken + (long long)w * ((a.rows + 31) / 32) + (key[k] >> 5);
+      const unsigned bit = 1u << (key[k] & 31);
+      if (!(__ldcg(word) & bit)) atomicOr(word, bit);  // (frequent rows find theirs set)
+    }
   }
 }
 
-// One level of sums.  FIRST: the entries are 32 sorted tokens, read from dy; otherwise they are the head and tail slots of
-// 32 chunks of the level below, each of which covers `span` sorted tokens.  A thread owns VEC columns and adds eight
-// entries' loads at a time.
-constexpr int kChunk = 32;
-template <typename In, int VEC, bool FIRST>
-__global__ void __launch_bounds__(256)
-embedding_sum_kernel(const In* __restrict__ dy, const float* __restrict__ below, const unsigned* __restrict__ keys,
-                     const unsigned* __restrict__ pos, EmbArgs a, int span, int chunks_below, int chunks, int shares,
-                     float scale,
-                     int accumulate, float* __restrict__ grads, float* __restrict__ slots) {
-  __shared__ unsigned skey[2 * kChunk + 1], ssrc[2 * kChunk];
-  __shared__ int warp_n[2];
-  // block order: column share fastest, then chunk, then worker
-  const int share = blockIdx.x % shares, item = blockIdx.x / shares;
-  const int w = item / chunks, chunk = item % chunks;
-  const unsigned* kw = keys + (long long)w * a.n;
-  const unsigned* pw = pos + (long long)w * a.n;
-  const unsigned none = (unsigned)a.rows;
-  // whether one row's entries lie on both sides of sorted place `at`
-  auto crosses = [&](long long at) { return at > 0 && at < a.n && kw[at] != none && kw[at - 1] == kw[at]; };
-  const long long chunk_span = FIRST ? kChunk : (long long)span * kChunk;
-  const long long begin = chunk * chunk_span, end = min((long long)a.n, begin + chunk_span);
-  const int lane = threadIdx.x & 31;
-  if (threadIdx.x < 2 * kChunk) {
-    bool valid = false;
-    unsigned key = none, src = 0u;
-    if (FIRST) {
-      const long long e = begin + threadIdx.x;
-      if (threadIdx.x < kChunk && e < end) {
-        key = kw[e];
-        valid = key != none;
-        src = pw[e];
-      }
-    } else {
-      const long long s = (long long)chunk * kChunk + (threadIdx.x >> 1);
-      if (s < chunks_below) {
-        const long long b = s * span, e = min((long long)a.n, b + span);
-        const bool head = crosses(b);
-        if ((threadIdx.x & 1) == 0) {
-          valid = head;
-          key = kw[b];
-        } else {
-          key = kw[e - 1];
-          valid = crosses(e) && !(head && kw[b] == key);
-        }
-        src = (unsigned)(2 * s + (threadIdx.x & 1));
-      }
-    }
-    const unsigned on = __ballot_sync(0xffffffffu, valid);
-    if (lane == 0) warp_n[threadIdx.x >> 5] = __popc(on);
-    __syncwarp();
-    // entries in order, without gaps (the second warp's go behind the first's, filled in below)
-    const int at = __popc(on & ((1u << lane) - 1u));
-    if (threadIdx.x < 32) {
-      if (valid) { skey[at] = key; ssrc[at] = src; }
-    }
-    asm volatile("bar.sync 1, 64;" ::: "memory");
-    if (threadIdx.x >= 32 && valid) { skey[warp_n[0] + at] = key; ssrc[warp_n[0] + at] = src; }
+// A block takes one chunk and 128 columns, each of its eight warps an eighth of the entries, in order: 16 sorted tokens at
+// the first level, 32 slots of the level below (two for each of its kFan chunks) at the others.  A run that crosses from
+// one warp to the next is finished by the warp where it begins, from the sums that the others leave in shared memory.  The
+// loads of a batch of entries go out together, with accumulation (ACC) those of the rows that are added to among them.  What
+// steers the sums is the same for a whole warp: masks of the entries there are and of those that end a run.
+constexpr int kChunk = 128, kFan = 128;
+constexpr unsigned kNoKey = 0xffffffffu;
+struct EmbLevel {
+  const unsigned* keys;   // first level: sorted rows, [W][n]; otherwise the slots' rows, [W][2 chunks of the level below]
+  const unsigned* pos;    // first level: sorted positions
+  int count, chunks;      // keys per worker; chunks of this level per worker
+  float* slots;           // [W][chunks][2][cols]: where this level leaves its partial sums
+  unsigned* slot_keys;    // [W][chunks][2]: their rows; kNoKey: nothing there
+};
+
+// Four columns of a lane: 4 / VEC vectors, 32 VEC columns apart.
+template <int VEC> struct Lane4 { Vals<VEC> c[4 / VEC]; };
+template <typename T, int VEC> struct LaneRaw { typename Raw<T, VEC>::type c[4 / VEC]; };
+template <int VEC, typename T>
+__device__ __forceinline__ void load_lane(LaneRaw<T, VEC>& v, const T* p, const bool* on) {
+#pragma unroll
+  for (int u = 0; u < 4 / VEC; ++u)
+    if (on[u]) v.c[u] = load_raw<VEC>(p + 32 * VEC * u);
+}
+template <int VEC> __device__ __forceinline__ void store_lane(float* p, const Lane4<VEC>& v, const bool* on) {
+#pragma unroll
+  for (int u = 0; u < 4 / VEC; ++u)
+    if (on[u]) store_vals<VEC>(p + 32 * VEC * u, v.c[u]);
+}
+template <int VEC, typename T>
+__device__ __forceinline__ void add_lane(Lane4<VEC>& s, const LaneRaw<T, VEC>& v, bool fresh) {
+#pragma unroll
+  for (int u = 0; u < 4 / VEC; ++u) {
+    const Vals<VEC> x = unpack(v.c[u]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s.c[u].v[j] = fresh ? x.v[j] : s.c[u].v[j] + x.v[j];
   }
-  __syncthreads();
-  const int count = warp_n[0] + warp_n[1];
-  if (count == 0) return;
-  const bool open_left = crosses(begin), open_right = crosses(end);
-  const int col = (share * (int)blockDim.x + (int)threadIdx.x) * VEC;
-  if (col >= a.cols) return;
-  const In* dw = FIRST ? dy + (long long)w * a.n * a.cols + col : nullptr;
-  const float* bw = FIRST ? nullptr : below + (long long)w * 2 * chunks_below * a.cols + col;
-  float* gw = grads + (long long)w * a.stride + a.offset + col;
-  float* sw = slots + ((long long)w * chunks + chunk) * 2 * a.cols + col;
-  Vals<VEC> sum{};
-  bool first_run = true;
-  for (int e0 = 0; e0 < count; e0 += 8) {
-    Vals<VEC> v[8];
+}
+template <int VEC, bool ACC>
+__device__ __forceinline__ void scale_lane(Lane4<VEC>& s, float scale, const LaneRaw<float, VEC>& o) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      v[k] = Vals<VEC>{};
-      if (e0 + k < count) {
-        const long long src = (long long)ssrc[e0 + k] * a.cols;
-        if constexpr (FIRST) v[k] = load_vals<VEC>(dw + src);
-        else v[k] = load_vals<VEC>(bw + src);
-      }
+  for (int u = 0; u < 4 / VEC; ++u) {
+    const Vals<VEC> x = unpack(o.c[u]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s.c[u].v[j] = ACC ? fmaf(scale, s.c[u].v[j], x.v[j]) : scale * s.c[u].v[j];
+  }
+}
+
+// In: the values' type at the first level (FIRST); float above.
+template <typename In, int VEC, bool FIRST, bool ACC>
+__global__ void __launch_bounds__(256, ACC ? (sizeof(In) == 2 ? 3 : 2) : (sizeof(In) == 2 ? 4 : 3))
+embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs a, int groups, float scale, float* grads,
+                     const unsigned* __restrict__ sorted, const EmbZero z) {
+  constexpr int kPart = FIRST ? kChunk / 8 : 2 * kFan / 8;  // entries per warp
+  __shared__ unsigned skey[8 * kPart + 2], smask[8], sends[8];
+  __shared__ __align__(16) float shead[8][128];  // read and written four columns at a time
+  let_next_start();
+  await_previous();
+  if (!ACC && (int)blockIdx.x >= z.first_block) {
+    zero_piece_around(z, a, sorted);
+    return;
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int wc = blockIdx.x / groups, group = blockIdx.x % groups;  // column group fastest, then chunk, then worker
+  const int w = wc / l.chunks, chunk = wc % l.chunks;
+  const unsigned* kw = l.keys + (long long)w * l.count;
+  const int c0 = chunk * 8 * kPart;
+
+  // the chunk's keys at skey[1 ..], the keys beside it at either end
+  for (int t = threadIdx.x; t < 8 * kPart + 2; t += 256) {
+    const int at = c0 - 1 + t;
+    const unsigned key = at >= 0 && at < l.count ? kw[at] : kNoKey;
+    skey[t] = key == (unsigned)a.rows ? kNoKey : key;
+  }
+  unsigned pos = 0u;
+  if (FIRST && lane < kPart && c0 + kPart * warp + lane < l.count) pos = l.pos[(long long)w * l.count + c0 + kPart * warp + lane];
+  __syncthreads();
+  const unsigned* own = skey + 1 + kPart * warp;
+  const unsigned key = lane < kPart ? own[lane] : kNoKey;
+  const unsigned mask = __ballot_sync(0xffffffffu, key != kNoKey);
+  if (lane == 0) smask[warp] = mask;
+  __syncthreads();
+  // an entry ends a run if the next one has another row; the chunk's last one always does
+  unsigned next = kNoKey;
+  if (FIRST) {
+    if (lane < kPart && kPart * warp + lane + 1 < 8 * kPart) next = own[lane + 1];
+  } else {
+    unsigned behind = lane == 31 ? 0u : mask >> (lane + 1) << (lane + 1);
+    int q = warp;
+    while (behind == 0u && q + 1 < 8) behind = smask[++q];
+    if (behind != 0u) next = skey[kPart * q + __ffs(behind)];
+  }
+  const unsigned ends = __ballot_sync(0xffffffffu, key != kNoKey && key != next);
+  if (lane == 0) sends[warp] = ends;
+  // is the chunk's first (last) run open to the left (right), and the warp's first run?
+  const bool open_left = skey[1] != kNoKey && (!FIRST || skey[0] == skey[1]);
+  const bool open_right = skey[8 * kPart + 1] != kNoKey && (!FIRST || skey[8 * kPart] == skey[8 * kPart + 1]);
+  int before = warp - 1, last_warp = 7;
+  while (before >= 0 && smask[before] == 0u) --before;
+  while (last_warp > 0 && smask[last_warp] == 0u) --last_warp;
+  const int last_entry = 31 - __clz(smask[last_warp]);
+  const bool left = before < 0 ? warp == 0 && open_left
+                               : mask != 0u && skey[kPart * before + 32 - __clz(smask[before])] == own[__ffs(mask) - 1];
+  __syncthreads();
+  if (group == 0 && l.chunks > 1 && threadIdx.x < 2) {
+    int runs = 0;
+    for (int q = 0; q < 8; ++q) runs += __popc(sends[q]);
+    unsigned slot_key = kNoKey;
+    if (threadIdx.x == 0 && open_left) slot_key = skey[1];
+    if (threadIdx.x == 1 && open_right && !(open_left && runs == 1)) slot_key = skey[kPart * last_warp + 1 + last_entry];
+    l.slot_keys[(long long)wc * 2 + threadIdx.x] = slot_key;
+  }
+
+  const int col = group * 128 + lane * VEC;
+  bool on[4 / VEC], all_on[4 / VEC];
+#pragma unroll
+  for (int u = 0; u < 4 / VEC; ++u) {
+    on[u] = col + 32 * VEC * u < a.cols;
+    all_on[u] = true;
+  }
+  const In* iw = in + (long long)w * l.count * a.cols + col;
+  float* gw = grads + (long long)w * a.stride + a.offset + col;
+  float* tail_slot = l.slots + ((long long)wc * 2 + 1) * a.cols + col;
+  float* head = shead[warp] + lane * VEC;
+  Lane4<VEC> sum;
+  bool fresh = true, first_run = true;
+  // 32 registers of loads in flight: 16 entries of bf16 at once, of fp32 (and of rows that are added to) eight
+  constexpr int kBatch = sizeof(In) == 2 && !ACC ? 16 : 8;
+  unsigned todo = mask;
+#pragma unroll 1
+  while (todo != 0u) {
+    LaneRaw<In, VEC> v[kBatch];
+    LaneRaw<float, VEC> o[ACC ? kBatch : 1];
+    unsigned batch = todo;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (todo == 0u) continue;
+      const int e = __ffs(todo) - 1;
+      todo &= todo - 1u;
+      const unsigned from = FIRST ? __shfl_sync(0xffffffffu, pos, e) : (unsigned)(c0 + kPart * warp + e);
+      load_lane<VEC>(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
+      if (ACC && (ends >> e & 1u)) load_lane<VEC>(o[k], (const float*)gw + (unsigned long long)own[e] * (unsigned)a.cols, on);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int e = e0 + k;
-      if (e >= count) break;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) sum.v[j] += v[k].v[j];
-      const bool last = e + 1 == count;
-      if (!last && skey[e + 1] == skey[e]) continue;
-      if (first_run && open_left) {
-        store_vals<VEC>(sw, sum);
-      } else if (last && open_right) {
-        store_vals<VEC>(sw + a.cols, sum);
+    for (int k = 0; k < kBatch; ++k) {
+      if (batch == 0u) break;
+      const int e = __ffs(batch) - 1;
+      batch &= batch - 1u;
+      add_lane<VEC>(sum, v[k], fresh);
+      fresh = ends >> e & 1u;
+      if (!fresh) continue;
+      if (first_run && left) {
+        store_lane<VEC>(head, sum, all_on);
+      } else if (open_right && warp == last_warp && e == last_entry) {
+        store_lane<VEC>(tail_slot, sum, on);
       } else {
-        float* g = gw + (long long)skey[e] * a.cols;
-        Vals<VEC> o{};
-        if (accumulate) o = load_vals<VEC>(g);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) o.v[j] = fmaf(scale, sum.v[j], o.v[j]);
-        store_vals<VEC>(g, o);
+        scale_lane<VEC, ACC>(sum, scale, o[ACC ? k : 0]);
+        store_lane<VEC>(gw + (unsigned long long)own[e] * (unsigned)a.cols, sum, on);
       }
-      sum = Vals<VEC>{};
       first_run = false;
     }
+  }
+  bool pending = !fresh;  // a run goes on behind this warp
+  if (pending && first_run && left) {
+    store_lane<VEC>(head, sum, all_on);
+    pending = false;
+  }
+  __syncthreads();
+  // the rest of a run that ends in a later warp: adds the heads up to there, returns whether it ends the chunk
+  auto finish_run = [&](int q) {
+    for (;; ++q) {
+      if (smask[q] == 0u) continue;
+      LaneRaw<float, VEC> h;
+      load_lane<VEC>(h, (const float*)shead[q] + lane * VEC, all_on);
+      add_lane<VEC>(sum, h, false);
+      if (sends[q] != 0u) return q == last_warp && __ffs(sends[q]) - 1 == last_entry;
+    }
+  };
+  if (pending) {
+    const unsigned row = own[31 - __clz(mask)];
+    float* g = gw + (unsigned long long)row * (unsigned)a.cols;
+    LaneRaw<float, VEC> o;
+    if (ACC) load_lane<VEC>(o, (const float*)g, on);
+    if (finish_run(warp + 1) && open_right) {
+      store_lane<VEC>(tail_slot, sum, on);
+    } else {
+      scale_lane<VEC, ACC>(sum, scale, o);
+      store_lane<VEC>(g, sum, on);
+    }
+  }
+  if (warp == 0 && open_left) {
+    LaneRaw<float, VEC> h;
+    load_lane<VEC>(h, (const float*)shead[0] + lane * VEC, all_on);
+    add_lane<VEC>(sum, h, true);
+    if (sends[0] == 0u) finish_run(1);
+    store_lane<VEC>(tail_slot - a.cols, sum, on);
   }
 }
 
@@ -398,10 +613,10 @@ static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Workspace of the gradient: two (row, position) lists, the radix sort's histograms, the levels' slots.
 struct EmbPlan {
-  size_t keys[2], pos[2], hist, slots[2], total;
+  size_t keys[2], pos[2], hist, slots[2], slot_keys[2], rows_taken, total;
   int n_tiles;
 };
-static EmbPlan emb_plan(int W, int cols, long long n) {
+static EmbPlan emb_plan(int W, int rows, int cols, long long n) {
   EmbPlan p{};
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = align256(o + bytes); return at; };
@@ -413,15 +628,19 @@ static EmbPlan emb_plan(int W, int cols, long long n) {
   p.n_tiles = (int)((n + kSortTile - 1) / kSortTile);
   p.hist = take(radix ? sizeof(unsigned) * (size_t)W * 256 * p.n_tiles : 0);
   // slots of the first level, and of the second (the third uses the first's again, and so on)
-  const long long c1 = (n + kChunk - 1) / kChunk, c2 = (c1 + kChunk - 1) / kChunk;
+  const long long c1 = (n + kChunk - 1) / kChunk, c2 = (c1 + kFan - 1) / kFan;
   p.slots[0] = take(c1 > 1 ? sizeof(float) * (size_t)W * c1 * 2 * cols : 0);
   p.slots[1] = take(c2 > 1 ? sizeof(float) * (size_t)W * c2 * 2 * cols : 0);
+  p.slot_keys[0] = take(c1 > 1 ? sizeof(unsigned) * (size_t)W * c1 * 2 : 0);
+  p.slot_keys[1] = take(c2 > 1 ? sizeof(unsigned) * (size_t)W * c2 * 2 : 0);
+  p.rows_taken = take(radix ? sizeof(unsigned) * (size_t)W * ((rows + 31) / 32) : 0);
   p.total = o < 256 ? 256 : o;
   return p;
 }
 
 size_t embedding_workspace(const acc_ctx* ctx, int layer, long long n) {
-  return emb_plan(ctx->cfg.n_workers, ctx->plan.layers[layer].cols, n).total;
+  const DevLayer& L = ctx->plan.layers[layer];
+  return emb_plan(ctx->cfg.n_workers, L.rows, L.cols, n).total;
 }
 
 template <typename Tok, typename Out, int VEC>
@@ -449,99 +668,127 @@ cudaError_t launch_embedding_lookup(acc_ctx* ctx, int layer, const float* params
   return cudaGetLastError();
 }
 
-template <typename In, int VEC>
-static void sum_levels(acc_ctx* ctx, const EmbArgs& a, const EmbPlan& p, char* ws, const unsigned* keys,
-                       const unsigned* pos, const void* dy, float scale, int accumulate, float* grads, cudaStream_t s) {
-  const int W = ctx->cfg.n_workers;
-  // columns in equal shares of at most 256 threads
-  const int nv = a.cols / VEC, shares = (nv + 255) / 256, threads = ((nv + shares - 1) / shares + 31) / 32 * 32;
-  const int block = threads < 64 ? 64 : threads;
-  const int per = (nv + block - 1) / block;
-  float* slots[2] = {reinterpret_cast<float*>(ws + p.slots[0]), reinterpret_cast<float*>(ws + p.slots[1])};
-  long long span = kChunk;
-  int chunks = (a.n + kChunk - 1) / kChunk;
-  {
-    PhaseTimer pt(ctx, PH_EMB_SUM, s);
-    embedding_sum_kernel<In, VEC, true><<<(unsigned)((long long)W * chunks * per), block, 0, s>>>(
-        static_cast<const In*>(dy), nullptr, keys, pos, a, 1, 0, chunks, per, scale, accumulate, grads, slots[0]);
+// The kernels of one gradient call, in order: `first` for the one that starts behind everything before the call, the others
+// may start early.  Each takes up to `share` of the pieces that are still to clear.
+constexpr int kAll = 0x7fffffff;
+// Pieces (64 KB) that take about as long as a launch of the sort, the sums of a few hundred tokens, a level of joining.
+constexpr int kSortShare = 384, kSumShare = 640, kJoinShare = 192;
+struct EmbLaunch {
+  acc_ctx* ctx;
+  cudaStream_t s;
+  EmbZero z;
+  int pieces;
+  bool first = true;
+  cudaError_t err = cudaSuccess;
+
+  template <typename... Params, typename... Args>
+  void operator()(int phase, void (*kernel)(Params...), long long blocks, int threads, int share, Args... args) {
+    const int mine = pieces - z.from < share ? pieces - z.from : share;
+    z.first_block = (int)blocks;
+    if (blocks + mine > 0 && err == cudaSuccess) {
+      PhaseTimer pt(ctx, phase, s);
+      cudaLaunchAttribute attr{};
+      attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      attr.val.programmaticStreamSerializationAllowed = 1;
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3((unsigned)(blocks + mine));
+      cfg.blockDim = dim3((unsigned)threads);
+      cfg.stream = s;
+      cfg.attrs = &attr;
+      cfg.numAttrs = first ? 0 : 1;
+      first = false;
+      err = cudaLaunchKernelEx(&cfg, kernel, args..., z);
+    }
+    z.from += mine;
   }
-  for (int level = 1; chunks > 1; ++level) {
-    const int below = chunks;
-    chunks = (below + kChunk - 1) / kChunk;
-    PhaseTimer pt(ctx, PH_EMB_JOIN, s);
-    embedding_sum_kernel<float, VEC, false><<<(unsigned)((long long)W * chunks * per), block, 0, s>>>(
-        nullptr, slots[(level - 1) & 1], keys, pos, a, (int)span, below, chunks, per, scale, accumulate, grads,
-        slots[level & 1]);
-    span *= kChunk;
+};
+
+template <typename In, int VEC>
+static void sum_levels(EmbLaunch& go, const EmbArgs& a, const EmbPlan& p, char* ws, const unsigned* keys,
+                       const unsigned* pos, const void* dy, float scale, int accumulate, float* grads) {
+  const int W = go.ctx->cfg.n_workers;
+  const int groups = (a.cols + 127) / 128;
+  auto level = [&](int k, const unsigned* lkeys, const unsigned* lpos, int count, int chunks) {
+    return EmbLevel{lkeys, lpos, count, chunks, reinterpret_cast<float*>(ws + p.slots[k & 1]),
+                    reinterpret_cast<unsigned*>(ws + p.slot_keys[k & 1])};
+  };
+  int chunks = (a.n + kChunk - 1) / kChunk, joins = 0;
+  for (int c = chunks; c > 1; c = (c + kFan - 1) / kFan) ++joins;
+  // what is still to clear is cleared beside the sums, but for a share that each of the short joining levels keeps
+  const int all = go.pieces, left = all - go.z.from, kept = std::min(left, joins * kJoinShare);
+  go.pieces = all - kept;
+  EmbLevel l = level(0, keys, pos, a.n, chunks);
+  go(PH_EMB_SUM, accumulate ? embedding_sum_kernel<In, VEC, true, true> : embedding_sum_kernel<In, VEC, true, false>,
+     (long long)W * chunks * groups, 256, kAll, static_cast<const In*>(dy), l, a, groups, scale, grads, keys);
+  go.pieces = all;
+  for (int k = 1; chunks > 1; ++k) {
+    const float* in = l.slots;
+    const unsigned* in_keys = l.slot_keys;
+    const int count = 2 * chunks;
+    chunks = (chunks + kFan - 1) / kFan;
+    l = level(k, in_keys, nullptr, count, chunks);
+    go(PH_EMB_JOIN, accumulate ? embedding_sum_kernel<float, VEC, false, true> : embedding_sum_kernel<float, VEC, false, false>,
+       (long long)W * chunks * groups, 256, chunks == 1 ? kAll : kJoinShare, in, l, a, groups, scale, grads, keys);
   }
 }
 
 cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, bool tok64, long long n, float scale,
                                   const void* dy, bool bf16, float* grads, int accumulate, void* workspace,
                                   cudaStream_t s) {
+  if (n == 0 && accumulate) return cudaSuccess;
   const DevLayer& L = ctx->plan.layers[layer];
   const int W = ctx->cfg.n_workers;
-  EmbArgs a{L.offset, ctx->cfg.worker_stride, (long long)L.rows * L.cols, L.rows, L.cols, (int)n};
+  const EmbArgs a{L.offset, ctx->cfg.worker_stride, (long long)L.rows * L.cols, L.rows, L.cols, (int)n};
   char* ws = static_cast<char*>(workspace);
-  const long long pieces = (a.size + kZeroPiece - 1) / kZeroPiece;
-  const long long zero_blocks = accumulate ? 0 : pieces * W;
-  if (n == 0 && accumulate) return cudaSuccess;
-  const EmbPlan p = emb_plan(W, L.cols, n);
+  const int pieces = (int)((a.size + kZeroPiece - 1) / kZeroPiece);
+  const EmbPlan p = emb_plan(W, L.rows, L.cols, n);
+  unsigned* rows_taken = n > kRankMost && !accumulate ? reinterpret_cast<unsigned*>(ws + p.rows_taken) : nullptr;
+  EmbLaunch go{ctx, s, EmbZero{grads, 0, 0, pieces, rows_taken}, accumulate ? 0 : pieces * W};
   unsigned* keys[2] = {reinterpret_cast<unsigned*>(ws + p.keys[0]), reinterpret_cast<unsigned*>(ws + p.keys[1])};
   unsigned* pos[2] = {reinterpret_cast<unsigned*>(ws + p.pos[0]), reinterpret_cast<unsigned*>(ws + p.pos[1])};
+  // Clearing a piece whole costs the rows with tokens a second write, clearing around them some 5 % of the piece's time:
+  // with fewer tokens than a sixteenth of the rows all but what fills the sums' time goes with the sort.
+  const int ahead = n == 0 ? kAll : n * 16 < a.rows ? std::max(0, go.pieces - kSumShare - kJoinShare) : kSortShare;
   int at = 0;
+  const auto* tok8 = static_cast<const long long*>(tokens);
+  const auto* tok4 = static_cast<const int*>(tokens);
   if (n <= kRankMost) {
-    const int per_worker = (int)((n + kRankBlock - 1) / kRankBlock), rank_blocks = per_worker * W;
-    PhaseTimer pt(ctx, PH_EMB_RANK, s);
-    const unsigned grid = (unsigned)(rank_blocks + zero_blocks);
+    const int per_worker = (int)((n + kRankBlock - 1) / kRankBlock);
     if (tok64)
-      embedding_rank_kernel<long long><<<grid, kRankBlock, 0, s>>>(static_cast<const long long*>(tokens), a, keys[0], pos[0],
-                                                                   rank_blocks, per_worker, grads, pieces, ctx->d_status);
+      go(PH_EMB_RANK, embedding_rank_kernel<long long>, (long long)per_worker * W, kRankThreads, ahead, tok8, a, keys[0],
+         pos[0], per_worker, ctx->d_status);
     else
-      embedding_rank_kernel<int><<<grid, kRankBlock, 0, s>>>(static_cast<const int*>(tokens), a, keys[0], pos[0], rank_blocks,
-                                                             per_worker, grads, pieces, ctx->d_status);
+      go(PH_EMB_RANK, embedding_rank_kernel<int>, (long long)per_worker * W, kRankThreads, ahead, tok4, a, keys[0], pos[0],
+         per_worker, ctx->d_status);
   } else {
     unsigned* hist = reinterpret_cast<unsigned*>(ws + p.hist);
-    const int blocks = p.n_tiles * W;
-    {
-      PhaseTimer pt(ctx, PH_EMB_KEYS, s);
-      const unsigned grid = (unsigned)(blocks + zero_blocks);
-      if (tok64)
-        embedding_keys_kernel<long long><<<grid, kSortThreads, 0, s>>>(static_cast<const long long*>(tokens), a, keys[0],
-                                                                       pos[0], hist, p.n_tiles, blocks, grads, pieces,
-                                                                       ctx->d_status);
-      else
-        embedding_keys_kernel<int><<<grid, kSortThreads, 0, s>>>(static_cast<const int*>(tokens), a, keys[0], pos[0], hist,
-                                                                 p.n_tiles, blocks, grads, pieces, ctx->d_status);
-    }
+    const long long blocks = (long long)p.n_tiles * W;
+    if (tok64)
+      go(PH_EMB_KEYS, embedding_keys_kernel<long long>, blocks, kSortThreads, ahead, tok8, a, keys[0], pos[0], hist,
+         p.n_tiles, ctx->d_status);
+    else
+      go(PH_EMB_KEYS, embedding_keys_kernel<int>, blocks, kSortThreads, ahead, tok4, a, keys[0], pos[0], hist, p.n_tiles,
+         ctx->d_status);
     for (int shift = 0; shift < 32 && (shift == 0 || (a.rows >> shift) != 0); shift += 8) {
-      if (shift > 0) {
-        PhaseTimer pt(ctx, PH_EMB_HIST, s);
-        embedding_hist_kernel<<<blocks, kSortThreads, 0, s>>>(keys[at], a.n, shift, hist, p.n_tiles);
-      }
-      {
-        PhaseTimer pt(ctx, PH_EMB_SCAN, s);
-        embedding_scan_kernel<<<W, 1024, 0, s>>>(hist, p.n_tiles);
-      }
-      {
-        PhaseTimer pt(ctx, PH_EMB_SCATTER, s);
-        embedding_scatter_kernel<<<blocks, kSortThreads, 0, s>>>(keys[at], pos[at], a.n, shift, hist, p.n_tiles,
-                                                                 keys[at ^ 1], pos[at ^ 1]);
-      }
+      if (shift > 0) go(PH_EMB_HIST, embedding_hist_kernel, blocks, kSortThreads, kSortShare, keys[at], a, shift, hist, p.n_tiles);
+      const bool scan = p.n_tiles > kScanTiles;
+      if (scan) go(PH_EMB_SCAN, embedding_scan_kernel, W, 1024, kSortShare, hist, p.n_tiles, a);
+      go(PH_EMB_SCATTER, scan ? embedding_scatter_kernel<true> : embedding_scatter_kernel<false>, blocks, kSortThreads, kSortShare, keys[at], pos[at], a, shift, hist,
+         p.n_tiles, keys[at ^ 1], pos[at ^ 1], (int)(shift >= 24 || (a.rows >> (shift + 8)) == 0));
       at ^= 1;
     }
   }
   if (n > 0) {
-    auto go = [&](auto in) {
+    auto sums = [&](auto in) {
       using In = decltype(in);
-      if (L.vec == 4) sum_levels<In, 4>(ctx, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads, s);
-      else if (L.vec == 2) sum_levels<In, 2>(ctx, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads, s);
-      else sum_levels<In, 1>(ctx, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads, s);
+      if (L.vec == 4) sum_levels<In, 4>(go, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads);
+      else if (L.vec == 2) sum_levels<In, 2>(go, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads);
+      else sum_levels<In, 1>(go, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads);
     };
-    if (bf16) go(__nv_bfloat16());
-    else go(0.f);
+    if (bf16) sums(__nv_bfloat16());
+    else sums(0.f);
   }
-  return cudaGetLastError();
+  return go.err == cudaSuccess ? cudaGetLastError() : go.err;
 }
 
 }  // namespace acc
