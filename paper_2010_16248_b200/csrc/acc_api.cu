@@ -687,7 +687,7 @@ const char* acc_profile_kernel_name(int32_t i) {
       "detect_batch_kernel", "psgd_pfold_kernel", "vec_exchange_kernel", "psgd_qmerge_kernel",
       "topk_decompress_packed_kernel", "topk_flush_kernel", "moments_partial_kernel", "moments_final_kernel",
       "adamw_coef_kernel", "adamw_kernel", "adamw_8bit_kernel", "clip_factor_kernel",
-      "embedding_lookup_kernel", "embedding_rank_kernel", "embedding_keys_kernel", "embedding_hist_kernel",
+      "embedding_lookup_kernel", "embedding_small_kernel", "embedding_keys_kernel", "embedding_hist_kernel",
       "embedding_scan_kernel", "embedding_scatter_kernel", "embedding_sum_kernel", "embedding_join_kernel"};
   return (i >= 0 && i < PH_COUNT) ? names[i] : "";
 }

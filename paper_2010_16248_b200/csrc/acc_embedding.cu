@@ -2,6 +2,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "acc_internal.cuh"
 
@@ -106,57 +107,40 @@ struct EmbArgs {
   int rows, cols, n;     // n: tokens per worker
 };
 
-// The next kernel of a call may start while this one runs; it waits for it in full before it touches memory.  (Only the
-// call's first kernel is launched without that permission, so it starts behind everything queued before the call.)
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-// Overwriting a gradient is mostly writing zeros: pieces of kZeroPiece elements, handed to the call's kernels behind their
-// own blocks.  While the tokens are sorted whole pieces are cleared, as many as fill that time (zero_piece; a row written
-// later is then written twice); the rest are cleared beside the sums, leaving the rows out that the sums write
-// (zero_piece_around).  So the memory system never waits for the sort or the last level of sums.
+// Overwriting a gradient is mostly writing zeros: pieces of PIECE elements, handed to the call's kernels behind their own
+// blocks, so that the memory system never waits for a sort or for the last sums.
 struct EmbZero {
   float* grads;
   int first_block;       // blocks behind this one clear pieces
   int from;              // number of the first such block's piece
   int pieces_per_worker;
-  unsigned* rows_taken;  // see zero_piece_around
+  unsigned* rows_taken;  // radix sort: [W][(rows + 31) / 32], a bit for each row that some token names
 };
-constexpr int kZeroPiece = 16384;
 
-__device__ __forceinline__ void zero_piece(const EmbZero& z, const EmbArgs& a) {
+// A piece whole; a row that the sums write later is then written twice.
+template <int PIECE> __device__ __forceinline__ void zero_piece(const EmbZero& z, const EmbArgs& a) {
   const int piece = z.from + (int)blockIdx.x - z.first_block;
   const int w = piece / z.pieces_per_worker;
-  const long long e0 = (long long)(piece - w * z.pieces_per_worker) * kZeroPiece;
+  const long long e0 = (long long)(piece - w * z.pieces_per_worker) * PIECE;
   float* g = z.grads + w * a.stride + a.offset + e0;
-  const int n = (int)min((long long)kZeroPiece, a.size - e0);
+  const int n = (int)min((long long)PIECE, a.size - e0);
   for (int i = 4 * (int)threadIdx.x; i + 4 <= n; i += 4 * (int)blockDim.x) st_stream4(g + i, make_float4(0.f, 0.f, 0.f, 0.f));
   for (int i = (n & ~3) + (int)threadIdx.x; i < n; i += blockDim.x) g[i] = 0.f;
 }
 
-// The rows of a piece that some token names: a bit each in `rows_taken` ([W][(rows + 31) / 32], set by the last pass of the
-// radix sort), or, where that is null, what a look at all of the worker's few sorted keys says.
-__device__ __forceinline__ void zero_piece_around(const EmbZero& z, const EmbArgs& a, const unsigned* __restrict__ keys) {
-  __shared__ unsigned taken[kZeroPiece / 32 + 3];  // bit r: row (row0 & ~31) + r
+// A piece without the rows that some token names.  mark(w, taken, row0, row1) sets bit r - (row0 & ~31) of `taken` for each
+// such row r in [row0, row1]; taken has room for PIECE / 32 + 3 words and is zero.
+template <int PIECE, typename Mark>
+__device__ __forceinline__ void zero_piece_around(const EmbZero& z, const EmbArgs& a, unsigned* taken, Mark mark) {
   const int piece = z.from + (int)blockIdx.x - z.first_block;
   const int w = piece / z.pieces_per_worker;
-  const unsigned e0 = (unsigned)(piece - w * z.pieces_per_worker) * kZeroPiece, cols = (unsigned)a.cols;
+  const unsigned e0 = (unsigned)(piece - w * z.pieces_per_worker) * PIECE, cols = (unsigned)a.cols;
   float* g = z.grads + w * a.stride + a.offset + e0;
-  const int n = (int)min((long long)kZeroPiece, a.size - e0);
-  const unsigned row0 = e0 / cols, row1 = (e0 + (unsigned)n - 1u) / cols, word0 = row0 >> 5, words = (row1 >> 5) - word0 + 1u;
-  if (z.rows_taken != nullptr) {
-    const unsigned* bits = z.rows_taken + (long long)w * ((a.rows + 31) / 32) + word0;
-    for (unsigned i = threadIdx.x; i < words; i += blockDim.x) taken[i] = bits[i];
-  } else {
-    const unsigned* kw = keys + (long long)w * a.n;
-    for (unsigned i = threadIdx.x; i < words; i += blockDim.x) taken[i] = 0u;
-    __syncthreads();
-#pragma unroll 4
-    for (int j = threadIdx.x; j < a.n; j += blockDim.x) {
-      const unsigned key = kw[j];
-      if (key >= row0 && key <= row1) atomicOr(&taken[(key >> 5) - word0], 1u << (key & 31));
-    }
-  }
+  const int n = (int)min((long long)PIECE, a.size - e0);
+  const unsigned row0 = e0 / cols, row1 = (e0 + (unsigned)n - 1u) / cols, word0 = row0 >> 5;
+  for (unsigned i = threadIdx.x; i <= (row1 >> 5) - word0; i += blockDim.x) taken[i] = 0u;
+  __syncthreads();
+  mark(w, taken, row0, row1);
   __syncthreads();
   auto free_row = [&](unsigned r) { return !(taken[(r >> 5) - word0] >> (r & 31) & 1u); };
   if (a.cols < 64) {  // element by element: which row a narrow one lies in, x / cols, exact for x below 2^32 / cols
@@ -179,52 +163,227 @@ __device__ __forceinline__ void zero_piece_around(const EmbZero& z, const EmbArg
   }
 }
 
-// Up to kRankMost tokens per worker: a token's place is the number of tokens before it in (row, position) order, counted
-// against all of them in shared memory.  Quadratic, but 64 tokens per block and one launch where the radix sort takes
-// four or more.
-constexpr int kRankMost = 2048, kRankThreads = 256, kRankBlock = kRankThreads / 4;  // tokens, threads, tokens per block
-template <typename Tok>
-__global__ void __launch_bounds__(kRankThreads)
-embedding_rank_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __restrict__ keys, unsigned* __restrict__ pos,
-                      int blocks_per_worker, int* status, EmbZero z) {
-  let_next_start();
-  if ((int)blockIdx.x >= z.first_block) {
-    zero_piece(z, a);
-    return;
+// The next kernel of a call may start while this one runs; it waits for it in full before it touches memory.  (Only the
+// call's first kernel is launched without that permission, so it starts behind everything queued before the call.)
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Columns of a lane: COLS / VEC vectors of VEC adjacent ones, 32 VEC columns apart.
+template <int VEC, int COLS> struct Lane { Vals<VEC> c[COLS / VEC]; };
+template <typename T, int VEC, int COLS> struct LaneRaw { typename Raw<T, VEC>::type c[COLS / VEC]; };
+template <int VEC, int COLS, typename T>
+__device__ __forceinline__ void load_lane(LaneRaw<T, VEC, COLS>& v, const T* p, const bool* on) {
+#pragma unroll
+  for (int u = 0; u < COLS / VEC; ++u)
+    if (on[u]) v.c[u] = load_raw<VEC>(p + 32 * VEC * u);
+}
+template <int VEC, int COLS> __device__ __forceinline__ void store_lane(float* p, const Lane<VEC, COLS>& v, const bool* on) {
+#pragma unroll
+  for (int u = 0; u < COLS / VEC; ++u)
+    if (on[u]) store_vals<VEC>(p + 32 * VEC * u, v.c[u]);
+}
+template <int VEC, int COLS, typename T>
+__device__ __forceinline__ void add_lane(Lane<VEC, COLS>& s, const LaneRaw<T, VEC, COLS>& v) {
+#pragma unroll
+  for (int u = 0; u < COLS / VEC; ++u) {
+    const Vals<VEC> x = unpack(v.c[u]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s.c[u].v[j] += x.v[j];
   }
-  __shared__ __align__(16) unsigned sk[kRankMost];
-  const int w = blockIdx.x / blocks_per_worker, first = (int)(blockIdx.x % blocks_per_worker) * kRankBlock;
-  const Tok* tok = tokens + (long long)w * a.n;
-  const int n4 = (a.n + 3) & ~3;
-  for (int j = threadIdx.x; j < n4; j += kRankThreads)
-    sk[j] = j < a.n ? token_row((long long)tok[j], a.rows, status) : 0xffffffffu;
-  __syncthreads();
-  // four lanes per token, each against every fourth vector of keys: those before the token's own vector count if they are
-  // smaller or equal, the others if they are smaller; equal ones before it in its own vector are added by the first lane
-  const int i = first + (int)(threadIdx.x >> 2), part = threadIdx.x & 3, own = i & ~3;
-  const unsigned key = i < a.n ? sk[i] : 0u;
-  int rank = 0, j = 4 * part;
-#pragma unroll 4
-  for (; j < min(own, n4); j += 16) {
-    const uint4 o = *reinterpret_cast<const uint4*>(sk + j);
-    rank += (o.x <= key) + (o.y <= key) + (o.z <= key) + (o.w <= key);
-  }
-#pragma unroll 4
-  for (; j < n4; j += 16) {
-    const uint4 o = *reinterpret_cast<const uint4*>(sk + j);
-    rank += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
-  }
-  if (part == 0 && i < a.n)
-    for (int k = own; k < i; ++k) rank += sk[k] == key;
-  rank += __shfl_xor_sync(0xffffffffu, rank, 1);
-  rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-  if (part == 0 && i < a.n) {
-    keys[(long long)w * a.n + rank] = key;
-    pos[(long long)w * a.n + rank] = (unsigned)i;
+}
+template <bool ACC, int VEC, int COLS>
+__device__ __forceinline__ void scale_lane(Lane<VEC, COLS>& s, float scale, const LaneRaw<float, VEC, COLS>& o) {
+#pragma unroll
+  for (int u = 0; u < COLS / VEC; ++u) {
+    const Vals<VEC> x = unpack(o.c[u]);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s.c[u].v[j] = ACC ? fmaf(scale, s.c[u].v[j], x.v[j]) : scale * s.c[u].v[j];
   }
 }
 
-// More tokens: a stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.
+// ---- up to kSmallMost tokens per worker: one launch -----------------------------------------------------------------
+// A block takes one worker and 64 columns.  It sorts all of the worker's tokens itself, in shared memory (2 us, the same in
+// every block, in place of a launch that every block would wait for), and hands every warp an equal share of the sorted
+// entries.  A run that crosses from one warp to the next is finished by the warp where it begins, from the sums that the
+// others leave in shared memory.  Blocks behind those clear the rest of the layer, around the rows of the worker's tokens.
+constexpr int kSmallMost = 2048, kSmallCols = 64, kSmallPiece = 32768;
+constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21;  // a word holds row and position; tables of more rows, or
+constexpr int kSmallWide = 1 << 20;                       // of more columns (32-bit offsets), take the long way
+
+// Ascending order of the block's words by a bitonic network over the first count2 (a power of two) of them; thread t holds
+// words t + r * THREADS.  Partners in a warp trade by shuffles, others through shared memory (two buffers in turn, so one
+// barrier a step).  Where the network sorts downwards the words are complemented, so that every step keeps the smaller word
+// at the lower place.
+template <int E, int THREADS>
+__device__ __forceinline__ void sort_words(unsigned (&x)[E], int count2, unsigned (*buf)[kSmallMost]) {
+  const int t = threadIdx.x, lane = t & 31;
+  int turn = 0;
+  for (int k = 2; k <= count2; k <<= 1) {
+#pragma unroll
+    for (int r = 0; r < E; ++r)
+      if ((t + r * THREADS) & k) x[r] = ~x[r];
+    for (int j = k >> 1; j >= 32; j >>= 1) {
+      if (E > 1 && j >= THREADS) {  // both words are this thread's
+#pragma unroll
+        for (int r = 0; r < E; ++r)
+#pragma unroll
+          for (int q = r + 1; q < E; ++q)
+            if ((q ^ r) * THREADS == j) {
+              const unsigned lo = min(x[r], x[q]), hi = max(x[r], x[q]);
+              x[r] = lo;
+              x[q] = hi;
+            }
+        continue;
+      }
+#pragma unroll
+      for (int r = 0; r < E; ++r) buf[turn][t + r * THREADS] = x[r];
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < E; ++r) {
+        const unsigned o = buf[turn][(t ^ j) + r * THREADS];
+        x[r] = (t & j) == 0 ? min(o, x[r]) : max(o, x[r]);
+      }
+      turn ^= 1;
+    }
+#pragma unroll
+    for (int j = 16; j > 0; j >>= 1)
+      if (j < k) {
+#pragma unroll
+        for (int r = 0; r < E; ++r) {
+          const unsigned o = __shfl_xor_sync(0xffffffffu, x[r], j);
+          x[r] = (lane & j) == 0 ? min(o, x[r]) : max(o, x[r]);
+        }
+      }
+#pragma unroll
+    for (int r = 0; r < E; ++r)
+      if ((t + r * THREADS) & k) x[r] = ~x[r];
+  }
+}
+
+template <typename Tok, typename In, int VEC, bool ACC>
+__global__ void __launch_bounds__(ACC ? 1024 : 512, ACC ? 1 : 2)
+embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy, const EmbArgs a, int groups, float scale,
+                       float* grads, int* status, const EmbZero z) {
+  constexpr int kThreads = ACC ? 1024 : 512, kWarps = kThreads / 32, kVecs = 2 / VEC, kMost = kSmallMost / kThreads;
+  __shared__ unsigned buf[2][kSmallMost];
+  unsigned* entry = buf[0];  // row above position, sorted; kNoEntry: a token without a row
+  __shared__ __align__(8) float shead[kWarps][kSmallCols];
+  constexpr unsigned kNoEntry = 0xffffffffu, kPosMask = (1u << kSmallPosBits) - 1u;
+  if (!ACC && (int)blockIdx.x >= z.first_block) {
+    zero_piece_around<kSmallPiece>(z, a, buf[0], [&](int w, unsigned* taken, unsigned row0, unsigned row1) {
+      const Tok* tok = tokens + (long long)w * a.n;
+#pragma unroll 4
+      for (int j = threadIdx.x; j < a.n; j += blockDim.x) {
+        const long long t = (long long)tok[j];
+        if (t >= (long long)row0 && t <= (long long)row1) atomicOr(&taken[((unsigned)t >> 5) - (row0 >> 5)], 1u << (t & 31));
+      }
+    });
+    return;
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int w = blockIdx.x / groups, group = blockIdx.x % groups;
+  const Tok* tok = tokens + (long long)w * a.n;
+  int count2 = 2;
+  while (count2 < a.n) count2 *= 2;
+  int count = 0;  // tokens that have a row
+  unsigned x[kMost];
+#pragma unroll
+  for (int r = 0; r < kMost; ++r) {
+    const int j = r * kThreads + (int)threadIdx.x;
+    x[r] = kNoEntry;
+    if (j < a.n) {
+      const unsigned row = token_row((long long)tok[j], a.rows, status);
+      if (row != (unsigned)a.rows) x[r] = row << kSmallPosBits | (unsigned)j;
+    }
+    if (r == 0 || a.n > r * kThreads) count += __syncthreads_count(x[r] != kNoEntry);
+  }
+  if (count2 <= kThreads) {
+    unsigned one[1] = {x[0]};
+    sort_words<1, kThreads>(one, count2, buf);
+    x[0] = one[0];
+  } else {
+    sort_words<kMost, kThreads>(x, count2, buf);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < kMost; ++r) entry[r * kThreads + threadIdx.x] = x[r];
+  __syncthreads();
+  auto row_at = [&](int e) { return entry[e] >> kSmallPosBits; };
+  auto ends_at = [&](int e) { return e + 1 == count || row_at(e + 1) != row_at(e); };
+  const int share = (count + kWarps - 1) / kWarps, begin = min(share * warp, count), end = min(begin + share, count);
+  const bool left = begin > 0 && begin < end && row_at(begin - 1) == row_at(begin);
+
+  const int col = group * kSmallCols + lane * VEC;
+  bool on[kVecs], all_on[kVecs];
+#pragma unroll
+  for (int u = 0; u < kVecs; ++u) {
+    on[u] = col + 32 * VEC * u < a.cols;
+    all_on[u] = true;
+  }
+  const In* dw = dy + (long long)w * a.n * a.cols + col;
+  float* gw = grads + (long long)w * a.stride + a.offset + col;
+  float* head = shead[warp] + lane * VEC;
+  Lane<VEC, 2> sum = {};
+  bool first_run = left;  // the run that an earlier warp began
+  constexpr int kBatch = 8;
+#pragma unroll 1
+  for (int t0 = begin; t0 < end; t0 += 32) {  // 32 entries, one per lane
+    const int e = t0 + lane;
+    const unsigned mine = e < end ? entry[e] : 0u;
+    const unsigned ends = __ballot_sync(0xffffffffu, e < end && ends_at(e));
+#pragma unroll 1
+    for (int k0 = 0; k0 < 32 && t0 + k0 < end; k0 += kBatch) {
+      LaneRaw<In, VEC, 2> v[kBatch];
+      LaneRaw<float, VEC, 2> o[ACC ? kBatch : 1];
+      const int here = end - t0 - k0;  // entries of this batch, or more
+      const unsigned e8 = ends >> k0;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const unsigned x = __shfl_sync(0xffffffffu, mine, k0 + k);
+        if (k < here) load_lane(v[k], dw + (x & kPosMask) * (unsigned)a.cols, on);  // (both offsets fit 32 bits)
+        if (ACC && (e8 >> k & 1u)) load_lane(o[k], (const float*)gw + (x >> kSmallPosBits) * (unsigned)a.cols, on);
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (k >= here) break;
+        add_lane(sum, v[k]);
+        if (!(e8 >> k & 1u)) continue;
+        if (first_run) {
+          store_lane(head, sum, all_on);
+        } else {
+          scale_lane<ACC>(sum, scale, o[ACC ? k : 0]);
+          store_lane(gw + (__shfl_sync(0xffffffffu, mine, k0 + k) >> kSmallPosBits) * (unsigned)a.cols, sum, on);
+        }
+        sum = {};
+        first_run = false;
+      }
+    }
+  }
+  bool pending = begin < end && !ends_at(end - 1);  // a run goes on behind this warp
+  if (pending && first_run) {
+    store_lane(head, sum, all_on);
+    pending = false;
+  }
+  __syncthreads();
+  if (!pending) return;
+  float* g = gw + row_at(end - 1) * (unsigned)a.cols;
+  LaneRaw<float, VEC, 2> o;
+  if (ACC) load_lane(o, (const float*)g, on);
+  for (int q = warp + 1;; ++q) {
+    LaneRaw<float, VEC, 2> h;
+    load_lane(h, (const float*)shead[q] + lane * VEC, all_on);
+    add_lane(sum, h);
+    const int last = min(share * (q + 1), count) - 1;
+    if (row_at(last) != row_at(end - 1) || ends_at(last)) break;  // (the run ends inside that warp's share)
+  }
+  scale_lane<ACC>(sum, scale, o);
+  store_lane(g, sum, on);
+}
+
+// ---- more tokens: sort, sums by chunks, joins -------------------------------------------------------------------------
+// A stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.  Its launches clear pieces whole, as
+// many as fill their time.
+constexpr int kZeroPiece = 16384;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 
 __device__ __forceinline__ long long sort_hist_at(int w, int digit, int tile, int n_tiles) {
@@ -238,7 +397,7 @@ embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __res
                       unsigned* __restrict__ hist, int n_tiles, int* status, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
-    zero_piece(z, a);
+    zero_piece<kZeroPiece>(z, a);
     return;
   }
   __shared__ unsigned h[256];
@@ -266,7 +425,7 @@ embedding_hist_kernel(const unsigned* __restrict__ keys, EmbArgs a, int shift, u
                       EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
-    zero_piece(z, a);
+    zero_piece<kZeroPiece>(z, a);
     return;
   }
   await_previous();
@@ -290,7 +449,7 @@ __global__ void __launch_bounds__(1024)
 embedding_scan_kernel(unsigned* __restrict__ hist, int n_tiles, EmbArgs a, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
-    zero_piece(z, a);
+    zero_piece<kZeroPiece>(z, a);
     return;
   }
   await_previous();
@@ -332,7 +491,7 @@ embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __re
                          unsigned* __restrict__ pos_out, int last, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
-    zero_piece(z, a);
+    zero_piece<kZeroPiece>(z, a);
     return;
   }
   await_previous();
@@ -423,51 +582,22 @@ struct EmbLevel {
   unsigned* slot_keys;    // [W][chunks][2]: their rows; kNoKey: nothing there
 };
 
-// Four columns of a lane: 4 / VEC vectors, 32 VEC columns apart.
-template <int VEC> struct Lane4 { Vals<VEC> c[4 / VEC]; };
-template <typename T, int VEC> struct LaneRaw { typename Raw<T, VEC>::type c[4 / VEC]; };
-template <int VEC, typename T>
-__device__ __forceinline__ void load_lane(LaneRaw<T, VEC>& v, const T* p, const bool* on) {
-#pragma unroll
-  for (int u = 0; u < 4 / VEC; ++u)
-    if (on[u]) v.c[u] = load_raw<VEC>(p + 32 * VEC * u);
-}
-template <int VEC> __device__ __forceinline__ void store_lane(float* p, const Lane4<VEC>& v, const bool* on) {
-#pragma unroll
-  for (int u = 0; u < 4 / VEC; ++u)
-    if (on[u]) store_vals<VEC>(p + 32 * VEC * u, v.c[u]);
-}
-template <int VEC, typename T>
-__device__ __forceinline__ void add_lane(Lane4<VEC>& s, const LaneRaw<T, VEC>& v, bool fresh) {
-#pragma unroll
-  for (int u = 0; u < 4 / VEC; ++u) {
-    const Vals<VEC> x = unpack(v.c[u]);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) s.c[u].v[j] = fresh ? x.v[j] : s.c[u].v[j] + x.v[j];
-  }
-}
-template <int VEC, bool ACC>
-__device__ __forceinline__ void scale_lane(Lane4<VEC>& s, float scale, const LaneRaw<float, VEC>& o) {
-#pragma unroll
-  for (int u = 0; u < 4 / VEC; ++u) {
-    const Vals<VEC> x = unpack(o.c[u]);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) s.c[u].v[j] = ACC ? fmaf(scale, s.c[u].v[j], x.v[j]) : scale * s.c[u].v[j];
-  }
-}
-
 // In: the values' type at the first level (FIRST); float above.
 template <typename In, int VEC, bool FIRST, bool ACC>
 __global__ void __launch_bounds__(256, ACC ? (sizeof(In) == 2 ? 3 : 2) : (sizeof(In) == 2 ? 4 : 3))
 embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs a, int groups, float scale, float* grads,
-                     const unsigned* __restrict__ sorted, const EmbZero z) {
+                     const EmbZero z) {
   constexpr int kPart = FIRST ? kChunk / 8 : 2 * kFan / 8;  // entries per warp
   __shared__ unsigned skey[8 * kPart + 2], smask[8], sends[8];
   __shared__ __align__(16) float shead[8][128];  // read and written four columns at a time
   let_next_start();
   await_previous();
   if (!ACC && (int)blockIdx.x >= z.first_block) {
-    zero_piece_around(z, a, sorted);
+    __shared__ unsigned taken[kZeroPiece / 32 + 3];
+    zero_piece_around<kZeroPiece>(z, a, taken, [&](int w, unsigned* t, unsigned row0, unsigned row1) {
+      const unsigned* bits = z.rows_taken + (long long)w * ((a.rows + 31) / 32);
+      for (unsigned i = (row0 >> 5) + threadIdx.x; i <= row1 >> 5; i += blockDim.x) t[i - (row0 >> 5)] = bits[i];
+    });
     return;
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -532,15 +662,15 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   float* gw = grads + (long long)w * a.stride + a.offset + col;
   float* tail_slot = l.slots + ((long long)wc * 2 + 1) * a.cols + col;
   float* head = shead[warp] + lane * VEC;
-  Lane4<VEC> sum;
-  bool fresh = true, first_run = true;
+  Lane<VEC, 4> sum = {};
+  bool first_run = left;  // the run that an earlier warp, or the chunk before, began
   // 32 registers of loads in flight: 16 entries of bf16 at once, of fp32 (and of rows that are added to) eight
   constexpr int kBatch = sizeof(In) == 2 && !ACC ? 16 : 8;
   unsigned todo = mask;
 #pragma unroll 1
   while (todo != 0u) {
-    LaneRaw<In, VEC> v[kBatch];
-    LaneRaw<float, VEC> o[ACC ? kBatch : 1];
+    LaneRaw<In, VEC, 4> v[kBatch];
+    LaneRaw<float, VEC, 4> o[ACC ? kBatch : 1];
     unsigned batch = todo;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
@@ -548,31 +678,31 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
       const int e = __ffs(todo) - 1;
       todo &= todo - 1u;
       const unsigned from = FIRST ? __shfl_sync(0xffffffffu, pos, e) : (unsigned)(c0 + kPart * warp + e);
-      load_lane<VEC>(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
-      if (ACC && (ends >> e & 1u)) load_lane<VEC>(o[k], (const float*)gw + (unsigned long long)own[e] * (unsigned)a.cols, on);
+      load_lane(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
+      if (ACC && (ends >> e & 1u)) load_lane(o[k], (const float*)gw + own[e] * (unsigned)a.cols, on);
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       if (batch == 0u) break;
       const int e = __ffs(batch) - 1;
       batch &= batch - 1u;
-      add_lane<VEC>(sum, v[k], fresh);
-      fresh = ends >> e & 1u;
-      if (!fresh) continue;
-      if (first_run && left) {
-        store_lane<VEC>(head, sum, all_on);
+      add_lane(sum, v[k]);
+      if (!(ends >> e & 1u)) continue;
+      if (first_run) {
+        store_lane(head, sum, all_on);
       } else if (open_right && warp == last_warp && e == last_entry) {
-        store_lane<VEC>(tail_slot, sum, on);
+        store_lane(tail_slot, sum, on);
       } else {
-        scale_lane<VEC, ACC>(sum, scale, o[ACC ? k : 0]);
-        store_lane<VEC>(gw + (unsigned long long)own[e] * (unsigned)a.cols, sum, on);
+        scale_lane<ACC>(sum, scale, o[ACC ? k : 0]);
+        store_lane(gw + own[e] * (unsigned)a.cols, sum, on);
       }
+      sum = {};
       first_run = false;
     }
   }
-  bool pending = !fresh;  // a run goes on behind this warp
-  if (pending && first_run && left) {
-    store_lane<VEC>(head, sum, all_on);
+  bool pending = mask != 0u && !(ends >> (31 - __clz(mask)) & 1u);  // a run goes on behind this warp
+  if (pending && first_run) {
+    store_lane(head, sum, all_on);
     pending = false;
   }
   __syncthreads();
@@ -580,30 +710,31 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   auto finish_run = [&](int q) {
     for (;; ++q) {
       if (smask[q] == 0u) continue;
-      LaneRaw<float, VEC> h;
-      load_lane<VEC>(h, (const float*)shead[q] + lane * VEC, all_on);
-      add_lane<VEC>(sum, h, false);
+      LaneRaw<float, VEC, 4> h;
+      load_lane(h, (const float*)shead[q] + lane * VEC, all_on);
+      add_lane(sum, h);
       if (sends[q] != 0u) return q == last_warp && __ffs(sends[q]) - 1 == last_entry;
     }
   };
   if (pending) {
     const unsigned row = own[31 - __clz(mask)];
-    float* g = gw + (unsigned long long)row * (unsigned)a.cols;
-    LaneRaw<float, VEC> o;
-    if (ACC) load_lane<VEC>(o, (const float*)g, on);
+    float* g = gw + row * (unsigned)a.cols;
+    LaneRaw<float, VEC, 4> o;
+    if (ACC) load_lane(o, (const float*)g, on);
     if (finish_run(warp + 1) && open_right) {
-      store_lane<VEC>(tail_slot, sum, on);
+      store_lane(tail_slot, sum, on);
     } else {
-      scale_lane<VEC, ACC>(sum, scale, o);
-      store_lane<VEC>(g, sum, on);
+      scale_lane<ACC>(sum, scale, o);
+      store_lane(g, sum, on);
     }
   }
   if (warp == 0 && open_left) {
-    LaneRaw<float, VEC> h;
-    load_lane<VEC>(h, (const float*)shead[0] + lane * VEC, all_on);
-    add_lane<VEC>(sum, h, true);
+    LaneRaw<float, VEC, 4> h;
+    load_lane(h, (const float*)shead[0] + lane * VEC, all_on);
+    sum = {};
+    add_lane(sum, h);
     if (sends[0] == 0u) finish_run(1);
-    store_lane<VEC>(tail_slot - a.cols, sum, on);
+    store_lane(tail_slot - a.cols, sum, on);
   }
 }
 
@@ -611,29 +742,34 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
 
 static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Workspace of the gradient: two (row, position) lists, the radix sort's histograms, the levels' slots.
+// Workspace of the gradient: two (row, position) lists, the radix sort's histograms, the levels' slots.  The one
+// launch for few tokens needs none.
 struct EmbPlan {
   size_t keys[2], pos[2], hist, slots[2], slot_keys[2], rows_taken, total;
   int n_tiles;
 };
+static bool small_way(int rows, int cols, long long n) {
+  return n <= kSmallMost && rows <= kSmallRows && cols <= kSmallWide;
+}
 static EmbPlan emb_plan(int W, int rows, int cols, long long n) {
   EmbPlan p{};
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = align256(o + bytes); return at; };
-  const bool radix = n > kRankMost;
-  for (int k = 0; k < 2; ++k) {
-    p.keys[k] = take(k == 0 || radix ? sizeof(unsigned) * (size_t)W * n : 0);
-    p.pos[k] = take(k == 0 || radix ? sizeof(unsigned) * (size_t)W * n : 0);
-  }
   p.n_tiles = (int)((n + kSortTile - 1) / kSortTile);
-  p.hist = take(radix ? sizeof(unsigned) * (size_t)W * 256 * p.n_tiles : 0);
-  // slots of the first level, and of the second (the third uses the first's again, and so on)
-  const long long c1 = (n + kChunk - 1) / kChunk, c2 = (c1 + kFan - 1) / kFan;
-  p.slots[0] = take(c1 > 1 ? sizeof(float) * (size_t)W * c1 * 2 * cols : 0);
-  p.slots[1] = take(c2 > 1 ? sizeof(float) * (size_t)W * c2 * 2 * cols : 0);
-  p.slot_keys[0] = take(c1 > 1 ? sizeof(unsigned) * (size_t)W * c1 * 2 : 0);
-  p.slot_keys[1] = take(c2 > 1 ? sizeof(unsigned) * (size_t)W * c2 * 2 : 0);
-  p.rows_taken = take(radix ? sizeof(unsigned) * (size_t)W * ((rows + 31) / 32) : 0);
+  if (!small_way(rows, cols, n)) {
+    for (int k = 0; k < 2; ++k) {
+      p.keys[k] = take(sizeof(unsigned) * (size_t)W * n);
+      p.pos[k] = take(sizeof(unsigned) * (size_t)W * n);
+    }
+    p.hist = take(sizeof(unsigned) * (size_t)W * 256 * p.n_tiles);
+    p.rows_taken = take(sizeof(unsigned) * (size_t)W * ((rows + 31) / 32));
+    // slots of the first level, and of the second (the third uses the first's again, and so on)
+    const long long c1 = (n + kChunk - 1) / kChunk, c2 = (c1 + kFan - 1) / kFan;
+    p.slots[0] = take(sizeof(float) * (size_t)W * c1 * 2 * cols);
+    p.slots[1] = take(c2 > 1 ? sizeof(float) * (size_t)W * c2 * 2 * cols : 0);
+    p.slot_keys[0] = take(sizeof(unsigned) * (size_t)W * c1 * 2);
+    p.slot_keys[1] = take(c2 > 1 ? sizeof(unsigned) * (size_t)W * c2 * 2 : 0);
+  }
   p.total = o < 256 ? 256 : o;
   return p;
 }
@@ -671,8 +807,8 @@ cudaError_t launch_embedding_lookup(acc_ctx* ctx, int layer, const float* params
 // The kernels of one gradient call, in order: `first` for the one that starts behind everything before the call, the others
 // may start early.  Each takes up to `share` of the pieces that are still to clear.
 constexpr int kAll = 0x7fffffff;
-// Pieces (64 KB) that take about as long as a launch of the sort, the sums of a few hundred tokens, a level of joining.
-constexpr int kSortShare = 384, kSumShare = 640, kJoinShare = 192;
+// Pieces (64 KB) that take about as long as a launch of the sort, a level of joining.
+constexpr int kSortShare = 384, kJoinShare = 192;
 struct EmbLaunch {
   acc_ctx* ctx;
   cudaStream_t s;
@@ -719,7 +855,7 @@ static void sum_levels(EmbLaunch& go, const EmbArgs& a, const EmbPlan& p, char* 
   go.pieces = all - kept;
   EmbLevel l = level(0, keys, pos, a.n, chunks);
   go(PH_EMB_SUM, accumulate ? embedding_sum_kernel<In, VEC, true, true> : embedding_sum_kernel<In, VEC, true, false>,
-     (long long)W * chunks * groups, 256, kAll, static_cast<const In*>(dy), l, a, groups, scale, grads, keys);
+     (long long)W * chunks * groups, 256, kAll, static_cast<const In*>(dy), l, a, groups, scale, grads);
   go.pieces = all;
   for (int k = 1; chunks > 1; ++k) {
     const float* in = l.slots;
@@ -728,7 +864,7 @@ static void sum_levels(EmbLaunch& go, const EmbArgs& a, const EmbPlan& p, char* 
     chunks = (chunks + kFan - 1) / kFan;
     l = level(k, in_keys, nullptr, count, chunks);
     go(PH_EMB_JOIN, accumulate ? embedding_sum_kernel<float, VEC, false, true> : embedding_sum_kernel<float, VEC, false, false>,
-       (long long)W * chunks * groups, 256, chunks == 1 ? kAll : kJoinShare, in, l, a, groups, scale, grads, keys);
+       (long long)W * chunks * groups, 256, chunks == 1 ? kAll : kJoinShare, in, l, a, groups, scale, grads);
   }
 }
 
@@ -740,34 +876,40 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
   const int W = ctx->cfg.n_workers;
   const EmbArgs a{L.offset, ctx->cfg.worker_stride, (long long)L.rows * L.cols, L.rows, L.cols, (int)n};
   char* ws = static_cast<char*>(workspace);
-  const int pieces = (int)((a.size + kZeroPiece - 1) / kZeroPiece);
+  const bool small = small_way(L.rows, L.cols, n);
+  const int piece = small ? kSmallPiece : kZeroPiece, pieces = (int)((a.size + piece - 1) / piece);
   const EmbPlan p = emb_plan(W, L.rows, L.cols, n);
-  unsigned* rows_taken = n > kRankMost && !accumulate ? reinterpret_cast<unsigned*>(ws + p.rows_taken) : nullptr;
+  unsigned* rows_taken = small || accumulate ? nullptr : reinterpret_cast<unsigned*>(ws + p.rows_taken);
   EmbLaunch go{ctx, s, EmbZero{grads, 0, 0, pieces, rows_taken}, accumulate ? 0 : pieces * W};
-  unsigned* keys[2] = {reinterpret_cast<unsigned*>(ws + p.keys[0]), reinterpret_cast<unsigned*>(ws + p.keys[1])};
-  unsigned* pos[2] = {reinterpret_cast<unsigned*>(ws + p.pos[0]), reinterpret_cast<unsigned*>(ws + p.pos[1])};
-  // Clearing a piece whole costs the rows with tokens a second write, clearing around them some 5 % of the piece's time:
-  // with fewer tokens than a sixteenth of the rows all but what fills the sums' time goes with the sort.
-  const int ahead = n == 0 ? kAll : n * 16 < a.rows ? std::max(0, go.pieces - kSumShare - kJoinShare) : kSortShare;
-  int at = 0;
   const auto* tok8 = static_cast<const long long*>(tokens);
   const auto* tok4 = static_cast<const int*>(tokens);
-  if (n <= kRankMost) {
-    const int per_worker = (int)((n + kRankBlock - 1) / kRankBlock);
-    if (tok64)
-      go(PH_EMB_RANK, embedding_rank_kernel<long long>, (long long)per_worker * W, kRankThreads, ahead, tok8, a, keys[0],
-         pos[0], per_worker, ctx->d_status);
-    else
-      go(PH_EMB_RANK, embedding_rank_kernel<int>, (long long)per_worker * W, kRankThreads, ahead, tok4, a, keys[0], pos[0],
-         per_worker, ctx->d_status);
+  if (small) {
+    const int groups = (L.cols + kSmallCols - 1) / kSmallCols;
+    auto run = [&](auto tok, auto in, auto vec) {
+      using Tok = decltype(tok);
+      using In = decltype(in);
+      constexpr int VEC = decltype(vec)::value;
+      go(PH_EMB_SMALL, accumulate ? embedding_small_kernel<Tok, In, VEC, true> : embedding_small_kernel<Tok, In, VEC, false>,
+         n == 0 ? 0ll : (long long)W * groups, accumulate ? 1024 : 512, kAll, static_cast<const Tok*>(tokens),
+         static_cast<const In*>(dy), a, groups, scale, grads, ctx->d_status);
+    };
+    auto typed = [&](auto tok, auto in) {
+      if (L.vec == 1) run(tok, in, std::integral_constant<int, 1>());
+      else run(tok, in, std::integral_constant<int, 2>());
+    };
+    if (tok64) bf16 ? typed((long long)0, __nv_bfloat16()) : typed((long long)0, 0.f);
+    else bf16 ? typed(0, __nv_bfloat16()) : typed(0, 0.f);
   } else {
+    unsigned* keys[2] = {reinterpret_cast<unsigned*>(ws + p.keys[0]), reinterpret_cast<unsigned*>(ws + p.keys[1])};
+    unsigned* pos[2] = {reinterpret_cast<unsigned*>(ws + p.pos[0]), reinterpret_cast<unsigned*>(ws + p.pos[1])};
+    int at = 0;
     unsigned* hist = reinterpret_cast<unsigned*>(ws + p.hist);
     const long long blocks = (long long)p.n_tiles * W;
     if (tok64)
-      go(PH_EMB_KEYS, embedding_keys_kernel<long long>, blocks, kSortThreads, ahead, tok8, a, keys[0], pos[0], hist,
+      go(PH_EMB_KEYS, embedding_keys_kernel<long long>, blocks, kSortThreads, kSortShare, tok8, a, keys[0], pos[0], hist,
          p.n_tiles, ctx->d_status);
     else
-      go(PH_EMB_KEYS, embedding_keys_kernel<int>, blocks, kSortThreads, ahead, tok4, a, keys[0], pos[0], hist, p.n_tiles,
+      go(PH_EMB_KEYS, embedding_keys_kernel<int>, blocks, kSortThreads, kSortShare, tok4, a, keys[0], pos[0], hist, p.n_tiles,
          ctx->d_status);
     for (int shift = 0; shift < 32 && (shift == 0 || (a.rows >> shift) != 0); shift += 8) {
       if (shift > 0) go(PH_EMB_HIST, embedding_hist_kernel, blocks, kSortThreads, kSortShare, keys[at], a, shift, hist, p.n_tiles);
@@ -777,8 +919,6 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
          p.n_tiles, keys[at ^ 1], pos[at ^ 1], (int)(shift >= 24 || (a.rows >> (shift + 8)) == 0));
       at ^= 1;
     }
-  }
-  if (n > 0) {
     auto sums = [&](auto in) {
       using In = decltype(in);
       if (L.vec == 4) sum_levels<In, 4>(go, a, p, ws, keys[at], pos[at], dy, scale, accumulate, grads);

@@ -73,7 +73,7 @@ enum Phase {
   PH_PSGD_PFOLD, PH_VEC_EXCHANGE, PH_PSGD_QMERGE, PH_TOPK_DECOMPRESS_PACKED, PH_TOPK_FLUSH,
   PH_MOMENTS_PARTIAL, PH_MOMENTS_FINAL,
   PH_ADAMW_COEF, PH_ADAMW, PH_ADAMW_8BIT, PH_CLIP_FACTOR,
-  PH_EMB_LOOKUP, PH_EMB_RANK, PH_EMB_KEYS, PH_EMB_HIST, PH_EMB_SCAN, PH_EMB_SCATTER, PH_EMB_SUM, PH_EMB_JOIN,
+  PH_EMB_LOOKUP, PH_EMB_SMALL, PH_EMB_KEYS, PH_EMB_HIST, PH_EMB_SCAN, PH_EMB_SCATTER, PH_EMB_SUM, PH_EMB_JOIN,
   PH_COUNT
 };
 
