@@ -114,7 +114,6 @@ struct EmbZero {
   int first_block;       // blocks behind this one clear pieces
   int from;              // number of the first such block's piece
   int pieces_per_worker;
-  unsigned* rows_taken;  // radix sort: [W][(rows + 31) / 32], a bit for each row that some token names
 };
 
 // A piece whole; a row that the sums write later is then written twice.
@@ -381,8 +380,9 @@ embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy
 }
 
 // ---- more tokens: sort, sums by chunks, joins -------------------------------------------------------------------------
-// A stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.  Its launches clear pieces whole, as
-// many as fill their time.
+// A stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.  Its launches clear
+// the pieces, whole: leaving out the rows that the sums write (a third of them for 16384 tokens of 33278 rows) and clearing
+// beside the sums instead was slower, 211 us against 185 us for 8 workers, as the sort's launches then waited alone.
 constexpr int kZeroPiece = 16384;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 
@@ -406,10 +406,6 @@ embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __res
   const int w = blockIdx.x / n_tiles, tile = blockIdx.x % n_tiles;
   const long long w0 = (long long)w * a.n;
   const int end = min((tile + 1) * kSortTile, a.n);
-  const int row_words = (a.rows + 31) / 32;
-  if (z.rows_taken != nullptr)
-    for (int i = tile * kSortThreads + (int)threadIdx.x; i < row_words; i += n_tiles * kSortThreads)
-      z.rows_taken[(long long)w * row_words + i] = 0u;
   for (int i = tile * kSortTile + (int)threadIdx.x; i < end; i += kSortThreads) {
     const unsigned key = token_row((long long)tokens[w0 + i], a.rows, status);
     keys[w0 + i] = key;
@@ -488,7 +484,7 @@ template <bool SCANNED>
 __global__ void __launch_bounds__(kSortThreads)
 embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ pos, EmbArgs a, int shift,
                          const unsigned* __restrict__ hist, int n_tiles, unsigned* __restrict__ keys_out,
-                         unsigned* __restrict__ pos_out, int last, EmbZero z) {
+                         unsigned* __restrict__ pos_out, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
     zero_piece<kZeroPiece>(z, a);
@@ -559,11 +555,6 @@ embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __re
     const long long to = w0 + cnt[warp][(key[k] >> shift) & 255u] + rank[k];
     keys_out[to] = key[k];
     pos_out[to] = pos[w0 + i0 + 32 * k];
-    if (last && z.rows_taken != nullptr && key[k] != (unsigned)a.rows) {
-      unsigned* word = z.rows_taken + (long long)w * ((a.rows + 31) / 32) + (key[k] >> 5);
-      const unsigned bit = 1u << (key[k] & 31);
-      if (!(__ldcg(word) & bit)) atomicOr(word, bit);  // (frequent rows find theirs set)
-    }
   }
 }
 
@@ -585,21 +576,12 @@ struct EmbLevel {
 // In: the values' type at the first level (FIRST); float above.
 template <typename In, int VEC, bool FIRST, bool ACC>
 __global__ void __launch_bounds__(256, ACC ? (sizeof(In) == 2 ? 3 : 2) : (sizeof(In) == 2 ? 4 : 3))
-embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs a, int groups, float scale, float* grads,
-                     const EmbZero z) {
+embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs a, int groups, float scale, float* grads) {
   constexpr int kPart = FIRST ? kChunk / 8 : 2 * kFan / 8;  // entries per warp
   __shared__ unsigned skey[8 * kPart + 2], smask[8], sends[8];
   __shared__ __align__(16) float shead[8][128];  // read and written four columns at a time
   let_next_start();
   await_previous();
-  if (!ACC && (int)blockIdx.x >= z.first_block) {
-    __shared__ unsigned taken[kZeroPiece / 32 + 3];
-    zero_piece_around<kZeroPiece>(z, a, taken, [&](int w, unsigned* t, unsigned row0, unsigned row1) {
-      const unsigned* bits = z.rows_taken + (long long)w * ((a.rows + 31) / 32);
-      for (unsigned i = (row0 >> 5) + threadIdx.x; i <= row1 >> 5; i += blockDim.x) t[i - (row0 >> 5)] = bits[i];
-    });
-    return;
-  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int wc = blockIdx.x / groups, group = blockIdx.x % groups;  // column group fastest, then chunk, then worker
   const int w = wc / l.chunks, chunk = wc % l.chunks;
@@ -745,7 +727,7 @@ static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // Workspace of the gradient: two (row, position) lists, the radix sort's histograms, the levels' slots.  The one
 // launch for few tokens needs none.
 struct EmbPlan {
-  size_t keys[2], pos[2], hist, slots[2], slot_keys[2], rows_taken, total;
+  size_t keys[2], pos[2], hist, slots[2], slot_keys[2], total;
   int n_tiles;
 };
 static bool small_way(int rows, int cols, long long n) {
@@ -762,7 +744,6 @@ static EmbPlan emb_plan(int W, int rows, int cols, long long n) {
       p.pos[k] = take(sizeof(unsigned) * (size_t)W * n);
     }
     p.hist = take(sizeof(unsigned) * (size_t)W * 256 * p.n_tiles);
-    p.rows_taken = take(sizeof(unsigned) * (size_t)W * ((rows + 31) / 32));
     // slots of the first level, and of the second (the third uses the first's again, and so on)
     const long long c1 = (n + kChunk - 1) / kChunk, c2 = (c1 + kFan - 1) / kFan;
     p.slots[0] = take(sizeof(float) * (size_t)W * c1 * 2 * cols);
@@ -804,38 +785,28 @@ cudaError_t launch_embedding_lookup(acc_ctx* ctx, int layer, const float* params
   return cudaGetLastError();
 }
 
-// The kernels of one gradient call, in order: `first` for the one that starts behind everything before the call, the others
-// may start early.  Each takes up to `share` of the pieces that are still to clear.
-constexpr int kAll = 0x7fffffff;
-// Pieces (64 KB) that take about as long as a launch of the sort, a level of joining.
-constexpr int kSortShare = 384, kJoinShare = 192;
+// The kernels of one gradient call, in order: the first starts behind everything before the call, the others may start early.
 struct EmbLaunch {
   acc_ctx* ctx;
   cudaStream_t s;
-  EmbZero z;
-  int pieces;
   bool first = true;
   cudaError_t err = cudaSuccess;
 
   template <typename... Params, typename... Args>
-  void operator()(int phase, void (*kernel)(Params...), long long blocks, int threads, int share, Args... args) {
-    const int mine = pieces - z.from < share ? pieces - z.from : share;
-    z.first_block = (int)blocks;
-    if (blocks + mine > 0 && err == cudaSuccess) {
-      PhaseTimer pt(ctx, phase, s);
-      cudaLaunchAttribute attr{};
-      attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      attr.val.programmaticStreamSerializationAllowed = 1;
-      cudaLaunchConfig_t cfg{};
-      cfg.gridDim = dim3((unsigned)(blocks + mine));
-      cfg.blockDim = dim3((unsigned)threads);
-      cfg.stream = s;
-      cfg.attrs = &attr;
-      cfg.numAttrs = first ? 0 : 1;
-      first = false;
-      err = cudaLaunchKernelEx(&cfg, kernel, args..., z);
-    }
-    z.from += mine;
+  void operator()(int phase, void (*kernel)(Params...), long long blocks, int threads, Args... args) {
+    if (blocks == 0 || err != cudaSuccess) return;
+    PhaseTimer pt(ctx, phase, s);
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = s;
+    cfg.attrs = &attr;
+    cfg.numAttrs = first ? 0 : 1;
+    first = false;
+    err = cudaLaunchKernelEx(&cfg, kernel, args...);
   }
 };
 
@@ -848,15 +819,10 @@ static void sum_levels(EmbLaunch& go, const EmbArgs& a, const EmbPlan& p, char* 
     return EmbLevel{lkeys, lpos, count, chunks, reinterpret_cast<float*>(ws + p.slots[k & 1]),
                     reinterpret_cast<unsigned*>(ws + p.slot_keys[k & 1])};
   };
-  int chunks = (a.n + kChunk - 1) / kChunk, joins = 0;
-  for (int c = chunks; c > 1; c = (c + kFan - 1) / kFan) ++joins;
-  // what is still to clear is cleared beside the sums, but for a share that each of the short joining levels keeps
-  const int all = go.pieces, left = all - go.z.from, kept = std::min(left, joins * kJoinShare);
-  go.pieces = all - kept;
+  int chunks = (a.n + kChunk - 1) / kChunk;
   EmbLevel l = level(0, keys, pos, a.n, chunks);
   go(PH_EMB_SUM, accumulate ? embedding_sum_kernel<In, VEC, true, true> : embedding_sum_kernel<In, VEC, true, false>,
-     (long long)W * chunks * groups, 256, kAll, static_cast<const In*>(dy), l, a, groups, scale, grads);
-  go.pieces = all;
+     (long long)W * chunks * groups, 256, static_cast<const In*>(dy), l, a, groups, scale, grads);
   for (int k = 1; chunks > 1; ++k) {
     const float* in = l.slots;
     const unsigned* in_keys = l.slot_keys;
@@ -864,7 +830,7 @@ static void sum_levels(EmbLaunch& go, const EmbArgs& a, const EmbPlan& p, char* 
     chunks = (chunks + kFan - 1) / kFan;
     l = level(k, in_keys, nullptr, count, chunks);
     go(PH_EMB_JOIN, accumulate ? embedding_sum_kernel<float, VEC, false, true> : embedding_sum_kernel<float, VEC, false, false>,
-       (long long)W * chunks * groups, 256, chunks == 1 ? kAll : kJoinShare, in, l, a, groups, scale, grads);
+       (long long)W * chunks * groups, 256, in, l, a, groups, scale, grads);
   }
 }
 
@@ -878,20 +844,18 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
   char* ws = static_cast<char*>(workspace);
   const bool small = small_way(L.rows, L.cols, n);
   const int piece = small ? kSmallPiece : kZeroPiece, pieces = (int)((a.size + piece - 1) / piece);
-  const EmbPlan p = emb_plan(W, L.rows, L.cols, n);
-  unsigned* rows_taken = small || accumulate ? nullptr : reinterpret_cast<unsigned*>(ws + p.rows_taken);
-  EmbLaunch go{ctx, s, EmbZero{grads, 0, 0, pieces, rows_taken}, accumulate ? 0 : pieces * W};
-  const auto* tok8 = static_cast<const long long*>(tokens);
-  const auto* tok4 = static_cast<const int*>(tokens);
+  const long long all = accumulate ? 0 : (long long)pieces * W;  // pieces to clear
+  EmbLaunch go{ctx, s};
   if (small) {
     const int groups = (L.cols + kSmallCols - 1) / kSmallCols;
+    const long long blocks = n == 0 ? 0 : (long long)W * groups;
     auto run = [&](auto tok, auto in, auto vec) {
       using Tok = decltype(tok);
       using In = decltype(in);
       constexpr int VEC = decltype(vec)::value;
       go(PH_EMB_SMALL, accumulate ? embedding_small_kernel<Tok, In, VEC, true> : embedding_small_kernel<Tok, In, VEC, false>,
-         n == 0 ? 0ll : (long long)W * groups, accumulate ? 1024 : 512, kAll, static_cast<const Tok*>(tokens),
-         static_cast<const In*>(dy), a, groups, scale, grads, ctx->d_status);
+         blocks + all, accumulate ? 1024 : 512, static_cast<const Tok*>(tokens), static_cast<const In*>(dy), a, groups,
+         scale, grads, ctx->d_status, EmbZero{grads, (int)blocks, 0, pieces});
     };
     auto typed = [&](auto tok, auto in) {
       if (L.vec == 1) run(tok, in, std::integral_constant<int, 1>());
@@ -900,24 +864,35 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
     if (tok64) bf16 ? typed((long long)0, __nv_bfloat16()) : typed((long long)0, 0.f);
     else bf16 ? typed(0, __nv_bfloat16()) : typed(0, 0.f);
   } else {
+    const EmbPlan p = emb_plan(W, L.rows, L.cols, n);
     unsigned* keys[2] = {reinterpret_cast<unsigned*>(ws + p.keys[0]), reinterpret_cast<unsigned*>(ws + p.keys[1])};
     unsigned* pos[2] = {reinterpret_cast<unsigned*>(ws + p.pos[0]), reinterpret_cast<unsigned*>(ws + p.pos[1])};
-    int at = 0;
     unsigned* hist = reinterpret_cast<unsigned*>(ws + p.hist);
     const long long blocks = (long long)p.n_tiles * W;
+    const bool scan = p.n_tiles > kScanTiles;
+    int passes = 0;
+    for (int shift = 0; shift < 32 && (shift == 0 || (a.rows >> shift) != 0); shift += 8) ++passes;
+    // every launch of the sort clears its share of the pieces behind its own blocks
+    const long long share = (all + passes * (scan ? 3 : 2) - 1) / (passes * (scan ? 3 : 2));
+    long long from = 0;
+    auto sort = [&](int phase, auto kernel, long long own, int threads, auto... args) {
+      const long long mine = std::min(share, all - from);
+      go(phase, kernel, own + mine, threads, args..., EmbZero{grads, (int)own, (int)from, pieces});
+      from += mine;
+    };
     if (tok64)
-      go(PH_EMB_KEYS, embedding_keys_kernel<long long>, blocks, kSortThreads, kSortShare, tok8, a, keys[0], pos[0], hist,
-         p.n_tiles, ctx->d_status);
+      sort(PH_EMB_KEYS, embedding_keys_kernel<long long>, blocks, kSortThreads, static_cast<const long long*>(tokens), a,
+           keys[0], pos[0], hist, p.n_tiles, ctx->d_status);
     else
-      go(PH_EMB_KEYS, embedding_keys_kernel<int>, blocks, kSortThreads, kSortShare, tok4, a, keys[0], pos[0], hist, p.n_tiles,
-         ctx->d_status);
-    for (int shift = 0; shift < 32 && (shift == 0 || (a.rows >> shift) != 0); shift += 8) {
-      if (shift > 0) go(PH_EMB_HIST, embedding_hist_kernel, blocks, kSortThreads, kSortShare, keys[at], a, shift, hist, p.n_tiles);
-      const bool scan = p.n_tiles > kScanTiles;
-      if (scan) go(PH_EMB_SCAN, embedding_scan_kernel, W, 1024, kSortShare, hist, p.n_tiles, a);
-      go(PH_EMB_SCATTER, scan ? embedding_scatter_kernel<true> : embedding_scatter_kernel<false>, blocks, kSortThreads, kSortShare, keys[at], pos[at], a, shift, hist,
-         p.n_tiles, keys[at ^ 1], pos[at ^ 1], (int)(shift >= 24 || (a.rows >> (shift + 8)) == 0));
-      at ^= 1;
+      sort(PH_EMB_KEYS, embedding_keys_kernel<int>, blocks, kSortThreads, static_cast<const int*>(tokens), a, keys[0], pos[0],
+           hist, p.n_tiles, ctx->d_status);
+    int at = 0;
+    for (int pass = 0; pass < passes; ++pass, at ^= 1) {
+      const int shift = 8 * pass;
+      if (pass > 0) sort(PH_EMB_HIST, embedding_hist_kernel, blocks, kSortThreads, keys[at], a, shift, hist, p.n_tiles);
+      if (scan) sort(PH_EMB_SCAN, embedding_scan_kernel, W, 1024, hist, p.n_tiles, a);
+      sort(PH_EMB_SCATTER, scan ? embedding_scatter_kernel<true> : embedding_scatter_kernel<false>, blocks, kSortThreads,
+           keys[at], pos[at], a, shift, hist, p.n_tiles, keys[at ^ 1], pos[at ^ 1]);
     }
     auto sums = [&](auto in) {
       using In = decltype(in);
