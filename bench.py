@@ -265,6 +265,12 @@ def main():
                     help="two-compressor configs: run the TopK step after the PowerSGD step instead of beside it")
     ap.add_argument("--sgd-tail", action="store_true",
                     help="single-compressor configs: apply the Nesterov update inside the step (fused optimiser tail)")
+    ap.add_argument("--adamw", type=int, default=0, choices=[32, 8],
+                    help="AdamW step on the averaged gradient, clipped by its global norm, with states of that many bits "
+                         "(single-compressor configs)")
+    ap.add_argument("--tokens", type=int, default=0,
+                    help="config 5: the encoder's gradient is made in the step from that many tokens per worker "
+                         "(embedding gradient of a Zipf-distributed batch), in place of the stream's")
     ap.add_argument("--batch-mode", action="store_true",
                     help="batch-size mode instead of compression: a step is n_accum micro-batch accumulations, the "
                          "uncompressed average with the fused Nesterov update, and (every check_every steps) the "
@@ -321,10 +327,18 @@ def main():
     if args.sgd_tail:
         assert n_comp == 1, "--sgd-tail needs a single-compressor config (2, 3 or 4)"
         optimizer = {"params": torch.zeros(table.stride, device=dev), "lr": 0.1, "momentum": 0.9}
+    if args.adamw:
+        assert n_comp == 1 and not args.sgd_tail, "--adamw needs a single-compressor config (2, 3 or 4) without --sgd-tail"
+        optimizer = {"kind": "adamw", "params": torch.zeros(table.stride, device=dev), "lr": 1e-3, "bits": args.adamw,
+                     "max_norm": 1.0}
+    embedding = None
+    if args.tokens:
+        assert args.config == 5, "--tokens needs config 5 (the language model's encoder)"
+        embedding = wl.token_batch(w, args.tokens, device=dev, rank=rank)
     eng = pipeline.AccordionStep(table, W, w.compressors, w.rank_low, w.rank_high, w.topk_low_bp, w.topk_high_bp,
                                  w.eta, 1e-8, w.check_every, device=dev, lazy_residual=not args.eager,
                                  optimizer=optimizer, extra_flags={"auto": 0, "always": 2, "never": 4}[args.pipeline],
-                                 overlap=not args.no_overlap, share_sms=args.share_sms)
+                                 overlap=not args.no_overlap, share_sms=args.share_sms, embedding=embedding)
     n_mat = table.n_matrix_params
     grad_bytes_step = n_comp * 4.0 * W * table.n_params
 
@@ -424,7 +438,7 @@ def main():
     by_regime = {}
     # the stored per-step traffic belongs to the default path (lazy residual, no optimiser tail, the library's choice
     # of first PowerSGD pass, the config's own worker count)
-    default_path = not (args.eager or args.sgd_tail or args.share_sms or args.pipeline != "auto")
+    default_path = not (args.eager or args.sgd_tail or args.adamw or args.tokens or args.share_sms or args.pipeline != "auto")
     for name in ("low", "high", "mixed"):
         ts = per_step[[r == name for r in regime]]
         if len(ts):
@@ -512,7 +526,11 @@ def main():
                            "compressors": list(w.compressors), "rank_low_high": [w.rank_low, w.rank_high],
                            "topk_bp_low_high": [w.topk_low_bp, w.topk_high_bp], "check_every": w.check_every,
                            "powersgd_residual": "eager" if args.eager else "lazy (applied on the next load)",
-                           "optimizer_tail": "Nesterov update fused into the step" if args.sgd_tail else "none",
+                           "optimizer_tail": ("Nesterov update fused into the step" if args.sgd_tail else
+                                              f"AdamW after the step, states in {args.adamw} bits, clipped"
+                                              if args.adamw else "none"),
+                           "encoder_gradient": (f"from {args.tokens} tokens per worker, in the step" if args.tokens
+                                                else "part of the gradient batch"),
                            "gradient_bytes_per_step": grad_bytes_step,
                            "l2_policy": f"inputs larger than L2: {RING} gradient batches of "
                                         f"{4 * W * table.stride / 1e6:.0f} MB cycled, no flush",

@@ -16,11 +16,92 @@ from . import binding
 from . import workloads as wl
 
 
+class AdamW:
+    """AdamW state of one flat parameter buffer (32-bit moments, or 8-bit ones with ``bits=8``) and the calls of one step:
+    with ``max_norm`` the layer norms of the gradient and the clip factor, then the update.  Everything the kernels read
+    -- hyper-parameters, step count, factor -- is on the device, so a captured step follows ``set_lr`` and counts itself;
+    a gradient whose norm is not finite leaves parameters, moments and step count alone."""
+
+    def __init__(self, ctx: "binding.Context", params: torch.Tensor, lr: float, betas=(0.9, 0.999), eps=1e-8,
+                 weight_decay=0.01, bits=32, max_norm: Optional[float] = None, decay_vectors=True,
+                 params_bf16: Optional[torch.Tensor] = None, seed=0):
+        if bits not in (32, 8):
+            raise ValueError(f"bits: expected 32 or 8, got {bits}")
+        dev = ctx.device
+        self.ctx, self.params, self.params_bf16 = ctx, params, params_bf16
+        self.max_norm, self.seed = max_norm, seed
+        self.flags = 0 if decay_vectors else binding.ACC_ADAMW_NO_VECTOR_DECAY
+        self.hyper = torch.tensor([lr, betas[0], betas[1], eps, weight_decay], dtype=torch.float64, device=dev)
+        self.step_count = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.bits = bits
+        if bits == 32:
+            self.m, self.v = torch.zeros(ctx.stride, device=dev), torch.zeros(ctx.stride, device=dev)
+        else:
+            self.m_code, self.r_code, self.m_scale, self.r_scale = ctx.new_adamw_8bit()
+        self.norm2 = torch.zeros(ctx.n_layers, dtype=torch.float64, device=dev)
+        self.norm = torch.zeros(1, dtype=torch.float64, device=dev)  # of the last gradient, with max_norm
+        self.factor = torch.ones(1, device=dev)
+
+    def set_lr(self, lr: float):
+        self.hyper[0:1].fill_(float(lr))
+
+    def step(self, d: torch.Tensor, stream=None) -> int:
+        """Updates the parameters from the gradient ``d`` ``[stride]``; returns the number of kernels launched."""
+        c, launches, factor = self.ctx, 0, None
+        if self.max_norm is not None:
+            factor = self.factor
+            c.acc_layer_norms(d, 1, self.norm2, stream=stream)
+            launches += c.last_launch_count()
+            c.acc_clip_factor(self.norm2, self.max_norm, factor, self.norm, stream=stream)
+            launches += c.last_launch_count()
+        if self.bits == 32:
+            c.acc_adamw(d, self.params, self.m, self.v, self.step_count, self.hyper, factor, self.params_bf16, self.flags,
+                        stream)
+        else:
+            c.acc_adamw_8bit(d, self.params, self.m_code, self.r_code, self.m_scale, self.r_scale, self.step_count,
+                             self.hyper, self.seed, factor, self.params_bf16, self.flags, stream)
+        return launches + c.last_launch_count()
+
+
+class TokenEmbedding:
+    """The embedding of one MATRIX layer (by name) for ``n`` tokens per worker: its lookup from the parameters and its
+    gradient into the layer's slice of every worker's gradient buffer."""
+
+    def __init__(self, ctx: "binding.Context", layer: str, n: int, scale=1.0, accumulate=False):
+        self.ctx, self.layer = ctx, ctx.table.names.index(layer)
+        self.scale, self.accumulate = float(scale), accumulate
+        self.workspace = ctx.new_embedding_workspace(self.layer, n)
+
+    def lookup(self, params: torch.Tensor, tokens: torch.Tensor, out: torch.Tensor, stream=None):
+        self.ctx.acc_embedding_lookup(self.layer, params, tokens, out, self.scale, stream)
+        return out
+
+    def backward(self, tokens: torch.Tensor, dy: torch.Tensor, grads: torch.Tensor, stream=None) -> int:
+        self.ctx.acc_embedding_grad(self.layer, tokens, dy, grads, self.scale, self.accumulate, self.workspace, stream)
+        return self.ctx.last_launch_count()
+
+
+def _make_optimizer(optimizer, ctx, stride, dev):
+    """``(params, mom, hyper, adamw)`` of an optimizer dict: the Nesterov tail's tensors, or an ``AdamW`` and its hyper-
+    parameters (``params`` and ``mom`` are then None: nothing is fused into the step)."""
+    if optimizer is None:
+        return None, None, None, None
+    kind = optimizer.get("kind", "nesterov")
+    if kind == "nesterov":
+        hyper = torch.tensor([optimizer["lr"], optimizer.get("momentum", 0.9), optimizer.get("weight_decay", 0.0)],
+                             dtype=torch.float32, device=dev)
+        return optimizer["params"], torch.zeros(stride, device=dev), hyper, None
+    if kind != "adamw":
+        raise ValueError(f"optimizer kind {kind!r}: expected 'nesterov' or 'adamw'")
+    adamw = AdamW(ctx, **{k: v for k, v in optimizer.items() if k != "kind"})
+    return None, None, adamw.hyper, adamw
+
+
 class AccordionStep:
     def __init__(self, table: wl.LayerTable, n_workers: int, compressors: Sequence[str] = ("powersgd",),
                  rank_low=2, rank_high=1, topk_low_bp=1000, topk_high_bp=100, eta=0.5, gs_eps=1e-8,
                  check_every=10, decider=0, q_init=None, device="cuda", lazy_residual=False, optimizer=None,
-                 extra_flags=0, overlap=True, share_sms=False):
+                 extra_flags=0, overlap=True, share_sms=False, embedding=None):
         """``overlap``: with two compressors, the TopK step runs on a second stream beside the PowerSGD step
         (they share only the gradients and the level array, both read-only), so that the short, latency-bound
         kernels of one hide behind the streaming kernels of the other; the results are the same bits.
@@ -29,7 +110,11 @@ class AccordionStep:
         ``extra_flags``: further ACC_FLAG_* bits for the context (e.g. forcing one implementation of the first
         PowerSGD pass).  ``optimizer``: None, or a dict ``{"params": tensor [stride], "lr": .., "momentum": 0.9,
         "weight_decay": 0.0}``: the Nesterov update (Appendix A) is then applied to ``params`` by the kernels
-        that produce the averaged gradient (one compressor only)."""
+        that produce the averaged gradient (one compressor only).  With ``"kind": "adamw"`` the dict holds the arguments
+        of ``AdamW`` (``params``, ``lr``, ``bits``, ``max_norm``, ...), whose step follows the compressor's.
+        ``embedding``: None, or a dict ``{"layer": name, "tokens": [W, n], "dy": [W, n, cols], "scale": 1.0,
+        "accumulate": False}`` of fixed device buffers: every step first writes (or adds) the embedding's gradient of the
+        tokens into that layer of the gradients it is given."""
         self.table, self.W = table, n_workers
         self.compressors = tuple(compressors)
         if optimizer is not None and len(self.compressors) != 1:
@@ -58,12 +143,12 @@ class AccordionStep:
         self.overlap = overlap
         self._side = torch.cuda.Stream(device=dev)
         self._fork, self._join = torch.cuda.Event(), torch.cuda.Event()
-        self.params = self.mom = self.hyper = None
-        if optimizer is not None:
-            self.params = optimizer["params"]
-            self.mom = torch.zeros(stride, device=dev)
-            self.hyper = torch.tensor([optimizer["lr"], optimizer.get("momentum", 0.9),
-                                       optimizer.get("weight_decay", 0.0)], dtype=torch.float32, device=dev)
+        self.params, self.mom, self.hyper, self.adamw = _make_optimizer(optimizer, self.ctx, stride, dev)
+        self.embedding = None
+        if embedding is not None:
+            self.tokens, self.dy = embedding["tokens"], embedding["dy"]
+            self.embedding = TokenEmbedding(self.ctx, embedding["layer"], self.tokens.shape[1], embedding.get("scale", 1.0),
+                                            embedding.get("accumulate", False))
         if "powersgd" in self.compressors:
             self.err_psgd = torch.zeros(n_workers, stride, device=dev)
             self.q = self.ctx.new_q(q_init if q_init is not None else wl.initial_q(table, rank_low, device=dev))
@@ -77,6 +162,8 @@ class AccordionStep:
     def step(self, grads: torch.Tensor, lr_curr: float = 0.1, lr_next: float = 0.1, stream=None):
         """One iteration on device-resident gradients ``[W, stride]``."""
         c = self.ctx
+        if self.embedding is not None:
+            self.launches += self.embedding.backward(self.tokens, self.dy, grads, stream)
         delta: Optional[torch.Tensor] = self.delta  # accumulated once per iteration, by the first compressor
         if self.overlap and len(self.compressors) == 2:
             main = stream if stream is not None else torch.cuda.current_stream(self.device)
@@ -112,6 +199,8 @@ class AccordionStep:
                 c.acc_topk_step(grads, self.err_topk, self.level, self.vals, self.idx, self.counts, self.out_topk,
                                 delta, stream)
             self.launches += c.last_launch_count()
+        if self.adamw is not None:
+            self.launches += self.adamw.step(self.outputs()[0], stream)
         self.t += 1
         if self.t % self.check_every == 0:
             c.acc_layer_norms(self.delta, 1, self.norm2_curr, stream=stream)
@@ -223,12 +312,7 @@ class BatchSizeStep:
         self.batch = torch.tensor([b_low], dtype=torch.int32, device=dev)  # the early phase is critical
         self.lr_scale = torch.ones(1, device=dev)
         self.pending = 0
-        self.params = self.mom = self.hyper = None
-        if optimizer is not None:
-            self.params = optimizer["params"]
-            self.mom = torch.zeros(stride, device=dev)
-            self.hyper = torch.tensor([optimizer["lr"], optimizer.get("momentum", 0.9),
-                                       optimizer.get("weight_decay", 0.0)], dtype=torch.float32, device=dev)
+        self.params, self.mom, self.hyper, self.adamw = _make_optimizer(optimizer, self.ctx, stride, dev)
 
     def micro_step(self, grads: torch.Tensor, stream=None):
         """One backward pass worth of gradients ``[W, stride]`` (device)."""
@@ -237,7 +321,11 @@ class BatchSizeStep:
 
     def apply(self, stream=None):
         """Ends the large batch: averages what was accumulated (and updates the parameters if asked)."""
-        self.ctx.acc_batch_average(self.acc, self.pending, self.out, self.params, self.mom, self.hyper, stream)
+        if self.adamw is None:
+            self.ctx.acc_batch_average(self.acc, self.pending, self.out, self.params, self.mom, self.hyper, stream)
+        else:
+            self.ctx.acc_batch_average(self.acc, self.pending, self.out, stream=stream)
+            self.adamw.step(self.out, stream)
         self.pending = 0
         return self.out
 
@@ -346,16 +434,11 @@ class DistributedStep:
         self.err = torch.zeros(n_local, stride, device=dev)
         self.out = torch.zeros(stride, device=dev)
         self.t = 0
-        self.params = self.mom = self.hyper = None
-        if optimizer is not None:
-            self.params = optimizer["params"]
-            self.mom = torch.zeros(stride, device=dev)
-            self.hyper = torch.tensor([optimizer["lr"], optimizer.get("momentum", 0.9),
-                                       optimizer.get("weight_decay", 0.0)], dtype=torch.float32, device=dev)
         self.parts = [_Part(self, ids, q_init) for ids in _layer_groups(table, groups)]
         # the whole table's context serves the detector (norms, Algorithm 1); with one group it is that group's
         self.ctx = self.parts[0].ctx if len(self.parts) == 1 else binding.Context(table, n_local, device=dev,
                                                                                    **self._cfg)
+        self.params, self.mom, self.hyper, self.adamw = _make_optimizer(optimizer, self.ctx, stride, dev)
         self._comm = torch.cuda.Stream(device=dev) if len(self.parts) > 1 else None
         one = self.parts[0]
         if len(self.parts) == 1:  # the single group's buffers under their plain names
@@ -426,6 +509,8 @@ class DistributedStep:
                 self._await(p, 0, main)
                 p.ctx.acc_topk_decompress(p.vals_all, p.idx_all, p.counts_all, self.world * self.n_local, p.vec,
                                           scale, self.out, self.params, self.mom, self.hyper, main)
+        if self.adamw is not None:  # every rank holds the same out, so every rank takes the same step
+            self.adamw.step(self.out, main)
         self.t += 1
         if self.t % self.check_every == 0:
             with torch.cuda.stream(main):

@@ -313,3 +313,15 @@ def initial_q(table: LayerTable, rank_max: int, seed: int = BASE_SEED, device="c
         else:
             qs.append(None)
     return qs
+
+
+def token_batch(wl: Workload, n: int, device="cpu", rank: int = 0):
+    """One batch for the embedding layer of the language-model workload: ``{"layer", "tokens" [W, n] int64, "dy"
+    [W, n, cols]}``, token ids Zipf(1)-distributed over a permutation of the rows, gradients of the layer's scale."""
+    layer = next(l for l, name in enumerate(wl.table.names) if name.startswith("encoder"))
+    rows, cols = int(wl.table.rows[layer]), int(wl.table.cols[layer])
+    g = _gen(device, wl.config_id, 2, rank)
+    weights = 1.0 / (torch.randperm(rows, generator=g, device=device).double() + 1.0)
+    tokens = torch.multinomial(weights, wl.n_workers * n, replacement=True, generator=g).view(wl.n_workers, n)
+    dy = torch.randn(wl.n_workers, n, cols, generator=g, device=device) * 1e-3
+    return {"layer": wl.table.names[layer], "tokens": tokens, "dy": dy}

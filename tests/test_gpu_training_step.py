@@ -1,0 +1,184 @@
+"""The training operators as they are used together: lookup -> embedding gradient -> compression step -> norms, clip factor
+and AdamW, called one by one and through the pipeline's classes, eager and as a replayed graph."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import accordion_oracle as orc
+from oracle import training_oracle as tor
+from paper_2010_16248_b200 import binding, pipeline, workloads as wl
+from tests import helpers as H
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _lm(vocab=211, hidden=26):
+    return wl.make_table(wl.shapes_lstm(vocab, hidden))
+
+
+def _grads(table, W, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    mask = torch.zeros(table.stride, device="cuda")
+    for _, sl in table.slices():
+        mask[sl] = 1.0
+    return torch.randn(W, table.stride, generator=g, device="cuda") * mask * 0.1
+
+
+def _tokens(W, n, rows, seed, pad=True):
+    rng = np.random.default_rng(seed)
+    t = np.minimum((rng.pareto(0.8, (W, n)) * 2).astype(np.int64), rows - 1)
+    if pad:
+        t[rng.random((W, n)) < 0.1] = -1
+    return torch.from_numpy(t).cuda()
+
+
+@pytest.mark.parametrize("compressor", ["powersgd", "topk"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_token_to_parameter_run_matches_the_oracles(compressor, bits):
+    """Two steps of a small language model's update, each stage checked against its oracle from the stage's own inputs."""
+    table, W, n, scale = _lm(), 3, 50, 5.0
+    layers = H.layers_of(table)
+    rows, cols = 211, 26
+    sl = slice(0, rows * cols)
+    ctx = binding.Context(table, W, rank_low=2, rank_high=1, topk_low_bp=1000, topk_high_bp=100)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    params = torch.randn(table.stride, generator=g, device="cuda") * 0.1
+    level = torch.tensor([l % 2 for l in range(table.n_layers)], dtype=torch.uint8, device="cuda")
+    err = torch.zeros(W, table.stride, device="cuda")
+    q, p = ctx.new_q(wl.initial_q(table, 2, device="cuda")), ctx.new_p()
+    vals, idx, counts = ctx.new_topk_buffers()
+    out = torch.zeros(table.stride, device="cuda")
+    opt = pipeline.AdamW(ctx, params, 1e-2, bits=bits, max_norm=0.5, decay_vectors=False, seed=7)
+    emb = pipeline.TokenEmbedding(ctx, "encoder.weight", n, scale)
+    hyper = opt.hyper.cpu().numpy()
+    for it in range(2):
+        tokens = _tokens(W, n, rows, it)
+        y = torch.empty(W, n, cols, device="cuda")
+        emb.lookup(params, tokens, y)
+        want = tor.embedding_lookup(params[sl].view(rows, cols).cpu().numpy(), tokens.cpu().numpy(), scale)
+        assert np.abs(y.view(-1, cols).cpu().numpy() - want).max() <= U * np.abs(want).max()
+        dy = y * 0.01 + 0.02  # the gradient of a quadratic and a linear term
+        grads = _grads(table, W, it)
+        before = grads.clone()
+        emb.backward(tokens, dy, grads)
+        for w in range(W):
+            G, S, K = tor.embedding_grad(tokens[w].cpu().numpy(), dy[w].cpu().numpy(), rows, scale)
+            got = grads[w, sl].view(rows, cols).cpu().numpy()
+            assert (np.abs(got - G) <= 1.01 * U * (np.maximum(K - 1, 0)[:, None] * S + 2 * np.abs(G))).all()
+        assert torch.equal(grads[:, sl.stop:], before[:, sl.stop:])
+        e0, q0 = err.clone(), q.clone()
+        if compressor == "powersgd":
+            ctx.acc_powersgd_step(grads, err, q, p, level, out)
+            H.check_powersgd_against_oracle(ctx, table, grads, e0, q0, level, out, err, q, p, 2, 1, 1e-8)
+        else:
+            ctx.acc_topk_step(grads, err, level, vals, idx, counts, out)
+            H.check_topk_against_oracle(ctx, table, grads, e0, level, vals, idx, counts, out, err, 1000, 100)
+        x0 = params.cpu().numpy().copy()
+        if bits == 32:
+            m0, v0 = opt.m.cpu().numpy().copy(), opt.v.cpu().numpy().copy()
+        else:
+            m0, r0 = (tor.decode(c.view(torch.uint8).cpu().numpy(), s.view(torch.uint8).cpu().numpy(), layers)
+                      for c, s in ((opt.m_code, opt.m_scale), (opt.r_code, opt.r_scale)))
+            v0 = r0 * r0
+        assert opt.step(out) == 4  # two for the norms, the factor, the update of a table this small
+        factor, norm = tor.clip_factor(orc.layer_norms2(out.cpu().numpy(), layers), 0.5)
+        assert abs(float(opt.factor) - factor) <= 2 * U * factor and abs(float(opt.norm) - norm) <= 1e-9 * norm
+        X, M, V, T = tor.adamw(out.cpu().numpy(), x0, m0, v0, it, hyper, layers, float(opt.factor), decay_vectors=False)
+        # (the update's error is at most 14 u of its size lr / (1 - beta1^t) * |m| / denominator <= lr / (1 - beta1^t) *
+        # (1 / sqrt(1 - beta2)) at these two steps, and 2 u of the parameter: the element-wise bounds have their own tests)
+        bound = 2 * U * np.abs(X) + 40 * U * 1e-2 / (1 - 0.9 ** T) * 32
+        got = params.cpu().numpy()
+        for (off, r, c, kind) in layers:
+            s = slice(off, off + r * c)
+            assert (np.abs(got[s] - X[s]) <= bound[s]).all()
+        assert int(opt.step_count) == T
+    assert ctx.acc_device_status() == 0
+
+
+@pytest.mark.parametrize("compressor,bits,max_norm", [("powersgd", 32, 0.3), ("topk", 8, None)])
+def test_accordion_step_with_adamw_and_embedding(compressor, bits, max_norm):
+    """The engine gives the bits of the calls one by one, and its captured graphs those of the engine."""
+    table, W, n = _lm(), 2, 40
+    tokens, g = _tokens(W, n, 211, 9), torch.Generator(device="cuda").manual_seed(4)
+    dy = torch.randn(W, n, 26, generator=g, device="cuda")
+    x0 = torch.randn(table.stride, generator=g, device="cuda")
+    ring = [_grads(table, W, 50 + k) for k in range(2)]
+
+    def engine(accumulate=False):
+        x, low = x0.clone(), torch.zeros(table.stride, dtype=torch.bfloat16, device="cuda")
+        opt = {"kind": "adamw", "params": x, "lr": 0.01, "bits": bits, "max_norm": max_norm, "params_bf16": low, "seed": 5}
+        emb = {"layer": "encoder.weight", "tokens": tokens, "dy": dy, "scale": 2.0, "accumulate": accumulate}
+        return x, low, pipeline.AccordionStep(table, W, (compressor,), check_every=2, lazy_residual=True, optimizer=opt,
+                                              embedding=emb)
+
+    x, low, eng = engine()
+    for k in range(4):
+        eng.step(ring[k % 2].clone())
+    ctx = binding.Context(table, W, flags=binding.ACC_FLAG_LAZY_RESIDUAL)
+    y = x0.clone()
+    opt = pipeline.AdamW(ctx, y, 0.01, bits=bits, max_norm=max_norm, seed=5)
+    emb = pipeline.TokenEmbedding(ctx, "encoder.weight", n, 2.0)
+    ref = pipeline.AccordionStep(table, W, (compressor,), check_every=2, lazy_residual=True)
+    for k in range(4):
+        grads = ring[k % 2].clone()
+        emb.backward(tokens, dy, grads)
+        ref.step(grads)
+        opt.step(ref.outputs()[0])
+    assert torch.equal(x, y) and not torch.equal(x, x0)
+    cover = torch.zeros(table.stride, dtype=torch.bool, device="cuda")
+    for _, sl in table.slices():
+        cover[sl] = True
+    assert torch.equal(low[cover], x[cover].to(torch.bfloat16))
+    z, _, cap = engine()
+    bufs = [r.clone() for r in ring]
+    cap.capture_graphs(bufs)
+    for k in range(4):
+        bufs[k % 2].copy_(ring[k % 2])
+        cap.step_graph(k % 2)
+    torch.cuda.synchronize()
+    assert torch.equal(x, z) and int(cap.adamw.step_count) == 4
+    cap.set_lr(0.0)
+    cap.adamw.hyper[4:].fill_(0.0)
+    before = z.clone()
+    cap.step_graph(0)
+    torch.cuda.synchronize()
+    assert torch.equal(before, z)  # the replayed graph reads the new rate
+    _, _, acc = engine(accumulate=True)
+    grads = ring[0].clone()
+    acc.step(grads)
+    want = ring[0].clone()
+    ctx.acc_embedding_grad(0, tokens, dy, want, scale=2.0, accumulate=True, workspace=ctx.new_embedding_workspace(0, n))
+    assert torch.equal(grads, want)
+
+
+def test_batch_mode_and_real_workers_take_adamw():
+    table, W = _lm(64, 12), 2
+    x0 = torch.randn(table.stride, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    grads = [_grads(table, W, k) for k in range(2)]
+    x, y = x0.clone(), x0.clone()
+    batch = pipeline.BatchSizeStep(table, W, 2, 4, 1, optimizer={"kind": "adamw", "params": x, "lr": 0.01, "bits": 8})
+    for g in grads:
+        batch.micro_step(g)
+    out = batch.apply().clone()
+    opt = pipeline.AdamW(batch.ctx, y, 0.01, bits=8)
+    opt.step(out)
+    assert torch.equal(x, y) and int(batch.adamw.step_count) == 1
+    x, y = x0.clone(), x0.clone()
+    dist = pipeline.DistributedStep(table, W, "topk", optimizer={"kind": "adamw", "params": x, "lr": 0.01})
+    out = dist.step(grads[0]).clone()
+    pipeline.AdamW(dist.ctx, y, 0.01).step(out)
+    assert torch.equal(x, y)
+
+
+def test_unknown_optimisers_are_refused():
+    table = _lm(64, 12)
+    x = torch.zeros(table.stride, device="cuda")
+    with pytest.raises(ValueError, match="kind"):
+        pipeline.AccordionStep(table, 1, ("topk",), optimizer={"kind": "adam", "params": x, "lr": 0.1})
+    with pytest.raises(ValueError, match="bits"):
+        pipeline.AccordionStep(table, 1, ("topk",), optimizer={"kind": "adamw", "params": x, "lr": 0.1, "bits": 16})
+    with pytest.raises(ValueError, match="one compressor"):
+        pipeline.AccordionStep(table, 1, ("powersgd", "topk"), optimizer={"kind": "adamw", "params": x, "lr": 0.1})
+    with pytest.raises(ValueError):
+        pipeline.TokenEmbedding(binding.Context(table, 1), "no such layer", 4)
