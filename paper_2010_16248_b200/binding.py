@@ -183,20 +183,22 @@ def _marshal(device, *items):
     the GPU the call runs on (there is no CPU path)."""
     index = None if device is None else device.index
     out = []
-    for a in items:
-        if type(a) is not tuple:
-            out.append(a)
-            continue
-        t, dtype, least, _ = a
-        if t is None:
-            out.append(None)
-            continue
-        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() < least or not t.is_contiguous():
-            _refuse(device, items)
-        on = t.get_device()  # -1: not on a GPU
-        if on < 0 or (index is not None and on != index):
-            _refuse(device, items)
-        out.append(t.data_ptr())
+    try:
+        for a in items:
+            if type(a) is not tuple:
+                out.append(a)
+                continue
+            t, dtype, least, _ = a
+            if t is None:
+                out.append(None)
+                continue
+            on = t.get_device()  # -1: not on a GPU
+            if (t.dtype is not dtype or t.numel() < least or not t.is_contiguous() or on < 0 or
+                    (on != index and index is not None)):
+                _refuse(device, items)
+            out.append(t.data_ptr())
+    except AttributeError:  # not a tensor
+        _refuse(device, items)
     return out
 
 
@@ -230,6 +232,8 @@ def _stream(stream, index=None) -> Optional[int]:
 
 class Context:
     """Owns the workspace tensor and the ``acc_ctx``; methods mirror the C entry points."""
+
+    _embedding_cols = None  # columns of each layer, 0 for VECTOR layers (built by the first embedding call)
 
     def __init__(self, table, n_workers, device="cuda", **cfg_kwargs):
         self.table = table
@@ -289,12 +293,12 @@ class Context:
     def _call(self, name, *items, stream=None):
         """Checks and marshals the tensor arguments, then calls entry point ``name`` on this context."""
         args = _marshal(self.device, *items)
-        index = self.device.index
+        index, entry = self.device.index, getattr(_lib, name)
         if index is None or index == torch.cuda.current_device():
-            st = getattr(lib(), name)(self._h, *args, _stream(stream, index))
+            st = entry(self._h, *args, _stream(stream, index))
         else:
             with torch.cuda.device(index):  # kernels launch on the current device
-                st = getattr(lib(), name)(self._h, *args, _stream(stream, index))
+                st = entry(self._h, *args, _stream(stream, index))
         if st != ACC_OK:
             raise AccError(st, name)
 
@@ -427,18 +431,25 @@ class Context:
 
     def _embedding(self, layer, tokens, values, what):
         """Index of the MATRIX layer, token type, number of values' rows and value type of an embedding call."""
+        if self._embedding_cols is None:
+            self._embedding_cols = [int(c) if q >= 0 else 0 for c, q in zip(self.table.cols, self.q_row)]
         layer = int(layer)
-        if not 0 <= layer < self.n_layers or self.q_row[layer] < 0:
+        cols = self._embedding_cols[layer] if 0 <= layer < self.n_layers else 0
+        if not cols:
             raise ValueError(f"layer {layer}: expected the index of a MATRIX layer")
-        for t, dtypes, name in ((tokens, _TOKEN_TYPES, "tokens"), (values, _VALUE_TYPES, what)):
-            if not isinstance(t, torch.Tensor):
-                raise ValueError(f"{name}: expected a torch tensor")
-            if t.dtype not in dtypes:
-                raise ValueError(f"{name}: expected one of {list(dtypes)}, got {t.dtype}")
-        n, cols = tokens.numel(), int(self.table.cols[layer])
+        try:
+            token_type, value_type = _TOKEN_TYPES[tokens.dtype], _VALUE_TYPES[values.dtype]
+        except (AttributeError, KeyError, TypeError):
+            for t, dtypes, name in ((tokens, _TOKEN_TYPES, "tokens"), (values, _VALUE_TYPES, what)):
+                if not isinstance(t, torch.Tensor):
+                    raise ValueError(f"{name}: expected a torch tensor") from None
+                if t.dtype not in dtypes:
+                    raise ValueError(f"{name}: expected one of {list(dtypes)}, got {t.dtype}") from None
+            raise
+        n = tokens.numel()
         if values.numel() != n * cols:
             raise ValueError(f"{what}: {values.numel()} elements, {n} tokens of {cols} columns need {n * cols}")
-        return layer, n, _TOKEN_TYPES[tokens.dtype], _VALUE_TYPES[values.dtype]
+        return layer, n, token_type, value_type
 
     def acc_embedding_lookup(self, layer, params, tokens, out, scale=1.0, stream=None):
         """``out[i] = scale * row tokens[i]`` of layer ``layer`` (its index) of ``params``; shapes only have to agree in

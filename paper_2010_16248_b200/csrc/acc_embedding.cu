@@ -206,7 +206,7 @@ __device__ __forceinline__ void scale_lane(Lane<VEC, COLS>& s, float scale, cons
 // entries.  A run that crosses from one warp to the next is finished by the warp where it begins, from the sums that the
 // others leave in shared memory.  Blocks behind those clear the rest of the layer, around the rows of the worker's tokens.
 constexpr int kSmallMost = 2048, kSmallCols = 64, kSmallPiece = 32768;
-constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21;  // a word holds row and position; tables of more rows, or
+constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21;  // a word holds row and position; tables of as many rows, or
 constexpr int kSmallWide = 1 << 20;                       // of more columns (32-bit offsets), take the long way
 
 // Ascending order of the block's words by a bitonic network over the first count2 (a power of two) of them; thread t holds
@@ -731,7 +731,7 @@ struct EmbPlan {
   int n_tiles;
 };
 static bool small_way(int rows, int cols, long long n) {
-  return n <= kSmallMost && rows <= kSmallRows && cols <= kSmallWide;
+  return n <= kSmallMost && rows < kSmallRows && cols <= kSmallWide;  // (all ones is no row's word)
 }
 static EmbPlan emb_plan(int W, int rows, int cols, long long n) {
   EmbPlan p{};

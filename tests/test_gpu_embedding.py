@@ -270,3 +270,65 @@ def test_refusals():
     assert lib.acc_embedding_grad(ctx._h, layer, t + 4, 1, 4, 1.0, d, 0, g, 0, w, n, None) == 2
     assert lib.acc_embedding_lookup(ctx._h, layer, g, t, 1, (1 << 28) + 1, 1.0, d, 0, None) == 1
     assert lib.acc_embedding_lookup(ctx._h, layer, None, t, 1, 4, 1.0, d, 0, None) == 1
+
+
+@pytest.mark.parametrize("n", [131072 - 1, 131072 + 1, 200000])
+def test_grad_many_sort_tiles(n):
+    """Either side of the count of tiles from which the sort's counts are summed by a kernel of their own."""
+    _run_grad(700, 8, 1, n, "zipf", dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("rows,n", [((1 << 21) - 1, 900), ((1 << 21) - 1, 2048), (1 << 21, 900), (1 << 21, 2048), ((1 << 21) + 1, 900), ((1 << 24) + 3, 2100)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_tables_of_many_rows(rows, n, accumulate):
+    """Rows that just fit, or no longer fit, a word beside the position; rows of more than three digits."""
+    cols = 2
+    table, ctx, layer = _ctx(rows, cols, 1)
+    rng = np.random.default_rng(n)
+    t = rng.integers(0, rows, (1, n))
+    t[0, ::7] = t[0, -1] = rows - 1
+    tokens = torch.from_numpy(t).cuda()
+    dy = torch.randn(1, n, cols, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda")
+    grads = torch.ones(1, table.stride, device="cuda")
+    ctx.acc_embedding_grad(layer, tokens, dy, grads, accumulate=accumulate, workspace=ctx.new_embedding_workspace(layer, n))
+    exact = torch.zeros(rows, cols, dtype=torch.float64, device="cuda")
+    exact.index_put_((tokens[0],), dy[0].double(), accumulate=True)
+    size = torch.zeros(rows, cols, dtype=torch.float64, device="cuda")
+    size.index_put_((tokens[0],), dy[0].double().abs(), accumulate=True)
+    got = grads[0, _slice(table, layer)].view(rows, cols).double()
+    base = 1.0 if accumulate else 0.0
+    # at most 62 additions a row (16 + 7 and 32 + 7), the scale's fma
+    bound = 1.01 * U * (62 * size + (exact + base).abs() + exact.abs())
+    assert bool(((got - base - exact).abs() <= bound).all())
+    outside = torch.ones(table.stride, dtype=torch.bool, device="cuda")
+    outside[_slice(table, layer)] = False
+    assert bool((grads[0, outside] == 1.0).all())
+
+
+def test_offsets_beyond_32_bits():
+    """The second worker's layer lies behind element 2^31 of the gradient buffers, the table behind element 2^31 of the
+    parameters."""
+    off, rows, cols, n = 2 ** 31 + 2 ** 18, 50, 6, 90
+    stride = off + 1024
+    table = wl.LayerTable(["far"], np.array([off], np.int64), np.array([rows], np.int32), np.array([cols], np.int32),
+                          np.array([wl.MATRIX], np.int32), stride)
+    ctx = binding.Context(table, 2)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    params = torch.empty(stride, device="cuda")
+    emb = torch.randn(rows, cols, generator=g, device="cuda")
+    params[off:off + rows * cols] = emb.reshape(-1)
+    grads = torch.empty(2, stride, device="cuda")
+    grads[:, off:].fill_(3.0)
+    for length in (n, 2500):
+        tokens = _tokens(np.random.default_rng(3), 2, length, rows, "padded")
+        out = torch.empty(2, length, cols, device="cuda")
+        ctx.acc_embedding_lookup(0, params, tokens, out)
+        want = emb[tokens.clamp(min=0)]
+        want[tokens < 0] = 0
+        assert torch.equal(out, want)
+        ctx.acc_embedding_grad(0, tokens, out, grads, workspace=ctx.new_embedding_workspace(0, length))
+        for w in range(2):
+            G, S, K = tor.embedding_grad(tokens[w].cpu().numpy(), out[w].cpu().numpy(), rows, 1.0)
+            got = grads[w, off:off + rows * cols].view(rows, cols).double().cpu().numpy()
+            assert (np.abs(got - G) <= 1.01 * U * (np.minimum(np.maximum(K - 1, 0), 62)[:, None] * S + 2 * np.abs(G))).all()
+        assert bool((grads[:, off + rows * cols:] == 3.0).all())
