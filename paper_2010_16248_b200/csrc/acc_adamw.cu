@@ -117,7 +117,8 @@ constexpr int kUnit = ACC_ADAMW_BLOCK, kUnitsPerTile = kTile / kUnit, kBlocksPer
 
 __global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* __restrict__ hyper,
                                   const float* __restrict__ factor, unsigned seed) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  await_previous();
+  let_next_start();  // (what the update loads ahead of its own wait was complete before this kernel's)
   bool skip;
   const float f = adam_factor(factor, skip);
   const long long t = *step + 1;
@@ -143,7 +144,7 @@ __device__ __forceinline__ bool adam_begin(AdamCoef& c, AdamCoef* sc, const Adam
     c = *sc;
     return true;
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  await_previous();
   c = *pre;
   return c.skip == 0;
 }
@@ -266,8 +267,8 @@ __device__ __forceinline__ unsigned top_bytes(unsigned a, unsigned b, unsigned c
   return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 
-// 16.03 B per parameter and 60 instructions, issued in some 60 % of the cycles: 50.1 M parameters take 132 us, 6.1 TB/s, the
-// last part of it the wait for loads at 40 warps per SM (48 registers; 142 us at 64 registers and 32 warps).
+// 16.03 B per parameter and 65 instructions, issued in some 60 % of the cycles: 50.1 M parameters take 136 us, 5.9 TB/s (133
+// us without the fp64 look at codes near a carry; 142 us at 64 registers and 32 warps per SM in place of 48 and 40).
 struct Adam8Regs { float4 d[2], x[2]; unsigned m[2], r[2], ms, rs; };
 struct Adam8Args {
   const float* d; float* params; unsigned char* mc; unsigned char* rc; unsigned char* ms; unsigned char* rs;
@@ -291,10 +292,35 @@ __device__ __forceinline__ void adam8_load(Adam8Regs& q, const AdamUnit& u, int 
   }
 }
 
+// Which way a code goes depends on whether the bits that are cut, plus the random ones, carry.  Where that sum is within
+// kNear of a carry -- one code in 30,000 --, fp32's roundings (up to 5 u of m's terms, 5 u of r; kNear is 32 u) could decide
+// it, so those elements' codes are worked out again in fp64: the codes are those of the 64-bit definition.
+constexpr unsigned kNear = 16u;
+__device__ __forceinline__ unsigned encode_exact(double y, unsigned rnd) {
+  if (y >= 0x1p-6) return (unsigned)((__double_as_longlong(y) + ((long long)rnd << 33)) >> 49) - ((1023u - 7u) << 3);
+  return (unsigned)floor(y * 512.0 + (double)rnd * 0x1p-16);
+}
+__device__ double scale_exact(unsigned byte) { return __longlong_as_double((long long)(byte + 1023u - 127u) << 52); }
+// Both codes of one element (m's in the low byte) from its old ones.
+__device__ __noinline__ unsigned adam8_exact(float d, unsigned mcode, unsigned rcode, unsigned ms, unsigned rs, unsigned bm,
+                                             unsigned br, unsigned word, float f, const double* hyper) {
+  const double b1 = hyper[1], b2 = hyper[2], g = (double)f * (double)d;
+  float a[4], b[4];
+  decode4(mcode, a);
+  decode4(rcode, b);
+  const double r0 = (double)b[0] * scale_exact(rs);
+  const double m = b1 * ((double)a[0] * scale_exact(ms)) + (1.0 - b1) * g;
+  const double r = sqrt(b2 * (r0 * r0) + (1.0 - b2) * (g * g));
+  unsigned qm = 0u, qr = 0u;
+  if (bm != 255u && bm != 0u) qm = encode_exact(fabs(m) / scale_exact(bm), (word ^ (word >> 16)) & 0xffffu) | (signbit(m) ? 0x80u : 0u);
+  if (br != 255u && br != 0u) qr = max(encode_exact(r / scale_exact(br), word >> 16), r > 0.0 ? 1u : 0u);
+  return qm | qr << 8;
+}
+
 // FULL: the unit has all of its 256 elements.
 template <bool FULL>
 __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u, int lane, const Adam8Args& p,
-                                           const AdamCoef& c) {
+                                           const AdamCoef& c, const double* __restrict__ hyper) {
   const float lrwd = u.decay ? c.lrwd : 0.f;
   const float sr = scale_of(q.rs);
   const float km = scale_of(q.ms) * c.b1, kr = sr * sr * c.b2;  // powers of two: exact
@@ -344,6 +370,7 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
     }
   }
   if (lane == 0) { p.ms[u.block] = (unsigned char)bm; p.rs[u.block] = (unsigned char)br; }
+  unsigned nearest = kNear * 2u;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int e = 128 * h + 4 * lane;
@@ -357,7 +384,9 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
       cm[k] = (tm & 0x80000000u) | ((tm << 4) & 0x7fffffffu);
       const float rk = r[4 * h + k];
       const float y = rk > 0.f ? fmaxf(rk * fr, 0x1p-129f) : 0.f;  // 2^-129: code 1
-      cr[k] = (__float_as_uint(y) + (hi << 4)) << 4;
+      const unsigned tr = __float_as_uint(y) + (hi << 4);
+      cr[k] = tr << 4;
+      nearest = __vimin3_u32(nearest, (tm + kNear) & 0xfffffu, (tr + kNear) & 0xfffffu);
     }
     const unsigned wm = top_bytes(cm[0], cm[1], cm[2], cm[3]), wr = top_bytes(cr[0], cr[1], cr[2], cr[3]);
     const long long at = u.base + e;
@@ -371,6 +400,20 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
           p.mc[at + k] = (unsigned char)(wm >> (8 * k));
           p.rc[at + k] = (unsigned char)(wr >> (8 * k));
         }
+    }
+  }
+  // (a lane's eight elements are shared out over eight lanes)
+  for (unsigned left = __ballot_sync(0xffffffffu, nearest < kNear * 2u); left != 0u; left &= left - 1u) {
+    const int owner = __ffs(left) - 1;
+    const unsigned m0 = __shfl_sync(0xffffffffu, q.m[0], owner), m1 = __shfl_sync(0xffffffffu, q.m[1], owner);
+    const unsigned r0 = __shfl_sync(0xffffffffu, q.r[0], owner), r1 = __shfl_sync(0xffffffffu, q.r[1], owner);
+    const int e = 128 * (lane >> 2) + 4 * owner + (lane & 3), sh = 8 * (lane & 3);
+    __syncwarp();  // the owner's own stores come first
+    if (lane < 8 && e < u.n) {
+      const unsigned codes = adam8_exact(p.d[u.base + e], (lane < 4 ? m0 : m1) >> sh & 0xffu, (lane < 4 ? r0 : r1) >> sh & 0xffu,
+                                         q.ms, q.rs, bm, br, mix32_open(c.key ^ (unsigned)(u.base + e)), c.f, hyper);
+      p.mc[u.base + e] = (unsigned char)codes;
+      p.rc[u.base + e] = (unsigned char)(codes >> 8);
     }
   }
 }
@@ -387,8 +430,8 @@ adamw_8bit_kernel(const FlatTile* __restrict__ tiles, const Adam8Args p, const A
   adam8_load(q, u, lane, p);
   AdamCoef c;
   if (!adam_begin<ONE>(c, &sc, pre, step, hyper, factor, seed)) return;
-  if (u.n == kUnit) adam8_unit<true>(q, u, lane, p, c);
-  else if (u.n > 0) adam8_unit<false>(q, u, lane, p, c);
+  if (u.n == kUnit) adam8_unit<true>(q, u, lane, p, c, hyper);
+  else if (u.n > 0) adam8_unit<false>(q, u, lane, p, c, hyper);
   adam_finish<ONE>(step, ticket);
 }
 
@@ -398,6 +441,8 @@ __global__ void __launch_bounds__(256)
 clip_factor_kernel(const double* __restrict__ n2_layers, int n_layers, double max_norm, float* __restrict__ factor,
                    double* __restrict__ norm) {
   __shared__ double sm[8];
+  await_previous();
+  let_next_start();
   double acc = 0.0;
   for (int l = threadIdx.x; l < n_layers; l += 256) acc += n2_layers[l];
   acc = warp_sum(acc);
@@ -420,23 +465,19 @@ static cudaError_t adam_launch(acc_ctx* ctx, int phase, int occupancy, void (*ke
                                unsigned seed, cudaStream_t s, Args... args) {
   const unsigned grid = (unsigned)ctx->plan.tiles.size() * kBlocksPerTile;
   const bool one = grid <= (unsigned)(occupancy * ctx->sm_count);
-  if (!one) {
+  if (one) {
+    PhaseTimer pt(ctx, phase, s);
+    kernel_one<<<grid, 256, 0, s>>>(args...);
+    return cudaGetLastError();
+  }
+  cudaError_t e;
+  {
     PhaseTimer pt(ctx, PH_ADAMW_COEF, s);
-    adamw_coef_kernel<<<1, 32, 0, s>>>(reinterpret_cast<AdamCoef*>(ctx->d_status + kAdamCoefWord),
-                                       reinterpret_cast<long long*>(step), hyper, factor, seed);
+    e = launch_early(adamw_coef_kernel, 1, 32, s, reinterpret_cast<AdamCoef*>(ctx->d_status + kAdamCoefWord),
+                     reinterpret_cast<long long*>(step), hyper, factor, seed);
   }
   PhaseTimer pt(ctx, phase, s);
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = one ? 0 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, one ? kernel_one : kernel_many, args...);
-  return e == cudaSuccess ? cudaGetLastError() : e;
+  return e == cudaSuccess ? launch_early(kernel_many, grid, 256, s, args...) : e;
 }
 
 cudaError_t launch_adamw(acc_ctx* ctx, const float* d, float* params, float* m, float* v, int64_t* step,
@@ -469,9 +510,8 @@ cudaError_t launch_clip_factor(acc_ctx* ctx, const double* n2_layers, double max
                                cudaStream_t s) {
   {
     PhaseTimer pt(ctx, PH_CLIP_FACTOR, s);
-    clip_factor_kernel<<<1, 256, 0, s>>>(n2_layers, ctx->cfg.n_layers, max_norm, factor, norm);
+    return launch_early(clip_factor_kernel, 1, 256, s, n2_layers, ctx->cfg.n_layers, max_norm, factor, norm);
   }
-  return cudaGetLastError();
 }
 
 }  // namespace acc

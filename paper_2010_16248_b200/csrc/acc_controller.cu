@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(256) norm_partial_kernel(const FlatTile* __res
                                                            const float* __restrict__ minus,
                                                            double* __restrict__ part, int n_tiles) {
   __shared__ double sm[8];
+  let_next_start();
   const FlatTile t = tiles[blockIdx.x];
   const int b = blockIdx.y;
   const float* x = buf + (long long)b * stride + t.base;
@@ -109,6 +110,8 @@ __global__ void norm_final_kernel(const DevLayer* __restrict__ layers, const dou
                                   double* __restrict__ norm2, int n_layers, int n_tiles) {
   const int l = blockIdx.x, b = blockIdx.y;
   const DevLayer L = layers[l];
+  await_previous();
+  let_next_start();
   double acc = 0.0;
 #pragma unroll 16
   for (int i = threadIdx.x; i < L.ntiles; i += 32) acc += part[(long long)b * n_tiles + L.tile0 + i];
@@ -225,10 +228,9 @@ cudaError_t launch_layer_norms(acc_ctx* ctx, const float* buf, long long stride,
   }
   {
     PhaseTimer pt(ctx, PH_NORM_FINAL, s);
-    norm_final_kernel<<<dim3((unsigned)ctx->cfg.n_layers, (unsigned)n_bufs), 32, 0, s>>>(
-        ctx->d_layers, ctx->d_norm_part, norm2, ctx->cfg.n_layers, nt);
+    return launch_early(norm_final_kernel, dim3((unsigned)ctx->cfg.n_layers, (unsigned)n_bufs), 32, s,
+                        (const DevLayer*)ctx->d_layers, (const double*)ctx->d_norm_part, norm2, ctx->cfg.n_layers, nt);
   }
-  return cudaGetLastError();
 }
 
 cudaError_t launch_layer_msdr(acc_ctx* ctx, const float* buf, long long stride, int n_bufs, double* moments,

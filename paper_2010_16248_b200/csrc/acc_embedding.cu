@@ -162,11 +162,6 @@ __device__ __forceinline__ void zero_piece_around(const EmbZero& z, const EmbArg
   }
 }
 
-// The next kernel of a call may start while this one runs; it waits for it in full before it touches memory.  (Only the
-// call's first kernel is launched without that permission, so it starts behind everything queued before the call.)
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // Columns of a lane: COLS / VEC vectors of VEC adjacent ones, 32 VEC columns apart.
 template <int VEC, int COLS> struct Lane { Vals<VEC> c[COLS / VEC]; };
 template <typename T, int VEC, int COLS> struct LaneRaw { typename Raw<T, VEC>::type c[COLS / VEC]; };
@@ -796,17 +791,13 @@ struct EmbLaunch {
   void operator()(int phase, void (*kernel)(Params...), long long blocks, int threads, Args... args) {
     if (blocks == 0 || err != cudaSuccess) return;
     PhaseTimer pt(ctx, phase, s);
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.stream = s;
-    cfg.attrs = &attr;
-    cfg.numAttrs = first ? 0 : 1;
+    if (first) {
+      kernel<<<(unsigned)blocks, threads, 0, s>>>(args...);
+      err = cudaGetLastError();
+    } else {
+      err = launch_early(kernel, (unsigned)blocks, threads, s, args...);
+    }
     first = false;
-    err = cudaLaunchKernelEx(&cfg, kernel, args...);
   }
 };
 
