@@ -641,40 +641,64 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   float* head = shead[warp] + lane * VEC;
   Lane<VEC, 4> sum = {};
   bool first_run = left;  // the run that an earlier warp, or the chunk before, began
+  const int tail_entry = open_right && warp == last_warp ? last_entry : -1;  // ends the chunk's last run, which goes on
+  auto finish_entry = [&](int e, const LaneRaw<float, VEC, 4>& o) {  // entry e ends a run
+    if (first_run) {
+      store_lane(head, sum, all_on);
+    } else if (e == tail_entry) {
+      store_lane(tail_slot, sum, on);
+    } else {
+      scale_lane<ACC>(sum, scale, o);
+      store_lane(gw + own[e] * (unsigned)a.cols, sum, on);
+    }
+    sum = {};
+    first_run = false;
+  };
   // 32 registers of loads in flight: 16 entries of bf16 at once, of fp32 (and of rows that are added to) eight
   constexpr int kBatch = sizeof(In) == 2 && !ACC ? 16 : 8;
-  unsigned todo = mask;
-#pragma unroll 1
-  while (todo != 0u) {
-    LaneRaw<In, VEC, 4> v[kBatch];
-    LaneRaw<float, VEC, 4> o[ACC ? kBatch : 1];
-    unsigned batch = todo;
+  if constexpr (FIRST) {  // the entries are the first ones of the warp's part
+    const int entries = __popc(mask);
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      if (todo == 0u) continue;
-      const int e = __ffs(todo) - 1;
-      todo &= todo - 1u;
-      const unsigned from = FIRST ? __shfl_sync(0xffffffffu, pos, e) : (unsigned)(c0 + kPart * warp + e);
-      load_lane(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
-      if (ACC && (ends >> e & 1u)) load_lane(o[k], (const float*)gw + own[e] * (unsigned)a.cols, on);
-    }
+    for (int e0 = 0; e0 < kPart; e0 += kBatch) {
+      if (e0 >= entries) break;
+      LaneRaw<In, VEC, 4> v[kBatch];
+      LaneRaw<float, VEC, 4> o[ACC ? kBatch : 1];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      if (batch == 0u) break;
-      const int e = __ffs(batch) - 1;
-      batch &= batch - 1u;
-      add_lane(sum, v[k]);
-      if (!(ends >> e & 1u)) continue;
-      if (first_run) {
-        store_lane(head, sum, all_on);
-      } else if (open_right && warp == last_warp && e == last_entry) {
-        store_lane(tail_slot, sum, on);
-      } else {
-        scale_lane<ACC>(sum, scale, o[ACC ? k : 0]);
-        store_lane(gw + own[e] * (unsigned)a.cols, sum, on);
+      for (int k = 0; k < kBatch; ++k) {
+        const unsigned from = __shfl_sync(0xffffffffu, pos, e0 + k);
+        if (e0 + k < entries) load_lane(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
+        if (ACC && (ends >> (e0 + k) & 1u)) load_lane(o[k], (const float*)gw + own[e0 + k] * (unsigned)a.cols, on);
       }
-      sum = {};
-      first_run = false;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (e0 + k >= entries) break;
+        add_lane(sum, v[k]);
+        if (ends >> (e0 + k) & 1u) finish_entry(e0 + k, o[ACC ? k : 0]);
+      }
+    }
+  } else {
+    unsigned todo = mask;
+#pragma unroll 1
+    while (todo != 0u) {
+      LaneRaw<In, VEC, 4> v[kBatch];
+      LaneRaw<float, VEC, 4> o[ACC ? kBatch : 1];
+      unsigned batch = todo;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (todo == 0u) continue;
+        const int e = __ffs(todo) - 1;
+        todo &= todo - 1u;
+        load_lane(v[k], iw + (unsigned long long)(unsigned)(c0 + kPart * warp + e) * (unsigned)a.cols, on);
+        if (ACC && (ends >> e & 1u)) load_lane(o[k], (const float*)gw + own[e] * (unsigned)a.cols, on);
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (batch == 0u) break;
+        const int e = __ffs(batch) - 1;
+        batch &= batch - 1u;
+        add_lane(sum, v[k]);
+        if (ends >> e & 1u) finish_entry(e, o[ACC ? k : 0]);
+      }
     }
   }
   bool pending = mask != 0u && !(ends >> (31 - __clz(mask)) & 1u);  // a run goes on behind this warp
