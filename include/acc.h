@@ -10,6 +10,9 @@
  *   - the compressor at the chosen level   PowerSGD rank r, or TopK K%   (Section "Experimental evaluation", first paragraph)
  *   - the mean over workers of the compressed gradients   (update rule of Section 3)
  *
+ * and, around it, what a training run with that step calls on the same buffers: the optimiser updates (Nesterov,
+ * AdamW with states in 32 or 8 bits), the gradient-norm clip, the lookup and the gradient of an embedding layer.
+ *
  * General rules, valid for every entry point unless it says otherwise:
  *   * Pointers named in "Device pointers" below are DEVICE pointers owned by the caller; the library
  *     never allocates or frees device memory.  `cfg`, `layers`, and every `int64_t*` / `size_t*`
@@ -393,7 +396,8 @@ int acc_download_out(acc_ctx* ctx, const float* out_dev, float* out_host, void* 
  * The pipelined kernels wait for their asynchronous shared-memory copies with a bounded number of polls;
  * should a wait ever give up, the block stores ACC_ETIMEOUT in a status word and returns instead of
  * hanging, and the results of that call are undefined.  This call copies the status word to *status
- * (HOST pointer; 0 = no such event) and blocks until the device has finished the work queued before it. */
+ * (HOST pointer; 0 = no such event) and blocks until the device has finished the work queued before it.
+ * The embedding calls store ACC_EINDEX there for a token id beyond the table (the first event is kept).      */
 int acc_device_status(acc_ctx* ctx, int32_t* status);
 
 /* Failure-detection self-test (no counterpart in the paper).  acc_selftest_wait_timeout launches one small kernel
