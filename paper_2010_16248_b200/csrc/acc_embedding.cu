@@ -163,33 +163,33 @@ __device__ __forceinline__ void zero_piece_around(const EmbZero& z, const EmbArg
   }
 }
 
-// Columns of a lane: COLS / VEC vectors of VEC adjacent ones, 32 VEC columns apart.
-template <int VEC, int COLS> struct Lane { Vals<VEC> c[COLS / VEC]; };
-template <typename T, int VEC, int COLS> struct LaneRaw { typename Raw<T, VEC>::type c[COLS / VEC]; };
-template <int VEC, int COLS, typename T>
-__device__ __forceinline__ void load_lane(LaneRaw<T, VEC, COLS>& v, const T* p, const bool* on) {
+// Four columns of a lane: 4 / VEC vectors of VEC adjacent ones, LANES VEC columns apart.
+template <int VEC> struct Lane { Vals<VEC> c[4 / VEC]; };
+template <typename T, int VEC> struct LaneRaw { typename Raw<T, VEC>::type c[4 / VEC]; };
+template <int LANES, int VEC, typename T>
+__device__ __forceinline__ void load_lane(LaneRaw<T, VEC>& v, const T* p, const bool* on) {
 #pragma unroll
-  for (int u = 0; u < COLS / VEC; ++u)
-    if (on[u]) v.c[u] = load_raw<VEC>(p + 32 * VEC * u);
+  for (int u = 0; u < 4 / VEC; ++u)
+    if (on[u]) v.c[u] = load_raw<VEC>(p + LANES * VEC * u);
 }
-template <int VEC, int COLS> __device__ __forceinline__ void store_lane(float* p, const Lane<VEC, COLS>& v, const bool* on) {
+template <int LANES, int VEC> __device__ __forceinline__ void store_lane(float* p, const Lane<VEC>& v, const bool* on) {
 #pragma unroll
-  for (int u = 0; u < COLS / VEC; ++u)
-    if (on[u]) store_vals<VEC>(p + 32 * VEC * u, v.c[u]);
+  for (int u = 0; u < 4 / VEC; ++u)
+    if (on[u]) store_vals<VEC>(p + LANES * VEC * u, v.c[u]);
 }
-template <int VEC, int COLS, typename T>
-__device__ __forceinline__ void add_lane(Lane<VEC, COLS>& s, const LaneRaw<T, VEC, COLS>& v) {
+template <int VEC, typename T>
+__device__ __forceinline__ void add_lane(Lane<VEC>& s, const LaneRaw<T, VEC>& v) {
 #pragma unroll
-  for (int u = 0; u < COLS / VEC; ++u) {
+  for (int u = 0; u < 4 / VEC; ++u) {
     const Vals<VEC> x = unpack(v.c[u]);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) s.c[u].v[j] += x.v[j];
   }
 }
-template <bool ACC, int VEC, int COLS>
-__device__ __forceinline__ void scale_lane(Lane<VEC, COLS>& s, float scale, const LaneRaw<float, VEC, COLS>& o) {
+template <bool ACC, int VEC>
+__device__ __forceinline__ void scale_lane(Lane<VEC>& s, float scale, const LaneRaw<float, VEC>& o) {
 #pragma unroll
-  for (int u = 0; u < COLS / VEC; ++u) {
+  for (int u = 0; u < 4 / VEC; ++u) {
     const Vals<VEC> x = unpack(o.c[u]);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) s.c[u].v[j] = ACC ? fmaf(scale, s.c[u].v[j], x.v[j]) : scale * s.c[u].v[j];
@@ -198,11 +198,12 @@ __device__ __forceinline__ void scale_lane(Lane<VEC, COLS>& s, float scale, cons
 
 // ---- up to kSmallMost tokens per worker: one launch -----------------------------------------------------------------
 // A block takes one worker and 64 columns.  It sorts all of the worker's tokens itself, in shared memory (2 us, the same in
-// every block, in place of a launch that every block would wait for), and hands every warp an equal share of the sorted
-// entries.  A run that crosses from one warp to the next is finished by the warp where it begins, from the sums that the
-// others leave in shared memory.  Blocks behind those clear the rest of the layer, around the rows of the worker's tokens.
-// 8 workers' 700 tokens of 650 columns are added to 33278 rows in 13 us (bound by the blocks' own instructions: 88 of the 148
-// SMs have one), written with all zeros in 112 us (692 MB: HBM).  This way / the long way below, accumulating: 64 tokens 5 /
+// every block, in place of a launch that every block would wait for), and hands every half warp an equal share of the sorted
+// entries, four columns to a lane: what steers the sums costs more instructions than the sums, so two entries share them.  A
+// run that crosses from one half warp to the next is finished by the one where it begins, from the sums that the others leave
+// in shared memory.  Blocks behind those clear the rest of the layer, around the rows of the worker's tokens.
+// 8 workers' 700 tokens of 650 columns are added to 33278 rows in 13 us (a chain of launch, tokens, sort and three batches of
+// loads on 88 of the 148 SMs; 5 us of it are its 32 MB), written with all zeros in 112 us (692 MB: HBM).  This way / the long way below, accumulating: 64 tokens 5 /
 // 13 us, 256 8 / 19, 1024 15 / 27, 2048 32 / 46 us.
 constexpr int kSmallMost = 2048, kSmallCols = 64, kSmallPiece = 32768;
 constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21;  // a word holds row and position; tables of as many rows, or
@@ -262,10 +263,10 @@ template <typename Tok, typename In, int VEC, bool ACC>
 __global__ void __launch_bounds__(ACC ? 1024 : 512, ACC ? 1 : 2)
 embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy, const EmbArgs a, int groups, float scale,
                        float* grads, int* status, const EmbZero z) {
-  constexpr int kThreads = ACC ? 1024 : 512, kWarps = kThreads / 32, kVecs = 2 / VEC, kMost = kSmallMost / kThreads;
+  constexpr int kThreads = ACC ? 1024 : 512, kParts = kThreads / 16, kVecs = 4 / VEC, kMost = kSmallMost / kThreads;
   __shared__ unsigned buf[2][kSmallMost];
   unsigned* entry = buf[0];  // row above position, sorted; kNoEntry: a token without a row
-  __shared__ __align__(8) float shead[kWarps][kSmallCols];
+  __shared__ __align__(16) float shead[kParts][kSmallCols];
   constexpr unsigned kNoEntry = 0xffffffffu, kPosMask = (1u << kSmallPosBits) - 1u;
   if (!ACC && (int)blockIdx.x >= z.first_block) {
     zero_piece_around<kSmallPiece>(z, a, buf[0], [&](int w, unsigned* taken, unsigned row0, unsigned row1) {
@@ -278,7 +279,8 @@ embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy
     });
     return;
   }
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 15, part = threadIdx.x >> 4;  // of a half warp; its number in the block
+  const unsigned half = 0xffffu << (threadIdx.x & 16);         // its lanes
   const int w = blockIdx.x / groups, group = blockIdx.x % groups;
   const Tok* tok = tokens + (long long)w * a.n;
   int count2 = 2;
@@ -308,74 +310,74 @@ embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy
   __syncthreads();
   auto row_at = [&](int e) { return entry[e] >> kSmallPosBits; };
   auto ends_at = [&](int e) { return e + 1 == count || row_at(e + 1) != row_at(e); };
-  const int share = (count + kWarps - 1) / kWarps, begin = min(share * warp, count), end = min(begin + share, count);
+  const int share = (count + kParts - 1) / kParts, begin = min(share * part, count), end = min(begin + share, count);
   const bool left = begin > 0 && begin < end && row_at(begin - 1) == row_at(begin);
 
   const int col = group * kSmallCols + lane * VEC;
   bool on[kVecs], all_on[kVecs];
 #pragma unroll
   for (int u = 0; u < kVecs; ++u) {
-    on[u] = col + 32 * VEC * u < a.cols;
+    on[u] = col + 16 * VEC * u < a.cols;
     all_on[u] = true;
   }
   const In* dw = dy + (long long)w * a.n * a.cols + col;
   float* gw = grads + (long long)w * a.stride + a.offset + col;
-  float* head = shead[warp] + lane * VEC;
-  Lane<VEC, 2> sum = {};
-  bool first_run = left;  // the run that an earlier warp began
-  constexpr int kBatch = 8;
+  float* head = shead[part] + lane * VEC;
+  Lane<VEC> sum = {};
+  bool first_run = left;  // the run that an earlier half warp began
+  constexpr int kBatch = 4;
 #pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += 32) {  // 32 entries, one per lane
+  for (int t0 = begin; t0 < end; t0 += 16) {  // 16 entries, one per lane
     const int e = t0 + lane;
     const unsigned mine = e < end ? entry[e] : 0u;
-    const unsigned ends = __ballot_sync(0xffffffffu, e < end && ends_at(e));
+    const unsigned ends = __ballot_sync(half, e < end && ends_at(e)) >> (threadIdx.x & 16);
 #pragma unroll 1
-    for (int k0 = 0; k0 < 32 && t0 + k0 < end; k0 += kBatch) {
-      LaneRaw<In, VEC, 2> v[kBatch];
-      LaneRaw<float, VEC, 2> o[ACC ? kBatch : 1];
+    for (int k0 = 0; k0 < 16 && t0 + k0 < end; k0 += kBatch) {
+      LaneRaw<In, VEC> v[kBatch];
+      LaneRaw<float, VEC> o[ACC ? kBatch : 1];
       const int here = end - t0 - k0;  // entries of this batch, or more
-      const unsigned e8 = ends >> k0;
+      const unsigned e4 = ends >> k0;
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
-        const unsigned x = __shfl_sync(0xffffffffu, mine, k0 + k);
-        if (k < here) load_lane(v[k], dw + (x & kPosMask) * (unsigned)a.cols, on);  // (both offsets fit 32 bits)
-        if (ACC && (e8 >> k & 1u)) load_lane(o[k], (const float*)gw + (x >> kSmallPosBits) * (unsigned)a.cols, on);
+        const unsigned x = __shfl_sync(half, mine, k0 + k, 16);
+        if (k < here) load_lane<16>(v[k], dw + (x & kPosMask) * (unsigned)a.cols, on);  // (both offsets fit 32 bits)
+        if (ACC && (e4 >> k & 1u)) load_lane<16>(o[k], (const float*)gw + (x >> kSmallPosBits) * (unsigned)a.cols, on);
       }
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         if (k >= here) break;
         add_lane(sum, v[k]);
-        if (!(e8 >> k & 1u)) continue;
+        if (!(e4 >> k & 1u)) continue;
         if (first_run) {
-          store_lane(head, sum, all_on);
+          store_lane<16>(head, sum, all_on);
         } else {
           scale_lane<ACC>(sum, scale, o[ACC ? k : 0]);
-          store_lane(gw + (__shfl_sync(0xffffffffu, mine, k0 + k) >> kSmallPosBits) * (unsigned)a.cols, sum, on);
+          store_lane<16>(gw + row_at(t0 + k0 + k) * (unsigned)a.cols, sum, on);
         }
         sum = {};
         first_run = false;
       }
     }
   }
-  bool pending = begin < end && !ends_at(end - 1);  // a run goes on behind this warp
+  bool pending = begin < end && !ends_at(end - 1);  // a run goes on behind this half warp
   if (pending && first_run) {
-    store_lane(head, sum, all_on);
+    store_lane<16>(head, sum, all_on);
     pending = false;
   }
   __syncthreads();
   if (!pending) return;
   float* g = gw + row_at(end - 1) * (unsigned)a.cols;
-  LaneRaw<float, VEC, 2> o;
-  if (ACC) load_lane(o, (const float*)g, on);
-  for (int q = warp + 1;; ++q) {
-    LaneRaw<float, VEC, 2> h;
-    load_lane(h, (const float*)shead[q] + lane * VEC, all_on);
+  LaneRaw<float, VEC> o;
+  if (ACC) load_lane<16>(o, (const float*)g, on);
+  for (int q = part + 1;; ++q) {
+    LaneRaw<float, VEC> h;
+    load_lane<16>(h, (const float*)shead[q] + lane * VEC, all_on);
     add_lane(sum, h);
     const int last = min(share * (q + 1), count) - 1;
-    if (row_at(last) != row_at(end - 1) || ends_at(last)) break;  // (the run ends inside that warp's share)
+    if (row_at(last) != row_at(end - 1) || ends_at(last)) break;  // (the run ends inside that share)
   }
   scale_lane<ACC>(sum, scale, o);
-  store_lane(g, sum, on);
+  store_lane<16>(g, sum, on);
 }
 
 // ---- more tokens: sort, sums by chunks, joins -------------------------------------------------------------------------
@@ -644,17 +646,17 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   float* gw = grads + (long long)w * a.stride + a.offset + col;
   float* tail_slot = l.slots + ((long long)wc * 2 + 1) * a.cols + col;
   float* head = shead[warp] + lane * VEC;
-  Lane<VEC, 4> sum = {};
+  Lane<VEC> sum = {};
   bool first_run = left;  // the run that an earlier warp, or the chunk before, began
   const int tail_entry = open_right && warp == last_warp ? last_entry : -1;  // ends the chunk's last run, which goes on
-  auto finish_entry = [&](int e, const LaneRaw<float, VEC, 4>& o) {  // entry e ends a run
+  auto finish_entry = [&](int e, const LaneRaw<float, VEC>& o) {  // entry e ends a run
     if (first_run) {
-      store_lane(head, sum, all_on);
+      store_lane<32>(head, sum, all_on);
     } else if (e == tail_entry) {
-      store_lane(tail_slot, sum, on);
+      store_lane<32>(tail_slot, sum, on);
     } else {
       scale_lane<ACC>(sum, scale, o);
-      store_lane(gw + own[e] * (unsigned)a.cols, sum, on);
+      store_lane<32>(gw + own[e] * (unsigned)a.cols, sum, on);
     }
     sum = {};
     first_run = false;
@@ -666,13 +668,13 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
 #pragma unroll
     for (int e0 = 0; e0 < kPart; e0 += kBatch) {
       if (e0 >= entries) break;
-      LaneRaw<In, VEC, 4> v[kBatch];
-      LaneRaw<float, VEC, 4> o[ACC ? kBatch : 1];
+      LaneRaw<In, VEC> v[kBatch];
+      LaneRaw<float, VEC> o[ACC ? kBatch : 1];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const unsigned from = __shfl_sync(0xffffffffu, pos, e0 + k);
-        if (e0 + k < entries) load_lane(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
-        if (ACC && (ends >> (e0 + k) & 1u)) load_lane(o[k], (const float*)gw + own[e0 + k] * (unsigned)a.cols, on);
+        if (e0 + k < entries) load_lane<32>(v[k], iw + (unsigned long long)from * (unsigned)a.cols, on);
+        if (ACC && (ends >> (e0 + k) & 1u)) load_lane<32>(o[k], (const float*)gw + own[e0 + k] * (unsigned)a.cols, on);
       }
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
@@ -685,16 +687,16 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
     unsigned todo = mask;
 #pragma unroll 1
     while (todo != 0u) {
-      LaneRaw<In, VEC, 4> v[kBatch];
-      LaneRaw<float, VEC, 4> o[ACC ? kBatch : 1];
+      LaneRaw<In, VEC> v[kBatch];
+      LaneRaw<float, VEC> o[ACC ? kBatch : 1];
       unsigned batch = todo;
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         if (todo == 0u) continue;
         const int e = __ffs(todo) - 1;
         todo &= todo - 1u;
-        load_lane(v[k], iw + (unsigned long long)(unsigned)(c0 + kPart * warp + e) * (unsigned)a.cols, on);
-        if (ACC && (ends >> e & 1u)) load_lane(o[k], (const float*)gw + own[e] * (unsigned)a.cols, on);
+        load_lane<32>(v[k], iw + (unsigned long long)(unsigned)(c0 + kPart * warp + e) * (unsigned)a.cols, on);
+        if (ACC && (ends >> e & 1u)) load_lane<32>(o[k], (const float*)gw + own[e] * (unsigned)a.cols, on);
       }
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
@@ -708,7 +710,7 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   }
   bool pending = mask != 0u && !(ends >> (31 - __clz(mask)) & 1u);  // a run goes on behind this warp
   if (pending && first_run) {
-    store_lane(head, sum, all_on);
+    store_lane<32>(head, sum, all_on);
     pending = false;
   }
   __syncthreads();
@@ -716,8 +718,8 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   auto finish_run = [&](int q) {
     for (;; ++q) {
       if (smask[q] == 0u) continue;
-      LaneRaw<float, VEC, 4> h;
-      load_lane(h, (const float*)shead[q] + lane * VEC, all_on);
+      LaneRaw<float, VEC> h;
+      load_lane<32>(h, (const float*)shead[q] + lane * VEC, all_on);
       add_lane(sum, h);
       if (sends[q] != 0u) return q == last_warp && __ffs(sends[q]) - 1 == last_entry;
     }
@@ -725,22 +727,22 @@ embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs 
   if (pending) {
     const unsigned row = own[31 - __clz(mask)];
     float* g = gw + row * (unsigned)a.cols;
-    LaneRaw<float, VEC, 4> o;
-    if (ACC) load_lane(o, (const float*)g, on);
+    LaneRaw<float, VEC> o;
+    if (ACC) load_lane<32>(o, (const float*)g, on);
     if (finish_run(warp + 1) && open_right) {
-      store_lane(tail_slot, sum, on);
+      store_lane<32>(tail_slot, sum, on);
     } else {
       scale_lane<ACC>(sum, scale, o);
-      store_lane(g, sum, on);
+      store_lane<32>(g, sum, on);
     }
   }
   if (warp == 0 && open_left) {
-    LaneRaw<float, VEC, 4> h;
-    load_lane(h, (const float*)shead[0] + lane * VEC, all_on);
+    LaneRaw<float, VEC> h;
+    load_lane<32>(h, (const float*)shead[0] + lane * VEC, all_on);
     sum = {};
     add_lane(sum, h);
     if (sends[0] == 0u) finish_run(1);
-    store_lane(tail_slot - a.cols, sum, on);
+    store_lane<32>(tail_slot - a.cols, sum, on);
   }
 }
 
@@ -879,7 +881,8 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
     };
     auto typed = [&](auto tok, auto in) {
       if (L.vec == 1) run(tok, in, std::integral_constant<int, 1>());
-      else run(tok, in, std::integral_constant<int, 2>());
+      else if (L.vec == 2) run(tok, in, std::integral_constant<int, 2>());
+      else run(tok, in, std::integral_constant<int, 4>());
     };
     if (tok64) bf16 ? typed((long long)0, __nv_bfloat16()) : typed((long long)0, 0.f);
     else bf16 ? typed(0, __nv_bfloat16()) : typed(0, 0.f);
