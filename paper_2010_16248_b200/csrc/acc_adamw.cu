@@ -69,14 +69,8 @@ __device__ __forceinline__ float adam_factor(const float* factor, bool& skip) {
   return f;
 }
 
-// Root and quotient as one special-function instruction each (sqrt.approx: relative error 2^-23; div.approx: 2 ulp for
-// divisors in [2^-126, 2^126]): the update's own roundings are of that size, and the correctly rounded forms with their
-// range checks were a fifth of the 8-bit kernel's instructions.
-__device__ __forceinline__ float sqrt_fast(float x) {
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
+// div.approx: 2 ulp for divisors in [2^-126, 2^126], one reciprocal and one product; the update's own roundings are of that
+// size, and the correctly rounded quotient with its range checks costs the 8-bit kernel ten more instructions per element.
 __device__ __forceinline__ float div_fast(float a, float b) {
   float r;
   asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -89,13 +83,14 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // NaN where eithe
 }
 
 // The update of one element: the old moments arrive as factors, beta1 m = ka a and beta2 v = kb b; m, v, r = sqrt(v) are
-// the new ones in fp32; returns the new parameter.
+// the new ones in fp32; returns the new parameter.  The moments are sums of two rounded products and a rounded root, the
+// formulas taken word by word: no fused step, so that a state's code does not hang on how a compiler contracts them.
 __device__ __forceinline__ float adam_update(float d, float x, float a, float ka, float b, float kb, float& m, float& v,
                                              float& r, const AdamCoef& c, float lrwd) {
   const float g = c.f * d;
-  m = fmaf(ka, a, c.ob1 * g);
-  v = fmaf(kb, b, c.ob2 * (g * g));
-  r = sqrt_fast(v);
+  m = __fadd_rn(__fmul_rn(ka, a), __fmul_rn(c.ob1, g));
+  v = __fadd_rn(__fmul_rn(kb, b), __fmul_rn(c.ob2, __fmul_rn(g, g)));
+  r = __fsqrt_rn(v);
   return fmaf(-c.size, div_fast(m, fmaf(r, c.rc2, c.eps)), fmaf(-lrwd, x, x));
 }
 
@@ -112,7 +107,7 @@ __device__ __forceinline__ uint2 bf16x4(const float4 v) {
 // once (ONE), each does so itself behind its loads, and the last block to finish advances the step count.  Larger tables,
 // whose blocks follow one another on an SM and would pay that time again and again, take them from a kernel of one warp
 // launched ahead; the update's blocks start beside it and wait for it behind their loads.  In every block / from a kernel
-// ahead: 0.29 M parameters 3.4 / 3.7 us (and one launch less), 5.1 M in 8 bits 20.9 / 16.4 us, 50.1 M in 8 bits 171 / 136 us.
+// ahead: 0.29 M parameters 3.4 / 3.7 us (and one launch less), 5.1 M in 8 bits 20.9 / 16.4 us, 50.1 M in 8 bits 171 / 138 us.
 constexpr int kUnit = ACC_ADAMW_BLOCK, kUnitsPerTile = kTile / kUnit, kBlocksPerTile = kUnitsPerTile / 8;
 
 __global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* __restrict__ hyper,
@@ -267,8 +262,8 @@ __device__ __forceinline__ unsigned top_bytes(unsigned a, unsigned b, unsigned c
   return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 
-// 16.03 B per parameter and 65 instructions, issued in some 60 % of the cycles: 50.1 M parameters take 136 us, 5.9 TB/s (133
-// us without the fp64 look at codes near a carry; 142 us at 64 registers and 32 warps per SM in place of 48 and 40).
+// 16.03 B per parameter and some 65 instructions, issued in 60 % of the cycles: 50.1 M parameters take 138 us, 5.8 TB/s (48
+// registers and 40 warps per SM; 8 us more at 64 registers and 32 warps).
 struct Adam8Regs { float4 d[2], x[2]; unsigned m[2], r[2], ms, rs; };
 struct Adam8Args {
   const float* d; float* params; unsigned char* mc; unsigned char* rc; unsigned char* ms; unsigned char* rs;
@@ -292,35 +287,10 @@ __device__ __forceinline__ void adam8_load(Adam8Regs& q, const AdamUnit& u, int 
   }
 }
 
-// Which way a code goes depends on whether the bits that are cut, plus the random ones, carry.  Where that sum is within
-// kNear of a carry -- one code in 30,000 --, fp32's roundings (up to 5 u of m's terms, 5 u of r; kNear is 32 u) could decide
-// it, so those elements' codes are worked out again in fp64: the codes are those of the 64-bit definition.
-constexpr unsigned kNear = 16u;
-__device__ __forceinline__ unsigned encode_exact(double y, unsigned rnd) {
-  if (y >= 0x1p-6) return (unsigned)((__double_as_longlong(y) + ((long long)rnd << 33)) >> 49) - ((1023u - 7u) << 3);
-  return (unsigned)floor(y * 512.0 + (double)rnd * 0x1p-16);
-}
-__device__ double scale_exact(unsigned byte) { return __longlong_as_double((long long)(byte + 1023u - 127u) << 52); }
-// Both codes of one element (m's in the low byte) from its old ones.
-__device__ __noinline__ unsigned adam8_exact(float d, unsigned mcode, unsigned rcode, unsigned ms, unsigned rs, unsigned bm,
-                                             unsigned br, unsigned word, float f, const double* hyper) {
-  const double b1 = hyper[1], b2 = hyper[2], g = (double)f * (double)d;
-  float a[4], b[4];
-  decode4(mcode, a);
-  decode4(rcode, b);
-  const double r0 = (double)b[0] * scale_exact(rs);
-  const double m = b1 * ((double)a[0] * scale_exact(ms)) + (1.0 - b1) * g;
-  const double r = sqrt(b2 * (r0 * r0) + (1.0 - b2) * (g * g));
-  unsigned qm = 0u, qr = 0u;
-  if (bm != 255u && bm != 0u) qm = encode_exact(fabs(m) / scale_exact(bm), (word ^ (word >> 16)) & 0xffffu) | (signbit(m) ? 0x80u : 0u);
-  if (br != 255u && br != 0u) qr = max(encode_exact(r / scale_exact(br), word >> 16), r > 0.0 ? 1u : 0u);
-  return qm | qr << 8;
-}
-
 // FULL: the unit has all of its 256 elements.
 template <bool FULL>
 __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u, int lane, const Adam8Args& p,
-                                           const AdamCoef& c, const double* __restrict__ hyper) {
+                                           const AdamCoef& c) {
   const float lrwd = u.decay ? c.lrwd : 0.f;
   const float sr = scale_of(q.rs);
   const float km = scale_of(q.ms) * c.b1, kr = sr * sr * c.b2;  // powers of two: exact
@@ -370,7 +340,6 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
     }
   }
   if (lane == 0) { p.ms[u.block] = (unsigned char)bm; p.rs[u.block] = (unsigned char)br; }
-  unsigned nearest = kNear * 2u;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int e = 128 * h + 4 * lane;
@@ -384,9 +353,7 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
       cm[k] = (tm & 0x80000000u) | ((tm << 4) & 0x7fffffffu);
       const float rk = r[4 * h + k];
       const float y = rk > 0.f ? fmaxf(rk * fr, 0x1p-129f) : 0.f;  // 2^-129: code 1
-      const unsigned tr = __float_as_uint(y) + (hi << 4);
-      cr[k] = tr << 4;
-      nearest = __vimin3_u32(nearest, (tm + kNear) & 0xfffffu, (tr + kNear) & 0xfffffu);
+      cr[k] = (__float_as_uint(y) + (hi << 4)) << 4;
     }
     const unsigned wm = top_bytes(cm[0], cm[1], cm[2], cm[3]), wr = top_bytes(cr[0], cr[1], cr[2], cr[3]);
     const long long at = u.base + e;
@@ -400,20 +367,6 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
           p.mc[at + k] = (unsigned char)(wm >> (8 * k));
           p.rc[at + k] = (unsigned char)(wr >> (8 * k));
         }
-    }
-  }
-  // (a lane's eight elements are shared out over eight lanes)
-  for (unsigned left = __ballot_sync(0xffffffffu, nearest < kNear * 2u); left != 0u; left &= left - 1u) {
-    const int owner = __ffs(left) - 1;
-    const unsigned m0 = __shfl_sync(0xffffffffu, q.m[0], owner), m1 = __shfl_sync(0xffffffffu, q.m[1], owner);
-    const unsigned r0 = __shfl_sync(0xffffffffu, q.r[0], owner), r1 = __shfl_sync(0xffffffffu, q.r[1], owner);
-    const int e = 128 * (lane >> 2) + 4 * owner + (lane & 3), sh = 8 * (lane & 3);
-    __syncwarp();  // the owner's own stores come first
-    if (lane < 8 && e < u.n) {
-      const unsigned codes = adam8_exact(p.d[u.base + e], (lane < 4 ? m0 : m1) >> sh & 0xffu, (lane < 4 ? r0 : r1) >> sh & 0xffu,
-                                         q.ms, q.rs, bm, br, mix32_open(c.key ^ (unsigned)(u.base + e)), c.f, hyper);
-      p.mc[u.base + e] = (unsigned char)codes;
-      p.rc[u.base + e] = (unsigned char)(codes >> 8);
     }
   }
 }
@@ -430,8 +383,8 @@ adamw_8bit_kernel(const FlatTile* __restrict__ tiles, const Adam8Args p, const A
   adam8_load(q, u, lane, p);
   AdamCoef c;
   if (!adam_begin<ONE>(c, &sc, pre, step, hyper, factor, seed)) return;
-  if (u.n == kUnit) adam8_unit<true>(q, u, lane, p, c, hyper);
-  else if (u.n > 0) adam8_unit<false>(q, u, lane, p, c, hyper);
+  if (u.n == kUnit) adam8_unit<true>(q, u, lane, p, c);
+  else if (u.n > 0) adam8_unit<false>(q, u, lane, p, c);
   adam_finish<ONE>(step, ticket);
 }
 
