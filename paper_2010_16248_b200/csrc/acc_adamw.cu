@@ -42,7 +42,7 @@ __device__ __forceinline__ unsigned mix32(unsigned x) {
 }
 
 // Two lanes take one power each.
-__device__ __forceinline__ void adam_coef(AdamCoef* c, const double* __restrict__ hyper, long long t, float f,
+__device__ __forceinline__ void adam_coef(AdamCoef* c, const double* hyper, long long t, float f,
                                           unsigned seed) {
   if (threadIdx.x >= 2) return;
   const double lr = hyper[0], b = hyper[1 + threadIdx.x];
@@ -64,7 +64,7 @@ __device__ __forceinline__ void adam_coef(AdamCoef* c, const double* __restrict_
 
 // A factor that is not finite means that the gradient's norm was not: the call then changes nothing.
 __device__ __forceinline__ float adam_factor(const float* factor, bool& skip) {
-  const float f = factor != nullptr ? __ldg(factor) : 1.f;
+  const float f = factor != nullptr ? *factor : 1.f;
   skip = !isfinite(f);
   return f;
 }
@@ -110,8 +110,8 @@ __device__ __forceinline__ uint2 bf16x4(const float4 v) {
 // ahead: 0.29 M parameters 3.4 / 3.7 us (and one launch less), 5.1 M in 8 bits 20.9 / 16.4 us, 50.1 M in 8 bits 171 / 138 us.
 constexpr int kUnit = ACC_ADAMW_BLOCK, kUnitsPerTile = kTile / kUnit, kBlocksPerTile = kUnitsPerTile / 8;
 
-__global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* __restrict__ hyper,
-                                  const float* __restrict__ factor, unsigned seed) {
+__global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* hyper,
+                                  const float* factor, unsigned seed) {
   await_previous();
   let_next_start();  // (what the update loads ahead of its own wait was complete before this kernel's)
   bool skip;
@@ -128,7 +128,7 @@ __global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* __
 // The block's coefficients, from `pre` or worked out here; false where nothing is to change.
 template <bool ONE>
 __device__ __forceinline__ bool adam_begin(AdamCoef& c, AdamCoef* sc, const AdamCoef* pre, const long long* step,
-                                           const double* __restrict__ hyper, const float* __restrict__ factor,
+                                           const double* hyper, const float* factor,
                                            unsigned seed) {
   if (ONE) {
     bool skip;
@@ -169,7 +169,7 @@ __device__ __forceinline__ AdamUnit adam_unit(const FlatTile* __restrict__ tiles
 template <bool ONE>
 __global__ void __launch_bounds__(256)
 adamw_kernel(const FlatTile* __restrict__ tiles, const float* __restrict__ d, float* params, float* ms, float* vs,
-             const AdamCoef* pre, long long* step, const double* __restrict__ hyper, const float* __restrict__ factor,
+             const AdamCoef* pre, long long* step, const double* hyper, const float* factor,
              unsigned short* low, int flags, unsigned* ticket) {
   __shared__ AdamCoef sc;
   const int lane = threadIdx.x & 31;
@@ -374,7 +374,7 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
 template <bool ONE>
 __global__ void __launch_bounds__(256, 5)
 adamw_8bit_kernel(const FlatTile* __restrict__ tiles, const Adam8Args p, const AdamCoef* pre, long long* step,
-                  const double* __restrict__ hyper, const float* __restrict__ factor, unsigned seed, int flags,
+                  const double* hyper, const float* factor, unsigned seed, int flags,
                   unsigned* ticket) {
   __shared__ AdamCoef sc;
   const int lane = threadIdx.x & 31;
@@ -391,8 +391,7 @@ adamw_8bit_kernel(const FlatTile* __restrict__ tiles, const Adam8Args p, const A
 // One block: norm = sqrt(sum of the layers' squared norms, fp64, fixed order); factor = min(1, max_norm / norm), NaN where
 // the norm is not finite.
 __global__ void __launch_bounds__(256)
-clip_factor_kernel(const double* __restrict__ n2_layers, int n_layers, double max_norm, float* __restrict__ factor,
-                   double* __restrict__ norm) {
+clip_factor_kernel(const double* n2_layers, int n_layers, double max_norm, float* factor, double* norm) {
   __shared__ double sm[8];
   await_previous();
   let_next_start();

@@ -106,8 +106,8 @@ __global__ void __launch_bounds__(256) norm_partial_kernel(const FlatTile* __res
 }
 
 // One warp per (layer, buffer): sums the layer's tile partials in a fixed order.
-__global__ void norm_final_kernel(const DevLayer* __restrict__ layers, const double* __restrict__ part,
-                                  double* __restrict__ norm2, int n_layers, int n_tiles) {
+__global__ void norm_final_kernel(const DevLayer* __restrict__ layers, const double* part, double* norm2, int n_layers,
+                                  int n_tiles) {
   const int l = blockIdx.x, b = blockIdx.y;
   const DevLayer L = layers[l];
   await_previous();

@@ -65,8 +65,8 @@ __device__ __forceinline__ unsigned token_row(long long tok, int rows, int* stat
 }
 
 // One warp per token:  out_i = scale * row(tok_i), rounded once; zeros where there is no row.  A lane's loads of a batch of
-// VEC columns go out together.  Bound by what L2 delivers, 340 MB and 170 MB back for 8 x 16384 tokens of 650 columns to
-// bf16: 47 us (52 us with four loads at a time; 64 us with vectors of four columns, realigned by shuffles).
+// vectors of VEC columns go out together.  Bound by what L2 delivers, 340 MB and 170 MB back for 8 x 16384 tokens of 650
+// columns to bf16: 45 us (49 us with four loads at a time; 64 us with vectors of four columns, realigned by shuffles).
 template <typename Tok, typename Out, int VEC>
 __global__ void __launch_bounds__(256)
 embedding_lookup_kernel(const float* __restrict__ table, int rows, int cols, const Tok* __restrict__ tokens, long long n,
@@ -75,21 +75,25 @@ embedding_lookup_kernel(const float* __restrict__ table, int rows, int cols, con
   if (i >= n) return;
   const int lane = threadIdx.x & 31;
   const unsigned row = token_row((long long)tokens[i], rows, status);
-  const bool none = row == (unsigned)rows;
-  const float* src = table + (none ? 0ll : (long long)row * cols);
-  Out* dst = out + i * cols;
-  constexpr int kBatch = 6;
-  for (int c0 = VEC * lane; c0 < cols; c0 += 32 * VEC * kBatch) {
+  Out* dst = out + i * cols + VEC * lane;
+  int left = cols / VEC - lane;  // vectors of this lane: those k with 32 k < left
+  if (row == (unsigned)rows) {
+    for (; left > 0; left -= 32, dst += 32 * VEC) store_vals<VEC>(dst, Vals<VEC>{});
+    return;
+  }
+  const float* src = table + (long long)row * cols + VEC * lane;
+  constexpr int kBatch = VEC == 4 ? 6 : 12;
+  for (; left > 0; left -= 32 * kBatch, src += 32 * VEC * kBatch, dst += 32 * VEC * kBatch) {
     Vals<VEC> v[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k)
-      if (c0 + 32 * VEC * k < cols) v[k] = load_vals<VEC>(src + c0 + 32 * VEC * k);
+      if (32 * k < left) v[k] = load_vals<VEC>(src + 32 * VEC * k);
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      if (c0 + 32 * VEC * k >= cols) continue;
+      if (32 * k >= left) break;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) v[k].v[j] = none ? 0.f : v[k].v[j] * scale;
-      store_vals<VEC>(dst + c0 + 32 * VEC * k, v[k]);
+      for (int j = 0; j < VEC; ++j) v[k].v[j] *= scale;
+      store_vals<VEC>(dst + 32 * VEC * k, v[k]);
     }
   }
 }
@@ -203,11 +207,11 @@ __device__ __forceinline__ void scale_lane(Lane<VEC>& s, float scale, const Lane
 // run that crosses from one half warp to the next is finished by the one where it begins, from the sums that the others leave
 // in shared memory.  Blocks behind those clear the rest of the layer, around the rows of the worker's tokens.
 // 8 workers' 700 tokens of 650 columns are added to 33278 rows in 13 us (a chain of launch, tokens, sort and three batches of
-// loads on 88 of the 148 SMs; 5 us of it are its 32 MB), written with all zeros in 112 us (692 MB: HBM).  This way / the long way below, accumulating: 64 tokens 5 /
-// 13 us, 256 8 / 19, 1024 15 / 27, 2048 32 / 46 us.
+// loads on 88 of the 148 SMs; 5 us of it are its 32 MB), written with all zeros in 112 us (692 MB: HBM).  This way / the long
+// way below, accumulating: 64 tokens 5 / 13 us, 256 8 / 19, 1024 15 / 27, 2048 32 / 46 us.
 constexpr int kSmallMost = 2048, kSmallCols = 64, kSmallPiece = 32768;
-constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21;  // a word holds row and position; tables of as many rows, or
-constexpr int kSmallWide = 1 << 20;                       // of more columns (32-bit offsets), take the long way
+// (a word holds row and position; tables of as many rows, or of more columns -- 32-bit offsets --, take the long way)
+constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21, kSmallWide = 1 << 20;
 
 // Ascending order of the block's words by a bitonic network over the first count2 (a power of two) of them; thread t holds
 // words t + r * THREADS.  Partners in a warp trade by shuffles, others through shared memory (two buffers in turn, so one
@@ -381,9 +385,9 @@ embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy
 }
 
 // ---- more tokens: sort, sums by chunks, joins -------------------------------------------------------------------------
-// A stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.  Its launches clear
-// the pieces, whole: leaving out the rows that the sums write (a third of them for 16384 tokens of 33278 rows) and clearing
-// beside the sums instead was slower, 211 us against 185 us for 8 workers, as the sort's launches then waited alone.
+// A stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.  Its launches clear the pieces, whole:
+// leaving out the rows that the sums write (a third of them for 16384 tokens of 33278 rows) and clearing beside the sums
+// instead was slower, 211 us against 185 us for 8 workers, as the sort's launches then waited alone.
 constexpr int kZeroPiece = 16384;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 
@@ -418,8 +422,7 @@ embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __res
 }
 
 __global__ void __launch_bounds__(kSortThreads)
-embedding_hist_kernel(const unsigned* __restrict__ keys, EmbArgs a, int shift, unsigned* __restrict__ hist, int n_tiles,
-                      EmbZero z) {
+embedding_hist_kernel(const unsigned* keys, EmbArgs a, int shift, unsigned* hist, int n_tiles, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
     zero_piece<kZeroPiece>(z, a);
@@ -443,7 +446,7 @@ embedding_hist_kernel(const unsigned* __restrict__ keys, EmbArgs a, int shift, u
 // quicker summed by every block of the scatter pass (8 x 16384 tokens accumulated: 125 us with this launch, 121 us without).
 constexpr int kScanTiles = 64;
 __global__ void __launch_bounds__(1024)
-embedding_scan_kernel(unsigned* __restrict__ hist, int n_tiles, EmbArgs a, EmbZero z) {
+embedding_scan_kernel(unsigned* hist, int n_tiles, EmbArgs a, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
     zero_piece<kZeroPiece>(z, a);
@@ -483,9 +486,8 @@ embedding_scan_kernel(unsigned* __restrict__ hist, int n_tiles, EmbArgs a, EmbZe
 // digit rank themselves by lane, the warp's running counts give the rank among its earlier ones.
 template <bool SCANNED>
 __global__ void __launch_bounds__(kSortThreads)
-embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ pos, EmbArgs a, int shift,
-                         const unsigned* __restrict__ hist, int n_tiles, unsigned* __restrict__ keys_out,
-                         unsigned* __restrict__ pos_out, EmbZero z) {
+embedding_scatter_kernel(const unsigned* keys, const unsigned* pos, EmbArgs a, int shift, const unsigned* hist, int n_tiles,
+                         unsigned* keys_out, unsigned* pos_out, EmbZero z) {
   let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
     zero_piece<kZeroPiece>(z, a);
@@ -564,7 +566,7 @@ embedding_scatter_kernel(const unsigned* __restrict__ keys, const unsigned* __re
 // one warp to the next is finished by the warp where it begins, from the sums that the others leave in shared memory.  The
 // loads of a batch of entries go out together, with accumulation (ACC) those of the rows that are added to among them.  What
 // steers the sums is the same for a whole warp: masks of the entries there are and of those that end a run.
-// 8 x 16384 tokens of 650 columns in bf16 take 63 us, 403 MB to L2 at 6.4 TB/s; 60 % of the cycles issue.
+// 8 x 16384 tokens of 650 columns in bf16 take 63 us, 403 MB to and from L2 at 6.4 TB/s; half of the cycles issue.
 constexpr int kChunk = 128, kFan = 128;
 constexpr unsigned kNoKey = 0xffffffffu;
 struct EmbLevel {
@@ -578,7 +580,7 @@ struct EmbLevel {
 // In: the values' type at the first level (FIRST); float above.
 template <typename In, int VEC, bool FIRST, bool ACC>
 __global__ void __launch_bounds__(256, ACC ? (sizeof(In) == 2 ? 3 : 2) : (sizeof(In) == 2 ? 4 : 3))
-embedding_sum_kernel(const In* __restrict__ in, const EmbLevel l, const EmbArgs a, int groups, float scale, float* grads) {
+embedding_sum_kernel(const In* in, const EmbLevel l, const EmbArgs a, int groups, float scale, float* grads) {
   constexpr int kPart = FIRST ? kChunk / 8 : 2 * kFan / 8;  // entries per warp
   __shared__ unsigned skey[8 * kPart + 2], smask[8], sends[8];
   __shared__ __align__(16) float shead[8][128];  // read and written four columns at a time
