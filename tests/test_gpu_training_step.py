@@ -182,3 +182,78 @@ def test_unknown_optimisers_are_refused():
         pipeline.AccordionStep(table, 1, ("powersgd", "topk"), optimizer={"kind": "adamw", "params": x, "lr": 0.1})
     with pytest.raises(ValueError):
         pipeline.TokenEmbedding(binding.Context(table, 1), "no such layer", 4)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_large_clipped_step_replayed_as_a_graph(bits):
+    """A table of more blocks than fit the GPU at once: norms, factor, coefficients and update, each launched behind the one
+    before, give the same bits called one by one, in a captured graph, and with a synchronisation after every call."""
+    table = wl.make_table(wl.shapes_vgg19bn(10))
+    ctx = binding.Context(table, 1)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    mask = torch.zeros(table.stride, device="cuda")
+    for _, sl in table.slices():
+        mask[sl] = 1.0
+    x0 = torch.randn(table.stride, generator=g, device="cuda") * mask
+    ds = [torch.randn(table.stride, generator=g, device="cuda") * mask for _ in range(3)]
+    d = torch.empty_like(x0)
+
+    def state(opt):
+        s = [opt.m, opt.v] if bits == 32 else [t.view(torch.uint8) for t in (opt.m_code, opt.r_code, opt.m_scale, opt.r_scale)]
+        return [opt.params, opt.step_count, opt.factor, opt.norm] + s
+
+    runs = []
+    for how in ("calls", "graph", "waits"):
+        opt = pipeline.AdamW(ctx, x0.clone(), 1e-3, bits=bits, max_norm=1.0, seed=2)
+        if how == "graph":
+            d.copy_(ds[0])
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                launches = opt.step(d)
+            assert launches == 5
+        for src in ds:
+            d.copy_(src)
+            if how == "graph":
+                graph.replay()
+            elif how == "calls":
+                opt.step(d)
+            else:
+                torch.cuda.synchronize()
+                ctx.acc_layer_norms(d, 1, opt.norm2)
+                torch.cuda.synchronize()
+                ctx.acc_clip_factor(opt.norm2, 1.0, opt.factor, opt.norm)
+                torch.cuda.synchronize()
+                opt.max_norm = None
+                f = opt.factor.clone()
+                if bits == 32:
+                    ctx.acc_adamw(d, opt.params, opt.m, opt.v, opt.step_count, opt.hyper, f)
+                else:
+                    ctx.acc_adamw_8bit(d, opt.params, opt.m_code, opt.r_code, opt.m_scale, opt.r_scale, opt.step_count,
+                                       opt.hyper, 2, f)
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        runs.append([t.clone() for t in state(opt)])
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+    assert int(runs[0][1]) == 3 and 0 < float(runs[0][2]) < 1
+
+
+def test_embedding_calls_back_to_back_share_nothing_but_order():
+    """Long and short calls on the same gradients, workspace and stream without a wait between them: the second begins when
+    the first is complete (their kernels may start early behind one another, calls may not)."""
+    table, W = _lm(3001, 24), 2
+    ctx = binding.Context(table, W)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    sets = [(_tokens(W, n, 3001, n), torch.randn(W, n, 24, generator=g, device="cuda")) for n in (9000, 40, 2500, 700)]
+    ws = ctx.new_embedding_workspace(0, 9000)
+    want = torch.zeros(W, table.stride, device="cuda")
+    got = want.clone()
+    for k, (tokens, dy) in enumerate(sets):
+        ctx.acc_embedding_grad(0, tokens, dy, want, accumulate=k > 0, workspace=ws)
+        torch.cuda.synchronize()
+    for _ in range(5):
+        for k, (tokens, dy) in enumerate(sets):
+            ctx.acc_embedding_grad(0, tokens, dy, got, accumulate=k > 0, workspace=ws)
+        out = got.clone()
+        assert torch.equal(out, want)
