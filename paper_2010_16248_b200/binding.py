@@ -294,7 +294,7 @@ class Context:
         """Checks and marshals the tensor arguments, then calls entry point ``name`` on this context."""
         args = _marshal(self.device, *items)
         index, entry = self.device.index, getattr(_lib, name)
-        if index is None or index == torch.cuda.current_device():
+        if index is None or index == torch._C._cuda_getDevice():
             st = entry(self._h, *args, _stream(stream, index))
         else:
             with torch.cuda.device(index):  # kernels launch on the current device
@@ -406,24 +406,22 @@ class Context:
                    self._f(out, self.stride, "out"), self._f(delta, self.stride, "delta"),
                    *self._tail(params, mom, hyper), stream=stream)
 
-    def _adamw_args(self, d, params, states, step, hyper, grad_scale, params_bf16):
-        return (self._f(d, self.stride, "d"), self._f(params, self.stride, "params"), *states,
-                _Arg(step, torch.int64, 1, "step"), self._d(hyper, 5, "hyper"), self._f(grad_scale, 1, "grad_scale"),
-                _Arg(params_bf16, torch.bfloat16, self.stride, "params_bf16"))
-
+    # (tuples as _Arg makes them, written out: a call of few microseconds is made of such things)
     def acc_adamw(self, d, params, m, v, step, hyper, grad_scale=None, params_bf16=None, flags=0, stream=None):
-        self._call("acc_adamw", *self._adamw_args(d, params, (self._f(m, self.stride, "m"), self._f(v, self.stride, "v")),
-                                                  step, hyper, grad_scale, params_bf16), int(flags), stream=stream)
+        n, f32 = self.stride, torch.float32
+        self._call("acc_adamw", (d, f32, n, "d"), (params, f32, n, "params"), (m, f32, n, "m"), (v, f32, n, "v"),
+                   (step, torch.int64, 1, "step"), (hyper, torch.float64, 5, "hyper"), (grad_scale, f32, 1, "grad_scale"),
+                   (params_bf16, torch.bfloat16, n, "params_bf16"), int(flags), stream=stream)
 
     def acc_adamw_8bit(self, d, params, m_code, r_code, m_scale, r_scale, step, hyper, seed=0, grad_scale=None,
                        params_bf16=None, flags=0, stream=None):
         """The states are ``torch.float8_e4m3fn`` codes and ``torch.float8_e8m0fnu`` scales (``new_adamw_8bit``)."""
-        states = (_Arg(m_code, torch.float8_e4m3fn, self.stride, "m_code"),
-                  _Arg(r_code, torch.float8_e4m3fn, self.stride, "r_code"),
-                  _Arg(m_scale, torch.float8_e8m0fnu, self.adamw_blocks, "m_scale"),
-                  _Arg(r_scale, torch.float8_e8m0fnu, self.adamw_blocks, "r_scale"))
-        self._call("acc_adamw_8bit", *self._adamw_args(d, params, states, step, hyper, grad_scale, params_bf16),
-                   int(seed) & 0xFFFFFFFF, int(flags), stream=stream)
+        n, blocks, f32 = self.stride, self.adamw_blocks, torch.float32
+        e4m3, e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+        self._call("acc_adamw_8bit", (d, f32, n, "d"), (params, f32, n, "params"), (m_code, e4m3, n, "m_code"),
+                   (r_code, e4m3, n, "r_code"), (m_scale, e8m0, blocks, "m_scale"), (r_scale, e8m0, blocks, "r_scale"),
+                   (step, torch.int64, 1, "step"), (hyper, torch.float64, 5, "hyper"), (grad_scale, f32, 1, "grad_scale"),
+                   (params_bf16, torch.bfloat16, n, "params_bf16"), int(seed) & 0xFFFFFFFF, int(flags), stream=stream)
 
     def acc_clip_factor(self, norm2_layers, max_norm, factor, norm=None, stream=None):
         self._call("acc_clip_factor", self._d(norm2_layers, self.n_layers, "norm2_layers"), float(max_norm),
@@ -456,9 +454,8 @@ class Context:
         number: ``tokens`` of any shape (int32 / int64), ``out`` its shape times the layer's columns (float32 /
         bfloat16)."""
         layer, n, tt, ot = self._embedding(layer, tokens, out, "out")
-        self._call("acc_embedding_lookup", layer, self._f(params, self.stride, "params"),
-                   _Arg(tokens, tokens.dtype, n, "tokens"), tt, n, float(scale), _Arg(out, out.dtype, out.numel(), "out"),
-                   ot, stream=stream)
+        self._call("acc_embedding_lookup", layer, (params, torch.float32, self.stride, "params"),
+                   (tokens, tokens.dtype, n, "tokens"), tt, n, float(scale), (out, out.dtype, 0, "out"), ot, stream=stream)
 
     def acc_embedding_grad(self, layer, tokens, dy, grads, scale=1.0, accumulate=False, workspace=None, stream=None):
         """Gradient of the lookup into layer ``layer`` of ``grads`` ``[W, stride]``: ``tokens`` ``[W, n]``, ``dy``
@@ -468,9 +465,9 @@ class Context:
             raise ValueError(f"tokens: expected [{self.n_workers}, n]")
         n = total // self.n_workers
         nbytes = 0 if workspace is None else workspace.numel()
-        self._call("acc_embedding_grad", layer, _Arg(tokens, tokens.dtype, total, "tokens"), tt, n, float(scale),
-                   _Arg(dy, dy.dtype, dy.numel(), "dy"), vt, self._f(grads, self._wn, "grads"), int(bool(accumulate)),
-                   _Arg(workspace, torch.uint8, 0, "workspace"), nbytes, stream=stream)
+        self._call("acc_embedding_grad", layer, (tokens, tokens.dtype, total, "tokens"), tt, n, float(scale),
+                   (dy, dy.dtype, 0, "dy"), vt, (grads, torch.float32, self.n_workers * self.stride, "grads"),
+                   1 if accumulate else 0, (workspace, torch.uint8, 0, "workspace"), nbytes, stream=stream)
 
     def acc_batch_accumulate(self, grads, acc, delta=None, first=False, stream=None):
         self._call("acc_batch_accumulate", self._f(grads, self._wn, "grads"), self._f(acc, self._wn, "acc"),
