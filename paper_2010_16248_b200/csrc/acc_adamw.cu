@@ -125,6 +125,13 @@ __global__ void adamw_coef_kernel(AdamCoef* c, long long* step, const double* hy
   }
 }
 
+// ONE waits for the work ahead of the call itself; otherwise the coefficients' kernel has, before this one could begin.
+template <bool ONE>
+__device__ __forceinline__ void adam_enter() {
+  if (ONE) await_previous();
+  let_next_start();
+}
+
 // The block's coefficients, from `pre` or worked out here; false where nothing is to change.
 template <bool ONE>
 __device__ __forceinline__ bool adam_begin(AdamCoef& c, AdamCoef* sc, const AdamCoef* pre, const long long* step,
@@ -168,10 +175,11 @@ __device__ __forceinline__ AdamUnit adam_unit(const FlatTile* __restrict__ tiles
 // 6.6 TB/s; 234 us with a block per tile of 8192 elements and a loop over it, 252 us as persistent blocks).
 template <bool ONE>
 __global__ void __launch_bounds__(256)
-adamw_kernel(const FlatTile* __restrict__ tiles, const float* __restrict__ d, float* params, float* ms, float* vs,
+adamw_kernel(const FlatTile* __restrict__ tiles, const float* d, float* params, float* ms, float* vs,
              const AdamCoef* pre, long long* step, const double* hyper, const float* factor,
              unsigned short* low, int flags, unsigned* ticket) {
   __shared__ AdamCoef sc;
+  adam_enter<ONE>();
   const int lane = threadIdx.x & 31;
   const AdamUnit u = adam_unit(tiles, flags);
   float4 gs[2], xs[2], mv[2], vv[2];
@@ -377,6 +385,7 @@ adamw_8bit_kernel(const FlatTile* __restrict__ tiles, const Adam8Args p, const A
                   const double* hyper, const float* factor, unsigned seed, int flags,
                   unsigned* ticket) {
   __shared__ AdamCoef sc;
+  adam_enter<ONE>();
   const int lane = threadIdx.x & 31;
   const AdamUnit u = adam_unit(tiles, flags);
   Adam8Regs q;
@@ -419,8 +428,7 @@ static cudaError_t adam_launch(acc_ctx* ctx, int phase, int occupancy, void (*ke
   const bool one = grid <= (unsigned)(occupancy * ctx->sm_count);
   if (one) {
     PhaseTimer pt(ctx, phase, s);
-    kernel_one<<<grid, 256, 0, s>>>(args...);
-    return cudaGetLastError();
+    return launch_early(kernel_one, grid, 256, s, args...);
   }
   cudaError_t e;
   {

@@ -54,12 +54,12 @@ __global__ void __launch_bounds__(256) ef_kernel(const DevLayer* __restrict__ la
 // One block per (tile, buffer): fp64 sum of squares of the tile, reduced in a fixed order.
 template <bool MINUS>
 __global__ void __launch_bounds__(256) norm_partial_kernel(const FlatTile* __restrict__ tiles,
-                                                           const float* __restrict__ buf, long long stride,
-                                                           const float* __restrict__ minus,
-                                                           double* __restrict__ part, int n_tiles) {
+                                                           const float* buf, long long stride, const float* minus,
+                                                           double* part, int n_tiles) {
   __shared__ double sm[8];
-  let_next_start();
   const FlatTile t = tiles[blockIdx.x];
+  await_previous();
+  let_next_start();
   const int b = blockIdx.y;
   const float* x = buf + (long long)b * stride + t.base;
   const float* y = minus + t.base;  // MINUS: norms of (buf - minus), one buffer only
@@ -221,10 +221,9 @@ cudaError_t launch_layer_norms(acc_ctx* ctx, const float* buf, long long stride,
   {
     PhaseTimer pt(ctx, PH_NORM_PARTIAL, s);
     const dim3 grid((unsigned)nt, (unsigned)n_bufs);
-    if (minus != nullptr)
-      norm_partial_kernel<true><<<grid, 256, 0, s>>>(ctx->d_flat_tiles, buf, stride, minus, ctx->d_norm_part, nt);
-    else
-      norm_partial_kernel<false><<<grid, 256, 0, s>>>(ctx->d_flat_tiles, buf, stride, nullptr, ctx->d_norm_part, nt);
+    const cudaError_t e = launch_early(minus != nullptr ? norm_partial_kernel<true> : norm_partial_kernel<false>, grid, 256, s,
+                                       (const FlatTile*)ctx->d_flat_tiles, buf, stride, minus, ctx->d_norm_part, nt);
+    if (e != cudaSuccess) return e;
   }
   {
     PhaseTimer pt(ctx, PH_NORM_FINAL, s);

@@ -69,8 +69,10 @@ __device__ __forceinline__ unsigned token_row(long long tok, int rows, int* stat
 // columns to bf16: 45 us (49 us with four loads at a time; 64 us with vectors of four columns, realigned by shuffles).
 template <typename Tok, typename Out, int VEC>
 __global__ void __launch_bounds__(256)
-embedding_lookup_kernel(const float* __restrict__ table, int rows, int cols, const Tok* __restrict__ tokens, long long n,
-                        float scale, Out* __restrict__ out, int* status) {
+embedding_lookup_kernel(const float* table, int rows, int cols, const Tok* tokens, long long n, float scale, Out* out,
+                        int* status) {
+  await_previous();
+  let_next_start();
   const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (i >= n) return;
   const int lane = threadIdx.x & 31;
@@ -265,13 +267,15 @@ __device__ __forceinline__ void sort_words(unsigned (&x)[E], int count2, unsigne
 
 template <typename Tok, typename In, int VEC, bool ACC>
 __global__ void __launch_bounds__(ACC ? 1024 : 512, ACC ? 1 : 2)
-embedding_small_kernel(const Tok* __restrict__ tokens, const In* __restrict__ dy, const EmbArgs a, int groups, float scale,
-                       float* grads, int* status, const EmbZero z) {
+embedding_small_kernel(const Tok* tokens, const In* dy, const EmbArgs a, int groups, float scale, float* grads, int* status,
+                       const EmbZero z) {
   constexpr int kThreads = ACC ? 1024 : 512, kParts = kThreads / 16, kVecs = 4 / VEC, kMost = kSmallMost / kThreads;
   __shared__ unsigned buf[2][kSmallMost];
   unsigned* entry = buf[0];  // row above position, sorted; kNoEntry: a token without a row
   __shared__ __align__(16) float shead[kParts][kSmallCols];
   constexpr unsigned kNoEntry = 0xffffffffu, kPosMask = (1u << kSmallPosBits) - 1u;
+  await_previous();
+  let_next_start();
   if (!ACC && (int)blockIdx.x >= z.first_block) {
     zero_piece_around<kSmallPiece>(z, a, buf[0], [&](int w, unsigned* taken, unsigned row0, unsigned row1) {
       const Tok* tok = tokens + (long long)w * a.n;
@@ -398,9 +402,10 @@ __device__ __forceinline__ long long sort_hist_at(int w, int digit, int tile, in
 // First pass: rows from tokens, positions in order, and the first digit's histogram of every tile.
 template <typename Tok>
 __global__ void __launch_bounds__(kSortThreads)
-embedding_keys_kernel(const Tok* __restrict__ tokens, EmbArgs a, unsigned* __restrict__ keys, unsigned* __restrict__ pos,
-                      unsigned* __restrict__ hist, int n_tiles, int* status, EmbZero z) {
-  let_next_start();
+embedding_keys_kernel(const Tok* tokens, EmbArgs a, unsigned* keys, unsigned* pos, unsigned* hist, int n_tiles, int* status,
+                      EmbZero z) {
+  await_previous();
+  let_next_start();  // (only now: blocks of the launches behind clear pieces without a wait of their own)
   if ((int)blockIdx.x >= z.first_block) {
     zero_piece<kZeroPiece>(z, a);
     return;
@@ -788,49 +793,34 @@ size_t embedding_workspace(const acc_ctx* ctx, int layer, long long n) {
   return emb_plan(ctx->cfg.n_workers, L.rows, L.cols, n).total;
 }
 
-template <typename Tok, typename Out, int VEC>
-static void lookup(const DevLayer& L, const float* params, const void* tokens, long long n, float scale, void* out,
-                   int* status, cudaStream_t s) {
-  embedding_lookup_kernel<Tok, Out, VEC><<<(unsigned)((n + 7) / 8), 256, 0, s>>>(
-      params + L.offset, L.rows, L.cols, static_cast<const Tok*>(tokens), n, scale, static_cast<Out*>(out), status);
-}
-
 cudaError_t launch_embedding_lookup(acc_ctx* ctx, int layer, const float* params, const void* tokens, bool tok64,
                                     long long n, float scale, void* out, bool bf16, cudaStream_t s) {
   const DevLayer& L = ctx->plan.layers[layer];
-  {
-    PhaseTimer pt(ctx, PH_EMB_LOOKUP, s);
-    auto go = [&](auto tok, auto o) {
-      using Tok = decltype(tok);
-      using Out = decltype(o);
-      if (L.vec == 4) lookup<Tok, Out, 4>(L, params, tokens, n, scale, out, ctx->d_status, s);
-      else if (L.vec == 2) lookup<Tok, Out, 2>(L, params, tokens, n, scale, out, ctx->d_status, s);
-      else lookup<Tok, Out, 1>(L, params, tokens, n, scale, out, ctx->d_status, s);
-    };
-    if (tok64) bf16 ? go((long long)0, __nv_bfloat16()) : go((long long)0, 0.f);
-    else bf16 ? go(0, __nv_bfloat16()) : go(0, 0.f);
-  }
-  return cudaGetLastError();
+  PhaseTimer pt(ctx, PH_EMB_LOOKUP, s);
+  auto go = [&](auto tok, auto o) {
+    using Tok = decltype(tok);
+    using Out = decltype(o);
+    auto* kernel = L.vec == 4   ? embedding_lookup_kernel<Tok, Out, 4>
+                   : L.vec == 2 ? embedding_lookup_kernel<Tok, Out, 2>
+                                : embedding_lookup_kernel<Tok, Out, 1>;
+    return launch_early(kernel, (unsigned)((n + 7) / 8), 256, s, params + L.offset, L.rows, L.cols,
+                        static_cast<const Tok*>(tokens), n, scale, static_cast<Out*>(out), ctx->d_status);
+  };
+  if (tok64) return bf16 ? go((long long)0, __nv_bfloat16()) : go((long long)0, 0.f);
+  return bf16 ? go(0, __nv_bfloat16()) : go(0, 0.f);
 }
 
-// The kernels of one gradient call, in order: the first starts behind everything before the call, the others may start early.
+// The kernels of one gradient call, in order.
 struct EmbLaunch {
   acc_ctx* ctx;
   cudaStream_t s;
-  bool first = true;
   cudaError_t err = cudaSuccess;
 
   template <typename... Params, typename... Args>
   void operator()(int phase, void (*kernel)(Params...), long long blocks, int threads, Args... args) {
     if (blocks == 0 || err != cudaSuccess) return;
     PhaseTimer pt(ctx, phase, s);
-    if (first) {
-      kernel<<<(unsigned)blocks, threads, 0, s>>>(args...);
-      err = cudaGetLastError();
-    } else {
-      err = launch_early(kernel, (unsigned)blocks, threads, s, args...);
-    }
-    first = false;
+    err = launch_early(kernel, (unsigned)blocks, threads, s, args...);
   }
 };
 

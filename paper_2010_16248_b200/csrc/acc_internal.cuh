@@ -233,8 +233,9 @@ struct PhaseTimer {
 // Programmatic dependent launch.  A kernel that launch_early() starts may begin while the one before it on the stream still
 // runs: it calls await_previous(), which returns when that one is complete and its writes are visible, before it touches
 // anything that work ahead of it writes (and takes no const __restrict__ pointer to such data: loads through one count as
-// constant for the kernel's whole life and may move ahead of the wait); let_next_start() allows the next such kernel to begin.  A kernel launched in the
-// ordinary way waits for all of them.
+// constant for the kernel's whole life and may move ahead of the wait); let_next_start() allows the next such kernel to
+// begin.  A kernel launched in the ordinary way waits for all of them.  A kernel without let_next_start() (a caller's own,
+// say) allows the next to begin when it is complete.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... Params, typename... Args>

@@ -240,8 +240,8 @@ def test_a_large_clipped_step_replayed_as_a_graph(bits):
 
 
 def test_embedding_calls_back_to_back_share_nothing_but_order():
-    """Long and short calls on the same gradients, workspace and stream without a wait between them: the second begins when
-    the first is complete (their kernels may start early behind one another, calls may not)."""
+    """Long and short calls on the same gradients, workspace and stream without a wait between them: the second
+    touches nothing before the first is complete, though its kernels may be launched earlier."""
     table, W = _lm(3001, 24), 2
     ctx = binding.Context(table, W)
     g = torch.Generator(device="cuda").manual_seed(8)
@@ -257,3 +257,77 @@ def test_embedding_calls_back_to_back_share_nothing_but_order():
             ctx.acc_embedding_grad(0, tokens, dy, got, accumulate=k > 0, workspace=ws)
         out = got.clone()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("n", [40, 2500])
+def test_calls_behind_copies_clears_and_other_streams(n):
+    """Every call of a run, captured once and replayed, first behind a copy or a clear and behind torch's kernels that write
+    its inputs, and with calls of two streams that meet: the bits of the same calls with a wait after each of them."""
+    table, W, rows, cols = _lm(3001, 24), 2, 3001, 24
+    ctx = [binding.Context(table, W) for _ in range(2)]  # (a context's workspace serves one stream at a time)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    srcs = [(_tokens(W, n, rows, 30 + k), torch.randn(W, n, cols, generator=g, device="cuda")) for k in range(4)]
+    tokens, dy = torch.empty_like(srcs[0][0]), torch.empty_like(srcs[0][1])
+    x0 = torch.randn(table.stride, generator=g, device="cuda")
+    ws = ctx[0].new_embedding_workspace(0, n)
+
+    def state():
+        z = lambda *shape: torch.zeros(*shape, device="cuda")
+        return {"x": x0.clone(), "y": z(W, n, cols), "z": z(W, n, cols), "g": z(W, table.stride), "d": z(table.stride),
+                "n2": torch.zeros(table.n_layers, dtype=torch.float64, device="cuda"), "f": z(1),
+                "norm": torch.zeros(1, dtype=torch.float64, device="cuda")}
+
+    def run(st, opt, other, wait):
+        main = torch.cuda.current_stream()
+        ctx[0].acc_embedding_lookup(0, st["x"], tokens, st["y"], 2.0)  # (behind a copy)
+        wait()
+        st["y"].add_(dy)
+        wait()
+        st["g"].zero_()
+        wait()
+        ctx[0].acc_embedding_grad(0, tokens, st["y"], st["g"], accumulate=True, workspace=ws)
+        wait()
+        torch.mean(st["g"], 0, out=st["d"])
+        other.wait_stream(main)
+        wait()
+        with torch.cuda.stream(other):
+            ctx[1].acc_layer_norms(st["d"], 1, st["n2"])
+            ctx[1].acc_clip_factor(st["n2"], 0.5, st["f"], st["norm"])
+        ctx[0].acc_embedding_lookup(0, st["x"], tokens, st["z"], 3.0)  # (reads what the update behind it changes)
+        main.wait_stream(other)
+        wait()
+        ctx[0].acc_adamw(st["d"], st["x"], opt.m, opt.v, opt.step_count, opt.hyper, st["f"])
+        wait()
+        ctx[0].acc_embedding_lookup(0, st["x"], tokens, st["y"], 1.0)
+        ctx[0].acc_embedding_grad(0, tokens, st["y"], st["g"], workspace=ws)
+        wait()
+
+    results = []
+    for how in ("waits", "calls", "graph"):
+        st, other = state(), torch.cuda.Stream()
+        opt = pipeline.AdamW(ctx[0], st["x"], 1e-2)
+        st["x"] = opt.params
+        other.wait_stream(torch.cuda.current_stream())
+        graph = None
+        if how == "graph":
+            tokens.copy_(srcs[0][0])
+            dy.copy_(srcs[0][1])
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                run(st, opt, other, lambda: None)
+        for tok, grad in srcs:
+            dy.copy_(grad)
+            tokens.copy_(tok)
+            if graph is not None:
+                graph.replay()
+            else:
+                run(st, opt, other, torch.cuda.synchronize if how == "waits" else lambda: None)
+        torch.cuda.synchronize()
+        cover = torch.zeros(table.stride, dtype=torch.bool, device="cuda")
+        for _, sl in table.slices():
+            cover[sl] = True
+        results.append([st["x"][cover], st["g"][:, cover], st["y"], st["z"], st["n2"], st["f"], st["norm"], opt.step_count])
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+    assert int(results[0][-1]) == 4 and ctx[0].acc_device_status() == 0
