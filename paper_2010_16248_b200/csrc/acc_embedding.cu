@@ -405,7 +405,10 @@ __global__ void __launch_bounds__(kSortThreads)
 embedding_keys_kernel(const Tok* tokens, EmbArgs a, unsigned* keys, unsigned* pos, unsigned* hist, int n_tiles, int* status,
                       EmbZero z) {
   await_previous();
-  let_next_start();  // (only now: blocks of the launches behind clear pieces without a wait of their own)
+  // Only now: blocks of the launches behind clear pieces without a wait of their own.  Those launches' sorting blocks wait, so
+  // that each is complete only after the one before it, and the call's last only after all of them; a launch without any
+  // sorting block would not be, which is why an empty batch has this launch alone.
+  let_next_start();
   if ((int)blockIdx.x >= z.first_block) {
     zero_piece<kZeroPiece>(z, a);
     return;
@@ -887,8 +890,9 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
     const bool scan = p.n_tiles > kScanTiles;
     int passes = 0;
     for (int shift = 0; shift < 32 && (shift == 0 || (a.rows >> shift) != 0); shift += 8) ++passes;
-    // every launch of the sort clears its share of the pieces behind its own blocks
-    const long long share = (all + passes * (scan ? 3 : 2) - 1) / (passes * (scan ? 3 : 2));
+    // every launch of the sort clears its share of the pieces behind its own blocks; without tokens the first clears all
+    const int sharing = n == 0 ? 1 : passes * (scan ? 3 : 2);
+    const long long share = (all + sharing - 1) / sharing;
     long long from = 0;
     auto sort = [&](int phase, auto kernel, long long own, int threads, auto... args) {
       const long long mine = std::min(share, all - from);
@@ -901,6 +905,7 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
     else
       sort(PH_EMB_KEYS, embedding_keys_kernel<int>, blocks, kSortThreads, static_cast<const int*>(tokens), a, keys[0], pos[0],
            hist, p.n_tiles, ctx->d_status);
+    if (n == 0) return go.err;
     int at = 0;
     for (int pass = 0; pass < passes; ++pass, at ^= 1) {
       const int shift = 8 * pass;

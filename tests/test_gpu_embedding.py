@@ -12,7 +12,7 @@ import pytest
 import torch
 
 from oracle import training_oracle as tor
-from paper_2010_16248_b200 import binding, workloads as wl
+from paper_2010_16248_b200 import binding, pipeline, workloads as wl
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -334,3 +334,48 @@ def test_offsets_beyond_32_bits():
             got = grads[w, off:off + rows * cols].view(rows, cols).double().cpu().numpy()
             assert (np.abs(got - G) <= 1.01 * U * (np.minimum(np.maximum(K - 1, 0), 127)[:, None] * S + 2 * np.abs(G))).all()
         assert bool((grads[:, off + rows * cols:] == 3.0).all())
+
+
+@pytest.mark.parametrize("rows,cols,n", [((1 << 21) + 1, 2, 900), (1 << 21, 3, 900), (3, (1 << 20) + 4, 5)])
+def test_an_empty_batch_on_a_large_table(rows, cols, n):
+    """No tokens, on tables too large for the one launch of few tokens: one launch clears the layer behind whatever ran
+    before it, and the calls behind it (a gradient that is added, norms, clip and update) find it cleared: the bits of the
+    same calls with a wait after each, and of the gradient written at once."""
+    W = 2
+    table, ctx, layer = _ctx(rows, cols, W)
+    sl = _slice(table, layer)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    tokens = _tokens(np.random.default_rng(rows), W, n, rows, "uniform")
+    dy = torch.randn(W, n, cols, generator=g, device="cuda")
+    none, nothing = tokens[:, :0].contiguous(), dy[:, :0].contiguous()
+    ws = ctx.new_embedding_workspace(layer, n)
+    x0 = torch.randn(table.stride, generator=g, device="cuda")
+    want = torch.ones(W, table.stride, device="cuda")
+    ctx.acc_embedding_grad(layer, tokens, dy, want, scale=0.5, workspace=ws)
+    runs = []
+    for waits in (True, False, False, False):
+        wait = torch.cuda.synchronize if waits else lambda: None
+        opt = pipeline.AdamW(ctx, x0.clone(), 1e-2, max_norm=0.5)
+        grads = torch.full((W, table.stride), 1.0, device="cuda")
+        torch.cuda.synchronize()
+        ctx.acc_embedding_grad(layer, tokens, dy, grads, scale=3.0, workspace=ws)
+        wait()
+        ctx.acc_embedding_grad(layer, none, nothing, grads, workspace=ws)
+        assert ctx.last_launch_count() == 1
+        wait()
+        ctx.acc_embedding_grad(layer, tokens, dy, grads, scale=0.5, accumulate=True, workspace=ws)
+        wait()
+        opt.step(grads[0])
+        wait()
+        added = grads.clone()
+        ctx.acc_embedding_grad(layer, none, nothing, grads, workspace=ws)
+        opt.step(grads[1])
+        torch.cuda.synchronize()
+        assert torch.equal(added, want)
+        assert not bool(grads[:, sl].any()) and bool((grads[:, :sl.start] == 1.0).all()) and bool((grads[:, sl.stop:] == 1.0).all())
+        ctx.acc_embedding_grad(layer, none, nothing, grads, accumulate=True, workspace=ws)
+        assert ctx.last_launch_count() == 0
+        runs.append([opt.params, opt.m, opt.v, opt.norm, opt.step_count])
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+    assert ctx.acc_device_status() == 0
