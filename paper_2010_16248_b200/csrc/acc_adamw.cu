@@ -252,7 +252,9 @@ constexpr int kLowestM = 10, kLowestR = 73;
 // e4m3's exponent bias is 120 below fp32's, so y 2^-120 in fp32 has y's e4m3 code in its bits 20 to 26, subnormals
 // included (fp32's own subnormals begin where e4m3's do), and what rounding cuts below: adding 20 random bits there and
 // cutting rounds up with the probability that the cut bits stand for.  This is the factor 2^(127 - byte - 120), as one
-// float where that is normal; a block of larger values takes 2^-120 first (`big`).
+// float where that is normal; a block of larger values takes 2^-120 first (`big`).  Below the normal codes the product is
+// an fp32 subnormal that keeps 20 bits under a step of the grid: it is cut, not rounded (__fmul_rz), as rounding up would
+// carry some values before their random bits do.  What is cut lies below the 16 random bits and decides nothing.
 __device__ __forceinline__ float code_factor(unsigned byte, bool& big) {
   big = byte > 133u;
   return byte == 0u || byte == 255u ? 0.f : __uint_as_float((big ? 254u - byte : 134u - byte) << 23);
@@ -343,8 +345,8 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
   if (bigm || bigr) {  // (the whole warp; 255 comes here too, and leaves codes that its scale of NaN makes NaN)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (bigm) m[i] = bm == 255u ? 0.f : m[i] * 0x1p-120f;
-      if (bigr) r[i] = br == 255u ? 0.f : r[i] * 0x1p-120f;
+      if (bigm) m[i] = bm == 255u ? 0.f : __fmul_rz(m[i], 0x1p-120f);
+      if (bigr) r[i] = br == 255u ? 0.f : __fmul_rz(r[i], 0x1p-120f);
     }
   }
   if (lane == 0) { p.ms[u.block] = (unsigned char)bm; p.rs[u.block] = (unsigned char)br; }
@@ -357,10 +359,10 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const unsigned w = mix32_open(seed ^ (unsigned)k), hi = w >> 16;  // random word: its halves are w ^ hi and hi
-      const unsigned tm = __float_as_uint(m[4 * h + k] * fm) + (((w ^ hi) & 0xffffu) << 4);
+      const unsigned tm = __float_as_uint(__fmul_rz(m[4 * h + k], fm)) + (((w ^ hi) & 0xffffu) << 4);
       cm[k] = (tm & 0x80000000u) | ((tm << 4) & 0x7fffffffu);
       const float rk = r[4 * h + k];
-      const float y = rk > 0.f ? fmaxf(rk * fr, 0x1p-129f) : 0.f;  // 2^-129: code 1
+      const float y = rk > 0.f ? fmaxf(__fmul_rz(rk, fr), 0x1p-129f) : 0.f;  // 2^-129: code 1
       cr[k] = (__float_as_uint(y) + (hi << 4)) << 4;
     }
     const unsigned wm = top_bytes(cm[0], cm[1], cm[2], cm[3]), wr = top_bytes(cr[0], cr[1], cr[2], cr[3]);

@@ -489,3 +489,30 @@ def test_offsets_beyond_32_bits():
     byte, code, margin = tor.encode_block(M[:256], rnd[:256] & np.uint64(0xFFFF), tor.LOWEST_M, False)
     assert _bytes(scales[0])[0] == byte and np.mean(_np(codes[0].view(torch.uint8)[off:off + 256]) != code) < 0.02
     assert int(codes[0].view(torch.uint8)[:off].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("power", [-30, 0, 20])
+@pytest.mark.parametrize("which", ["m", "r"])
+def test_adamw_8bit_codes_next_to_a_carry(which, power):
+    """Codes below the normal ones, 2^-22 of a step under the value from which their random bits would carry them to the
+    next: rounding the scaled value to the 2^-20 of a step that are kept would carry them all.  beta1 = 1/2 and beta2 = 3/4
+    make m = g / 2 and r = |g| / 2 exact, so a gradient puts any value there."""
+    n, t, seed = 256 * 64, 8, 11
+    table = wl.make_table([("x", (n,))])
+    ctx = binding.Context(table, 1)
+    u = tor.random_words(seed, t, np.arange(n))
+    u = (u & np.uint64(0xFFFF) if which == "m" else u >> np.uint64(16)).astype(np.float64)
+    y = (1.0 + (65536.0 - u) / 65536.0 - 2.0 ** -22) / 512.0  # code 1, its random bits just short of code 2
+    y[::256] = 128.0  # a block's largest element: the scale is 2^power
+    y[3::7] *= -1.0
+    d = torch.zeros(table.stride, device="cuda")
+    exact = 2.0 * y * 2.0 ** power
+    d[:n] = torch.from_numpy(exact.astype(np.float32)).cuda()
+    assert np.array_equal(_np(d[:n]).astype(np.float64), exact)
+    state, x = ctx.new_adamw_8bit(), torch.zeros(table.stride, device="cuda")
+    ctx.acc_adamw_8bit(d, x, *state, torch.tensor([t - 1], device="cuda"), _hyper(b1=0.5, b2=0.75), seed=seed)
+    code, scale = (_bytes(state[k]) for k in ((0, 2) if which == "m" else (1, 3)))
+    assert (scale == 127 + power).all()
+    small = np.abs(y) < 1.0
+    sign = np.where((y < 0) & (which == "m"), 128, 0)
+    assert np.array_equal(code[:n][small], (1 | sign)[small])
