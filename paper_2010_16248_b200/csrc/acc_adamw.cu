@@ -346,7 +346,8 @@ __device__ __forceinline__ void adam8_unit(const Adam8Regs& q, const AdamUnit& u
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (bigm) m[i] = bm == 255u ? 0.f : __fmul_rz(m[i], 0x1p-120f);
-      if (bigr) r[i] = br == 255u ? 0.f : __fmul_rz(r[i], 0x1p-120f);
+      // (a positive r stays positive, however far below its block's largest)
+      if (bigr) r[i] = br == 255u || r[i] == 0.f ? 0.f : fmaxf(__fmul_rz(r[i], 0x1p-120f), 0x1p-149f);
     }
   }
   if (lane == 0) { p.ms[u.block] = (unsigned char)bm; p.rs[u.block] = (unsigned char)br; }

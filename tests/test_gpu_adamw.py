@@ -516,3 +516,61 @@ def test_adamw_8bit_codes_next_to_a_carry(which, power):
     small = np.abs(y) < 1.0
     sign = np.where((y < 0) & (which == "m"), 128, 0)
     assert np.array_equal(code[:n][small], (1 | sign)[small])
+
+
+def _codes_by_fp32(d, b, step0, hyper, layers, seed, f):
+    """The 8-bit states after a step, from the formulas taken operation by operation in fp32 and the codes' rounding in fp64,
+    which is exact for fp32 values."""
+    lr, b1, b2, eps, wd = hyper
+    one = np.float32
+    val, sc = tor.e4m3_values().astype(one), tor.scale_values().astype(one)
+    out = [a.copy() for a in b]
+    for k, (s, n) in enumerate(tor.block_starts(layers)):
+        sl = slice(s, s + n)
+        g = one(f) * d[sl]
+        m = (sc[b[2][k]] * one(b1)) * val[b[0][sl]] + one(1.0 - b1) * g
+        r = val[b[1][sl]]
+        v = (sc[b[3][k]] * sc[b[3][k]] * one(b2)) * (r * r) + one(1.0 - b2) * (g * g)
+        assert m.dtype == v.dtype == one
+        rnd = tor.random_words(seed, step0 + 1, np.arange(s, s + n))
+        out[2][k], out[0][sl], _ = tor.encode_block(m.astype(np.float64), rnd & np.uint64(0xFFFF), tor.LOWEST_M, False)
+        out[3][k], out[1][sl], _ = tor.encode_block(np.sqrt(v).astype(np.float64), rnd >> np.uint64(16), tor.LOWEST_R, True)
+    return out
+
+
+@pytest.mark.parametrize("clip", [None, 0.37])
+def test_adamw_8bit_codes_are_those_of_the_formulas_in_fp32(clip):
+    """Every code and scale, over blocks whose magnitudes lie 24 decades apart (those that take 2^-120 first among them) with
+    elements spread over five more."""
+    table = wl.make_table([("a", (301, 1001)), ("v", (257,)), ("b", (64, 1024))])
+    layers = H.layers_of(table)
+    ctx = binding.Context(table, 1)
+    d, x, m, v = _inputs(table, 41)
+    g = torch.Generator(device="cuda").manual_seed(42)
+    size = 10.0 ** (24.0 * torch.rand((table.stride + 255) // 256, generator=g, device="cuda") - 12.0)
+    size = size.repeat_interleave(256)[:table.stride]
+    d, m, v = d * size, m * size, v * size * size
+    state, step, hyper = _pack(table, ctx, m, v), torch.tensor([20], device="cuda"), _hyper()
+    factor = None if clip is None else torch.tensor([clip], device="cuda")
+    f = 1.0 if clip is None else float(np.float32(clip))
+    for k in range(3):
+        want = _codes_by_fp32(_np(d), [_bytes(t).copy() for t in state], 20 + k, _np(hyper), layers, 6, f)
+        ctx.acc_adamw_8bit(d, x, *state, step, hyper, seed=6, grad_scale=factor)
+        assert all(np.array_equal(_bytes(t), w) for t, w in zip(state, want))
+        d = d.roll(256)
+
+
+@pytest.mark.parametrize("top", [1.0, 1e5, 1e18])
+def test_adamw_8bit_a_positive_r_is_never_zero(top):
+    """One element far above the others of its block: their r is under the grid (and, scaled, under fp32's range), and still
+    gets the smallest code, also where the state before had one."""
+    table = wl.make_table([("x", (3 * 256 + 17,))])
+    ctx = binding.Context(table, 1)
+    d = torch.full((table.stride,), 1e-10, device="cuda")
+    d[::256] = top
+    d[7] = 0.0
+    state, x, step = ctx.new_adamw_8bit(), torch.zeros(table.stride, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    for _ in range(3):
+        ctx.acc_adamw_8bit(d, x, *state, step, _hyper(), seed=1)
+        r = _bytes(state[1])[:3 * 256 + 17]
+        assert r[7] == 0 and (np.delete(r, 7) > 0).all()
