@@ -379,3 +379,40 @@ def test_an_empty_batch_on_a_large_table(rows, cols, n):
     for other in runs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
     assert ctx.acc_device_status() == 0
+
+
+@pytest.mark.parametrize("W", [1, 3])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_many_sort_tiles_of_several_workers(W, accumulate):
+    """Sort counts summed by a kernel of their own, for every worker, written and added."""
+    _run_grad(700, 6, W, 131072 + 2049, "padded", dtype=torch.bfloat16, tok=torch.int32, scale=0.5, accumulate=accumulate)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_grad_of_more_than_three_levels(dtype, accumulate):
+    """2 * 128^3 + 300 tokens per worker: partial sums of the third level go where those of the first were.  Rows of a fraction
+    of all tokens, so that runs cross the edges of every level's chunks; the second worker's batch is padded.  All values are
+    positive: a lost or repeated partial sum would be off by far more than the bound, whose 140 additions are those of four levels."""
+    rows, cols, W, n = 7, 2, 2, 2 * 128 ** 3 + 300
+    table, ctx, layer = _ctx(rows, cols, W)
+    sl = _slice(table, layer)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    share = torch.tensor([0.1, 0.6, 0.05, 1e-5, 0.1, 0.05, 0.1], device="cuda")
+    tokens = torch.multinomial(share, W * n, replacement=True, generator=g).view(W, n)
+    tokens[1] = torch.where(torch.rand(n, generator=g, device="cuda") < 0.01, -1, tokens[1])
+    dy = (torch.rand(W, n, cols, generator=g, device="cuda") + 0.5).to(dtype)
+    grads = torch.rand(W, table.stride, generator=g, device="cuda")
+    before = grads.clone()
+    ctx.acc_embedding_grad(layer, tokens, dy, grads, scale=0.5, accumulate=accumulate, workspace=ctx.new_embedding_workspace(layer, n))
+    assert ctx.acc_device_status() == 0
+    for w in range(W):
+        live = tokens[w] >= 0
+        exact = torch.zeros(rows, cols, dtype=torch.float64, device="cuda").index_add_(0, tokens[w][live], 0.5 * dy[w][live].double())
+        want = exact + (before[w, sl].view(rows, cols).double() if accumulate else 0.0)
+        got = grads[w, sl].view(rows, cols).double()
+        # (u of every addition's result, at most the whole sum; the fp64 sums' own error is 2^-53 n of it, far less)
+        assert bool(((got - want).abs() <= 1.01 * U * (140 * exact + exact + want)).all())
+    outside = torch.ones(table.stride, dtype=torch.bool, device="cuda")
+    outside[sl] = False
+    assert torch.equal(grads[:, outside], before[:, outside])
