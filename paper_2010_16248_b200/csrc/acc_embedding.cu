@@ -923,7 +923,7 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
     if (bf16) sums(__nv_bfloat16());
     else sums(0.f);
   }
-  return go.err == cudaSuccess ? cudaGetLastError() : go.err;
+  return go.err;
 }
 
 }  // namespace acc

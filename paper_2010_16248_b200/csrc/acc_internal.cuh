@@ -250,7 +250,8 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads,
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-  return e == cudaSuccess ? cudaGetLastError() : e;
+  const cudaError_t last = cudaGetLastError();  // also takes back e, which the next call would find there otherwise
+  return e != cudaSuccess ? e : last;
 }
 
 // ---- small device helpers -------------------------------------------------------------------------

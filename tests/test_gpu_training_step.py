@@ -1,5 +1,7 @@
 """The training operators as they are used together: lookup -> embedding gradient -> compression step -> norms, clip factor
 and AdamW, called one by one and through the pipeline's classes, eager and as a replayed graph."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -331,3 +333,40 @@ def test_calls_behind_copies_clears_and_other_streams(n):
     for other in results[1:]:
         assert all(torch.equal(a, b) for a, b in zip(results[0], other))
     assert int(results[0][-1]) == 4 and ctx[0].acc_device_status() == 0
+
+
+def test_a_call_into_a_broken_capture_fails_alone():
+    """A launch that the runtime refuses (the stream's capture was invalidated by waiting for it) is an error of that call;
+    the calls behind it, on streams in order, succeed."""
+    rt = ctypes.CDLL("libcudart.so.12")
+    table, W, n = _lm(), 2, 3000
+    ctx = binding.Context(table, W)
+    d = _grads(table, W, 1)
+    opt = pipeline.AdamW(ctx, torch.zeros(table.stride, device="cuda"), 0.01)
+    opt8 = pipeline.AdamW(ctx, torch.zeros(table.stride, device="cuda"), 0.01, bits=8)
+    tokens, y = _tokens(W, n, 211, 2), torch.zeros(W, n, 26, device="cuda")
+    emb = pipeline.TokenEmbedding(ctx, "encoder.weight", n)
+    norm2 = torch.zeros(W, table.n_layers, dtype=torch.float64, device="cuda")
+    side = torch.cuda.Stream()
+    p = ctypes.c_void_p(side.cuda_stream)
+    few = (tokens[:, :40].contiguous(), y[:, :40].contiguous())
+    for call in (lambda s: ctx.acc_layer_norms(d, W, norm2, stream=s), lambda s: ctx.acc_clip_factor(opt.norm2, 1.0, opt.factor, stream=s),
+                 lambda s: opt.step(d[0], s), lambda s: opt8.step(d[0], s), lambda s: emb.lookup(d[0], tokens, y, s),
+                 lambda s: emb.backward(tokens, y, d, s), lambda s: emb.backward(*few, d, s)):
+        torch.cuda.synchronize()
+        call(None)
+        torch.cuda.synchronize()
+        assert rt.cudaStreamBeginCapture(p, 2) == 0  # (2: other threads and streams are not concerned)
+        try:
+            assert rt.cudaStreamSynchronize(p) != 0
+            with pytest.raises(binding.AccError) as e:
+                call(side)
+        finally:
+            graph = ctypes.c_void_p()
+            assert rt.cudaStreamEndCapture(p, ctypes.byref(graph)) != 0
+            rt.cudaGetLastError()
+        assert e.value.status == 4
+        call(None)
+        call(side)
+        torch.cuda.synchronize()
+    assert ctx.acc_device_status() == 0
