@@ -249,7 +249,8 @@ int acc_topk_step_sgd(acc_ctx* ctx, const float* grads, float* err, const uint8_
                       const float* hyper, void* stream);
 
 /* ---- AdamW (no counterpart in the paper, whose runs use the Nesterov update above) ------------------------------
- * The update of adaptive moments with decoupled weight decay, on every element of every layer in one launch:
+ * The update of adaptive moments with decoupled weight decay, on every element of every layer, in one launch or, for
+ * tables that do not fit the GPU at once, two:
  *   t = *step + 1;  g = f * d  with f = *grad_scale, 1 when grad_scale is NULL;
  *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
  *   x <- x - lr weight_decay x - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps);  *step <- t.
@@ -276,8 +277,9 @@ int acc_topk_step_sgd(acc_ctx* ctx, const float* grads, float* err, const uint8_
  * clips by the global norm.  max_norm >= 0 and not NaN, otherwise ACC_EINVAL.
  * Device pointers: d (read), params, m, v [worker_stride] floats; m_code, r_code [worker_stride] bytes, 16-byte aligned;
  * m_scale, r_scale [n_blocks] bytes (no alignment); params_bf16 [worker_stride] 16-bit words; norm2_layers [L] doubles;
- * factor, grad_scale one float; norm one double.  Calls on one context share its count of finished blocks: order them
- * on one stream, as everything else on it.                                                                  */
+ * factor, grad_scale one float; norm one double.  Calls on one context share its count of finished blocks and the
+ * step's coefficients: order them on one stream, as everything else on it.  params_bf16 is 16-byte aligned like every
+ * buffer of one element per parameter, so that one rule holds for all of them.                                */
 #define ACC_ADAMW_BLOCK 256
 #define ACC_ADAMW_NO_VECTOR_DECAY 1
 int acc_adamw_layout(const acc_ctx* ctx, int64_t* block0 /*[L]*/, int64_t* n_blocks);
@@ -298,14 +300,16 @@ int acc_clip_factor(acc_ctx* ctx, const double* norm2_layers, double max_norm, f
  * acc_embedding_lookup:  out[i] = scale * row tokens[i] of the layer in params, i < n, in fp32, rounded once to out_type
  *   (ACC_F32 / ACC_BF16).  params [worker_stride] floats (read), tokens [n], out [n][cols] (written).
  * acc_embedding_grad, for each of the W workers w:
- *   G_w[row] = scale * sum over i with tokens[w][i] == row of dy[w][i]   (fp32 sums in an order that depends on the tokens
- *   alone: bit-reproducible), G_w being the layer in worker w's slice of grads [W][worker_stride].  accumulate = 0: every
- *   other row of G_w becomes zero, nothing outside the layer is touched.  accumulate != 0: the sums are added to what G_w
- *   holds (weights shared with another layer, micro-batches) and rows without a token are not touched.
+ *   G_w[row] = scale * sum over i with tokens[w][i] == row of dy[w][i]   (fp32 sums in an order that depends on the
+ *   tokens, the layer's size and accumulate alone: bit-reproducible), G_w being the layer in worker w's slice of grads
+ *   [W][worker_stride].  accumulate = 0: every other row of G_w becomes zero, nothing outside the layer is touched.
+ *   accumulate != 0: the sums are added to what G_w holds (weights shared with another layer, micro-batches) and rows
+ *   without a token are not touched.
  *   tokens [W][n], dy [W][n][cols] of dy_type (read).  workspace: acc_embedding_workspace_bytes(n) bytes of DEVICE memory,
  *   256-byte aligned, caller-owned, for one call at a time; its contents before and after do not matter.
- * n = 0 is allowed (tokens, out and dy may then be NULL).  n (lookup) and W * n (gradient) are at most
- * ACC_EMBEDDING_MAX_TOKENS, otherwise ACC_EINVAL, as for a VECTOR layer or an unknown type.                    */
+ * out and dy are 16-byte aligned as a whole, whatever the columns (the rule for every float buffer above): a view that
+ * starts at some token's row may not be.  n = 0 is allowed (tokens, out and dy may then be NULL).  n (lookup) and W * n
+ * (gradient) are at most ACC_EMBEDDING_MAX_TOKENS, otherwise ACC_EINVAL, as for a VECTOR layer or an unknown type. */
 #define ACC_F32 0
 #define ACC_BF16 1
 #define ACC_I32 0

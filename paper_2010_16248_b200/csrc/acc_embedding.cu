@@ -65,8 +65,10 @@ __device__ __forceinline__ unsigned token_row(long long tok, int rows, int* stat
 }
 
 // One warp per token:  out_i = scale * row(tok_i), rounded once; zeros where there is no row.  A lane's loads of a batch of
-// vectors of VEC columns go out together.  Bound by what L2 delivers, 340 MB and 170 MB back for 8 x 16384 tokens of 650
-// columns to bf16: 45 us (49 us with four loads at a time; 64 us with vectors of four columns, realigned by shuffles).
+// vectors of VEC columns go out together.  8 x 16384 tokens of 650 columns, a tenth of them padding, to bf16: 307 MB of rows
+// read, 48 MB of them distinct, and 170 MB written in 47 us (4 us more with four loads at a time, 19 us more with vectors of four
+// columns realigned by shuffles).  No unit is full (L1 67 %, L2 53 %, DRAM 45 %): warps wait for their loads two thirds of
+// the time.  Rows far narrower than a warp's 32 vectors leave lanes idle: 131072 tokens of 8 columns take 18 us, of 64 19 us.
 template <typename Tok, typename Out, int VEC>
 __global__ void __launch_bounds__(256)
 embedding_lookup_kernel(const float* table, int rows, int cols, const Tok* tokens, long long n, float scale, Out* out,
@@ -210,7 +212,10 @@ __device__ __forceinline__ void scale_lane(Lane<VEC>& s, float scale, const Lane
 // in shared memory.  Blocks behind those clear the rest of the layer, around the rows of the worker's tokens.
 // 8 workers' 700 tokens of 650 columns are added to 33278 rows in 13 us (a chain of launch, tokens, sort and three batches of
 // loads on 88 of the 148 SMs; 5 us of it are its 32 MB), written with all zeros in 112 us (692 MB: HBM).  This way / the long
-// way below, accumulating: 64 tokens 5 / 13 us, 256 8 / 19, 1024 15 / 27, 2048 32 / 46 us.
+// way below, accumulating: 64 tokens 5 / 13 us, 256 8 / 19, 1024 15 / 27, 2048 31 / 48 us.  These were measured with 8 workers
+// of 650 columns, 88 blocks; a block's time depends on the tokens alone, so fewer workers or columns only leave SMs idle: one
+// worker of 650 columns takes 12 us for 700 tokens, 25 us for 2048 (long way: 26), of 64 columns 21 us.
+// With vectors of one or two values the kernel that adds spills 8 bytes of its 64 registers.
 constexpr int kSmallMost = 2048, kSmallCols = 64, kSmallPiece = 32768;
 // (a word holds row and position; tables of as many rows, or of more columns -- 32-bit offsets --, take the long way)
 constexpr int kSmallPosBits = 11, kSmallRows = 1 << 21, kSmallWide = 1 << 20;
@@ -390,8 +395,9 @@ embedding_small_kernel(const Tok* tokens, const In* dy, const EmbArgs a, int gro
 
 // ---- more tokens: sort, sums by chunks, joins -------------------------------------------------------------------------
 // A stable radix sort, eight bits of the row at a time, in tiles of kSortTile tokens.  Its launches clear the pieces, whole:
-// leaving out the rows that the sums write (a third of them for 16384 tokens of 33278 rows) and clearing beside the sums
-// instead was slower, 211 us against 185 us for 8 workers, as the sort's launches then waited alone.
+// leaving out the rows that the sums write (15 % of them for 16384 Zipf-distributed tokens of 33278 rows) and clearing beside
+// the sums instead was slower, 211 us against 185 us for 8 workers (with sums that took 10 us more than now), as the sort's
+// launches then waited alone.
 constexpr int kZeroPiece = 16384;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 
@@ -574,7 +580,11 @@ embedding_scatter_kernel(const unsigned* keys, const unsigned* pos, EmbArgs a, i
 // one warp to the next is finished by the warp where it begins, from the sums that the others leave in shared memory.  The
 // loads of a batch of entries go out together, with accumulation (ACC) those of the rows that are added to among them.  What
 // steers the sums is the same for a whole warp: masks of the entries there are and of those that end a run.
-// 8 x 16384 tokens of 650 columns in bf16 take 63 us, 403 MB to and from L2 at 6.4 TB/s; half of the cycles issue.
+// 8 x 16384 tokens of 650 columns in bf16, a tenth of them padding, take 61 us for 153 MB read and 102 MB written.  No unit is
+// full (DRAM 46 %, L2 28 %): a scheduler issues in 60 % of the cycles, from seven warps that wait for loads, for barriers and
+// for their own latencies in equal parts.  Chunk and batches were measured at this width; of rows of few columns most lanes are
+// idle (one worker's 131072 tokens of 8 columns: 63 us).  Rows of an odd number of columns in bf16, 16 entries of four single
+// loads each, spill 56 bytes of their 64 registers (64 bytes of 80 with accumulation).
 constexpr int kChunk = 128, kFan = 128;
 constexpr unsigned kNoKey = 0xffffffffu;
 struct EmbLevel {

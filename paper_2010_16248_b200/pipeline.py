@@ -111,7 +111,8 @@ class AccordionStep:
         PowerSGD pass).  ``optimizer``: None, or a dict ``{"params": tensor [stride], "lr": .., "momentum": 0.9,
         "weight_decay": 0.0}``: the Nesterov update (Appendix A) is then applied to ``params`` by the kernels
         that produce the averaged gradient (one compressor only).  With ``"kind": "adamw"`` the dict holds the arguments
-        of ``AdamW`` (``params``, ``lr``, ``bits``, ``max_norm``, ...), whose step follows the compressor's.
+        of ``AdamW`` (``params``, ``lr``, ``bits``, ``max_norm``, ...), whose step follows the compressor's (the engine's
+        ``adamw``; its own ``params`` and ``mom`` belong to the fused update and are then None).
         ``embedding``: None, or a dict ``{"layer": name, "tokens": [W, n], "dy": [W, n, cols], "scale": 1.0,
         "accumulate": False}`` of fixed device buffers: every step first writes (or adds) the embedding's gradient of the
         tokens into that layer of the gradients it is given."""
