@@ -11,7 +11,8 @@
  *   - the mean over workers of the compressed gradients   (update rule of Section 3)
  *
  * and, around it, what a training run with that step calls on the same buffers: the optimiser updates (Nesterov,
- * AdamW with states in 32 or 8 bits), the gradient-norm clip, the lookup and the gradient of an embedding layer.
+ * AdamW with states in 32 or 8 bits), the gradient-norm clip, the lookup and the gradient of an embedding layer, the log
+ * probabilities at a language model's head with their gradient, and linear layers' gradients from 8-bit checkpoints.
  *
  * General rules, valid for every entry point unless it says otherwise:
  *   * Pointers named in "Device pointers" below are DEVICE pointers owned by the caller; the library
@@ -51,7 +52,7 @@ extern "C" {
 #define ACC_ECUDA 4       /* a CUDA runtime call or kernel launch reported an error */
 #define ACC_ETOOBIG 5     /* size beyond the fixed capacity of acc_sumsq_static    */
 #define ACC_ETIMEOUT 6    /* device side: a bounded wait on an asynchronous copy gave up (acc_device_status) */
-#define ACC_EINDEX 7      /* device side: a token id beyond the embedding's rows (acc_device_status)          */
+#define ACC_EINDEX 7      /* device side: a token id beyond the table (acc_device_status)                      */
 
 #define ACC_MATRIX 0
 #define ACC_VECTOR 1
@@ -322,6 +323,72 @@ int acc_embedding_grad(acc_ctx* ctx, int32_t layer, const void* tokens, int32_t 
                        const void* dy, int32_t dy_type, float* grads, int32_t accumulate, void* workspace,
                        size_t workspace_bytes, void* stream);
 
+/* ---- Log probabilities of given tokens (no counterpart in the paper: the loss of its language model, at the decoder whose
+ * gradient is half of what the step compresses) --------------------------------------------------------------------
+ * Rows of logits, fp32 or bf16 (logit_type ACC_F32 / ACC_BF16), `vocab` elements each and `ld` elements apart (ld >= vocab:
+ * what lies between the rows is neither read nor written); any start that suits the type.  scale > 0 multiplies the logits
+ * (1 / temperature).  Row i, with m = max_j z_j and S = sum_j exp(scale (z_j - m)):
+ *   norm[2i] = m, norm[2i + 1] = log S;  log p_j = scale (z_j - m) - log S;  logp[i] = log p_tokens[i];
+ *   entropy[i] = -sum_j p_j log p_j (a p_j of 0 adds nothing);
+ *   top_index[i][k], top_logp[i][k], k < top: the tokens of the `top` largest logits, equal ones by rising index, and their
+ *   log p; logits of -inf are no alternatives: places left over hold -1 and -inf.
+ * All in fp32, sums of a row in an order that depends on n, vocab and the row's alignment alone (bit-reproducible).
+ * tokens as for the embedding (int32 / int64; token_type), or NULL: then logp must be NULL.  A negative token pads the batch:
+ * its row is not read, logp, entropy and norm are 0, its alternatives -1 and -inf, its gradient zeros.  A token >= vocab is
+ * treated the same way and stores ACC_EINDEX in the status word.  A row of nothing but -inf has norm {-inf, 0}, entropy 0,
+ * logp -inf and a gradient of zeros; a row that holds a NaN or +inf has NaN everywhere but in norm[2i], and index -1.
+ * Outputs may be NULL when not wanted (at least one is); top is 0 exactly when both top_ outputs are NULL, at most
+ * ACC_LOGPROBS_MAX_TOP, and may exceed vocab.
+ *
+ * acc_token_logprobs_grad:  dlogits[i][j] = scale ( g_i ([j = tokens[i]] - p_j) - h_i p_j (log p_j + entropy_i) ),
+ *   g = g_logp, h = g_entropy: the loss's derivatives by logp and entropy, of n elements each or of one that serves every row
+ *   (g_logp_count, g_entropy_count), or NULL for zeros (not both; g_logp needs tokens, g_entropy needs entropy).  norm and
+ *   entropy are the forward call's.  Computed in fp32, rounded once to out_type (ACC_F32 / ACC_BF16); rows ld_out apart.
+ *   dlogits may be logits itself (same type and ld); otherwise they must not overlap.
+ * Device pointers: logits, dlogits (element-aligned), tokens [n], logp, entropy, g_* (4-byte aligned), norm [n][2] (8-byte),
+ * top_index [n][top] int32, top_logp [n][top].  n = 0 is allowed; n <= ACC_MAX_TOKENS, otherwise ACC_EINVAL.          */
+#define ACC_LOGPROBS_MAX_TOP 32
+#define ACC_MAX_TOKENS (1 << 28)
+int acc_token_logprobs(acc_ctx* ctx, const void* logits, int32_t logit_type, int64_t n, int32_t vocab, int64_t ld,
+                       const void* tokens, int32_t token_type, float scale, float* logp, float* norm, float* entropy,
+                       int32_t top, int32_t* top_index, float* top_logp, void* stream);
+int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type, int64_t n, int32_t vocab, int64_t ld,
+                            const void* tokens, int32_t token_type, float scale, const float* norm, const float* g_logp,
+                            int64_t g_logp_count, const float* g_entropy, int64_t g_entropy_count, const float* entropy,
+                            void* dlogits, int32_t out_type, int64_t ld_out, void* stream);
+
+/* ---- Activation checkpoints in 8 bits, and linear layers' gradients from them (no counterpart in the paper) --------
+ * A checkpoint of a row of `cols` values: ceil(cols / 32) * 32 e4m3 codes (those behind the columns are zeros) and one power of
+ * two for each block of ACC_CHECKPOINT_BLOCK = 32 columns, an e8m0 byte (2^(byte - 127)), ceil(cols / 32) bytes a row.
+ * acc_checkpoint_store: x [n] rows, ld elements apart, fp32 or bf16.  A block's scale brings its largest magnitude into
+ *   [128, 256) -- not below 2^-126 --, and every value is rounded to the nearest code (ties to even): half a step is 2^-4 of
+ *   a value, or 2^-17 of the block's largest where that is more.  A block of zeros has the byte 0; one that holds a NaN or an
+ *   infinity the byte 255: it reads as NaN.  tokens: NULL, or one per row: rows of negative tokens are not read and stored as
+ *   zeros (padding then adds nothing to a gradient).
+ * acc_checkpoint_load: the values, out [n] rows, ld elements apart, in fp32 (exact) or bf16 (exact but below 2^-126).
+ * acc_linear_grad: for a MATRIX layer y = x W^T (W: rows x cols) and each of the W workers w,
+ *   G_w (+)= scale * sum_t dy[w][t]^T x[w][t]   (rows x cols, t < n tokens)
+ *   with x read from a checkpoint [W][n] and G_w the layer in worker w's slice of grads [W][worker_stride].  accumulate = 0
+ *   writes the layer, nothing outside it is touched; accumulate != 0 adds to it (micro-batches, shared weights).  dy holds
+ *   rows of rows_l elements, ld apart, workers dy_stride apart (each >= rows_l where there is more than one), fp32 or bf16.
+ *   Products are those of fp32 (fp32 values of dy count with all 24 bits), sums in fp32 on the tensor cores in an order that
+ *   depends on the sizes and types alone: bit-reproducible.  Every token counts: a padded one's dy has to be zeros (as
+ *   acc_token_logprobs_grad leaves it) and its checkpoint finite.  workspace: acc_linear_grad_workspace_bytes(layer, n)
+ *   bytes of DEVICE memory, 256-byte aligned, caller-owned, for one call at a time; contents before and after do not matter.
+ * Device pointers: x, out, dy (element-aligned), code [n][ceil(cols/32)*32] (16-byte aligned), code_scale
+ * [n][ceil(cols/32)] (no alignment), tokens [n], grads (16-byte aligned).  n = 0 is allowed; n (gradient: W * n) is at most
+ * ACC_MAX_TOKENS, otherwise ACC_EINVAL.  bf16 rows of dy that start on 16 bytes (ld and dy_stride multiples of 8) are the
+ * fast way: they are copied to the tensor cores by the copy engine, others by loads.                              */
+#define ACC_CHECKPOINT_BLOCK 32
+int acc_checkpoint_store(acc_ctx* ctx, const void* x, int32_t x_type, int64_t n, int32_t cols, int64_t ld, const void* tokens,
+                         int32_t token_type, uint8_t* code, uint8_t* code_scale, void* stream);
+int acc_checkpoint_load(acc_ctx* ctx, const uint8_t* code, const uint8_t* code_scale, int64_t n, int32_t cols, void* out,
+                        int32_t out_type, int64_t ld, void* stream);
+int acc_linear_grad_workspace_bytes(const acc_ctx* ctx, int32_t layer, int64_t n, size_t* bytes);
+int acc_linear_grad(acc_ctx* ctx, int32_t layer, const void* dy, int32_t dy_type, int64_t n, int64_t ld, int64_t dy_stride,
+                    float scale, const uint8_t* code, const uint8_t* code_scale, float* grads, int32_t accumulate,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Batch-size mode (Section 4.2: "For batch size we use the same algorithm", switching between B_low and
  * B_high at the granularity of the whole model; Section 5.1: the learning rate scales in the same ratio;
  * Appendix A: large batches are simulated by accumulating several backward passes before the exchange, and
@@ -401,7 +468,8 @@ int acc_download_out(acc_ctx* ctx, const float* out_dev, float* out_host, void* 
  * should a wait ever give up, the block stores ACC_ETIMEOUT in a status word and returns instead of
  * hanging, and the results of that call are undefined.  This call copies the status word to *status
  * (HOST pointer; 0 = no such event) and blocks until the device has finished the work queued before it.
- * The embedding calls store ACC_EINDEX there for a token id beyond the table (the first event is kept).      */
+ * The embedding and log-probability calls store ACC_EINDEX there for a token id beyond the table or vocabulary (the
+ * first event is kept).                                                                               */
 int acc_device_status(acc_ctx* ctx, int32_t* status);
 
 /* Failure-detection self-test (no counterpart in the paper).  acc_selftest_wait_timeout launches one small kernel

@@ -25,6 +25,8 @@ ACC_FLAG_SHARE_SMS = 8
 ACC_ADAMW_BLOCK = 256
 ACC_ADAMW_NO_VECTOR_DECAY = 1
 ACC_EINDEX = 7
+ACC_LOGPROBS_MAX_TOP = 32
+ACC_CHECKPOINT_BLOCK = 32
 POWERSGD, TOPK = 0, 1
 ACC_TOPK_PATH_DENSE, ACC_TOPK_PATH_LIST, ACC_TOPK_PATH_LIST_PREDICTED, ACC_TOPK_PATH_STAGED, ACC_TOPK_PATH_ZERO_FILL = range(5)
 
@@ -61,7 +63,9 @@ EXPORTS = ["acc_workspace_bytes", "acc_create", "acc_destroy", "acc_factor_layou
            "acc_topk_compress", "acc_topk_decompress", "acc_topk_flush",
            "acc_upload_grads", "acc_download_out", "acc_selftest_wait_timeout", "acc_reset_device_status",
            "acc_layer_msdr", "acc_detect_regime_lr", "acc_adamw_layout", "acc_adamw", "acc_adamw_8bit", "acc_clip_factor",
-           "acc_embedding_lookup", "acc_embedding_workspace_bytes", "acc_embedding_grad"]
+           "acc_embedding_lookup", "acc_embedding_workspace_bytes", "acc_embedding_grad",
+           "acc_token_logprobs", "acc_token_logprobs_grad", "acc_checkpoint_store", "acc_checkpoint_load",
+           "acc_linear_grad_workspace_bytes", "acc_linear_grad"]
 
 _lib = None
 
@@ -131,6 +135,12 @@ def lib() -> C.CDLL:
     L.acc_embedding_lookup.argtypes = [vp, i32, vp, vp, i32, i64, f32, vp, i32, vp]
     L.acc_embedding_workspace_bytes.argtypes = [vp, i32, i64, C.POINTER(C.c_size_t)]
     L.acc_embedding_grad.argtypes = [vp, i32, vp, i32, i64, f32, vp, i32, vp, i32, vp, C.c_size_t, vp]
+    L.acc_token_logprobs.argtypes = [vp, vp, i32, i64, i32, i64, vp, i32, f32, vp, vp, vp, i32, vp, vp, vp]
+    L.acc_token_logprobs_grad.argtypes = [vp, vp, i32, i64, i32, i64, vp, i32, f32, vp, vp, i64, vp, i64, vp, vp, i32, i64, vp]
+    L.acc_checkpoint_store.argtypes = [vp, vp, i32, i64, i32, i64, vp, i32, vp, vp, vp]
+    L.acc_checkpoint_load.argtypes = [vp, vp, vp, i64, i32, vp, i32, i64, vp]
+    L.acc_linear_grad_workspace_bytes.argtypes = [vp, i32, i64, C.POINTER(C.c_size_t)]
+    L.acc_linear_grad.argtypes = [vp, i32, vp, i32, i64, i64, i64, f32, vp, vp, vp, i32, vp, C.c_size_t, vp]
     for name in EXPORTS:
         if name not in ("acc_floats_sent", "acc_last_launch_count", "acc_strerror", "acc_profile_kernel_count",
                         "acc_profile_kernel_name"):
@@ -220,6 +230,30 @@ def _refuse(device, items):
         if device is not None and device.index is not None and t.device.index != device.index:
             raise ValueError(f"{what}: lives on {t.device}, the context on {device}")
     raise ValueError("a tensor argument of the call cannot be used")
+
+
+def _rows(t, dtypes, what, device, dims=2):
+    """Checks a tensor whose rows (its last dimension) are contiguous and may lie apart; returns its address, its type's
+    number and its shape and strides but the last."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{what}: expected a torch tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: expected one of {list(dtypes)}, got {t.dtype}")
+    if t.dim() != dims:
+        raise ValueError(f"{what}: expected {dims} dimensions, got {tuple(t.shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: expected contiguous rows")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a CUDA tensor (the library has no CPU path)")
+    if device.index is not None and t.get_device() != device.index:
+        raise ValueError(f"{what}: lives on {t.device}, the context on {device}")
+    return t.data_ptr() or None, dtypes[t.dtype], t.shape, t.stride()
+
+
+def _sized(t, numel, what):
+    """Checks the number of elements of a tensor that may be missing."""
+    if t is not None and isinstance(t, torch.Tensor) and t.numel() != numel:
+        raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
 
 
 def _stream(stream, index=None) -> Optional[int]:
@@ -469,6 +503,95 @@ class Context:
                    (dy, dy.dtype, 0, "dy"), vt, (grads, torch.float32, self.n_workers * self.stride, "grads"),
                    1 if accumulate else 0, (workspace, torch.uint8, 0, "workspace"), nbytes, stream=stream)
 
+    def _row_tokens(self, tokens, n):
+        """Token type of one token per row (None: no tokens)."""
+        if tokens is None:
+            return 0
+        if not isinstance(tokens, torch.Tensor):
+            raise ValueError("tokens: expected a torch tensor")
+        if tokens.dtype not in _TOKEN_TYPES:
+            raise ValueError(f"tokens: expected one of {list(_TOKEN_TYPES)}, got {tokens.dtype}")
+        _sized(tokens, n, "tokens")
+        return _TOKEN_TYPES[tokens.dtype]
+
+    def acc_token_logprobs(self, logits, tokens=None, logp=None, norm=None, entropy=None, top_index=None, top_logp=None,
+                           scale=1.0, stream=None):
+        """Log probabilities of ``tokens`` ``[n]`` (None: no given tokens) under the rows of ``logits`` ``[n, vocab]``
+        (float32 / bfloat16; rows may lie apart), into the given outputs: ``logp`` ``[n]``, ``norm`` ``[n, 2]``, ``entropy``
+        ``[n]``, ``top_index`` (int32) and ``top_logp`` ``[n, top]``."""
+        f32 = torch.float32
+        at, lt, (n, vocab), (ld, _) = _rows(logits, _VALUE_TYPES, "logits", self.device)
+        tt = self._row_tokens(tokens, n)
+        top = 0
+        for t, what in ((top_index, "top_index"), (top_logp, "top_logp")):
+            if t is not None:
+                if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[0] != n or (top and t.shape[1] != top):
+                    raise ValueError(f"{what}: expected a tensor [{n}, top]")
+                top = t.shape[1]
+        _sized(logp, n, "logp"), _sized(norm, 2 * n, "norm"), _sized(entropy, n, "entropy")
+        self._call("acc_token_logprobs", at, lt, n, vocab, ld, (tokens, None if tokens is None else tokens.dtype, n, "tokens"), tt, float(scale), (logp, f32, n, "logp"),
+                   (norm, f32, 2 * n, "norm"), (entropy, f32, n, "entropy"), top, (top_index, torch.int32, n * top, "top_index"),
+                   (top_logp, f32, n * top, "top_logp"), stream=stream)
+
+    def acc_token_logprobs_grad(self, logits, tokens, norm, dlogits, g_logp=None, g_entropy=None, entropy=None, scale=1.0,
+                                stream=None):
+        """Gradient of a loss with derivatives ``g_logp`` and ``g_entropy`` (``[n]``, or one element for every row) by
+        ``acc_token_logprobs``'s outputs into ``dlogits`` ``[n, vocab]`` (may be ``logits`` itself)."""
+        f32 = torch.float32
+        at, lt, (n, vocab), (ld, _) = _rows(logits, _VALUE_TYPES, "logits", self.device)
+        out, ot, shape, (ld_out, _) = _rows(dlogits, _VALUE_TYPES, "dlogits", self.device)
+        if shape != (n, vocab):
+            raise ValueError(f"dlogits: expected {(n, vocab)}, got {tuple(shape)}")
+        tt = self._row_tokens(tokens, n)
+        counts = []
+        for t, what in ((g_logp, "g_logp"), (g_entropy, "g_entropy")):
+            if t is not None and (not isinstance(t, torch.Tensor) or t.numel() not in (1, n)):
+                raise ValueError(f"{what}: expected a tensor of {n} elements, or of one")
+            counts.append(0 if t is None else t.numel())
+        _sized(norm, 2 * n, "norm"), _sized(entropy, n, "entropy")
+        self._call("acc_token_logprobs_grad", at, lt, n, vocab, ld, (tokens, None if tokens is None else tokens.dtype, n, "tokens"),
+                   tt, float(scale), (norm, f32, 2 * n, "norm"), (g_logp, f32, 0, "g_logp"), counts[0],
+                   (g_entropy, f32, 0, "g_entropy"), counts[1], (entropy, f32, n, "entropy"), out, ot, ld_out, stream=stream)
+
+    def _checkpoint(self, code, scale, n, cols):
+        """The ``_Arg`` items of a checkpoint of ``n`` rows, its size checked to the element."""
+        blocks = (cols + ACC_CHECKPOINT_BLOCK - 1) // ACC_CHECKPOINT_BLOCK
+        _sized(code, n * blocks * ACC_CHECKPOINT_BLOCK, "code"), _sized(scale, n * blocks, "scale")
+        return (code, torch.float8_e4m3fn, 0, "code"), (scale, torch.float8_e8m0fnu, 0, "scale")
+
+    def acc_checkpoint_store(self, x, code, scale, tokens=None, stream=None):
+        """``x`` ``[n, cols]`` (float32 / bfloat16; rows may lie apart) into ``code, scale`` of ``new_checkpoint(n, cols)``;
+        rows of negative ``tokens`` ``[n]`` become zeros and are not read."""
+        at, xt, (n, cols), (ld, _) = _rows(x, _VALUE_TYPES, "x", self.device)
+        tt = self._row_tokens(tokens, n)
+        c, s = self._checkpoint(code, scale, n, cols)
+        self._call("acc_checkpoint_store", at, xt, n, cols, ld, (tokens, None if tokens is None else tokens.dtype, n, "tokens"), tt,
+                   c, s, stream=stream)
+
+    def acc_checkpoint_load(self, code, scale, out, stream=None):
+        """The values of a checkpoint into ``out`` ``[n, cols]`` (float32 / bfloat16; rows may lie apart)."""
+        at, ot, (n, cols), (ld, _) = _rows(out, _VALUE_TYPES, "out", self.device)
+        c, s = self._checkpoint(code, scale, n, cols)
+        self._call("acc_checkpoint_load", c, s, n, cols, at, ot, ld, stream=stream)
+
+    def acc_linear_grad(self, layer, dy, code, scales, grads, scale=1.0, accumulate=False, workspace=None, stream=None):
+        """Weight gradient of layer ``layer`` (its index) from its output's gradient ``dy`` ``[W, n, rows]`` (float32 / bfloat16;
+        rows and workers may lie apart) and the checkpoint ``code, scales`` of its input ``[W * n, cols]``, into ``grads``
+        ``[W, stride]``; ``workspace`` from ``new_linear_grad_workspace(layer, n)``."""
+        layer = int(layer)
+        if not 0 <= layer < self.n_layers or self.q_row[layer] < 0:
+            raise ValueError(f"layer {layer}: expected the index of a MATRIX layer")
+        rows, cols = int(self.table.rows[layer]), int(self.table.cols[layer])
+        at, dt, shape, (dy_stride, ld, _) = _rows(dy, _VALUE_TYPES, "dy", self.device, dims=3)
+        n = shape[1]
+        if shape[0] != self.n_workers or shape[2] != rows:
+            raise ValueError(f"dy: expected [{self.n_workers}, n, {rows}], got {tuple(shape)}")
+        c, s = self._checkpoint(code, scales, self.n_workers * n, cols)
+        nbytes = 0 if workspace is None else workspace.numel()
+        self._call("acc_linear_grad", layer, at, dt, n, ld, dy_stride, float(scale), c, s,
+                   (grads, torch.float32, self.n_workers * self.stride, "grads"), 1 if accumulate else 0,
+                   (workspace, torch.uint8, 0, "workspace"), nbytes, stream=stream)
+
     def acc_batch_accumulate(self, grads, acc, delta=None, first=False, stream=None):
         self._call("acc_batch_accumulate", self._f(grads, self._wn, "grads"), self._f(acc, self._wn, "acc"),
                    self._f(delta, self.stride, "delta"), int(bool(first)), stream=stream)
@@ -592,6 +715,19 @@ class Context:
         nbytes = C.c_size_t(0)
         self._check(lib().acc_embedding_workspace_bytes(self._h, int(layer), int(n), C.byref(nbytes)),
                     "acc_embedding_workspace_bytes")
+        return torch.empty(int(nbytes.value), dtype=torch.uint8, device=self.device)
+
+    def new_checkpoint(self, n, cols):
+        """``code, scale`` of a checkpoint of ``n`` rows of ``cols`` values (all zeros)."""
+        blocks = (int(cols) + ACC_CHECKPOINT_BLOCK - 1) // ACC_CHECKPOINT_BLOCK
+        zeros = lambda m, dtype: torch.zeros(int(n), m, dtype=torch.uint8, device=self.device).view(dtype)  # noqa: E731
+        return zeros(blocks * ACC_CHECKPOINT_BLOCK, torch.float8_e4m3fn), zeros(blocks, torch.float8_e8m0fnu)
+
+    def new_linear_grad_workspace(self, layer, n):
+        """Scratch of ``acc_linear_grad`` for ``n`` tokens per worker; one call at a time may use it."""
+        nbytes = C.c_size_t(0)
+        self._check(lib().acc_linear_grad_workspace_bytes(self._h, int(layer), int(n), C.byref(nbytes)),
+                    "acc_linear_grad_workspace_bytes")
         return torch.empty(int(nbytes.value), dtype=torch.uint8, device=self.device)
 
     def new_topk_buffers(self):

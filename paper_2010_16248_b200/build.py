@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libacc.so")
 SOURCES = ["acc_api.cu", "acc_controller.cu", "acc_powersgd.cu", "acc_topk.cu", "acc_batch.cu", "acc_static.cu",
-           "acc_adamw.cu", "acc_embedding.cu"]
+           "acc_adamw.cu", "acc_embedding.cu", "acc_logprobs.cu", "acc_checkpoint.cu", "acc_linear.cu"]
 
 
 def _nvcc() -> str:

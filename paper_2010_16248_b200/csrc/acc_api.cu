@@ -1,5 +1,6 @@
 // C-ABI entry points: configuration checks, launch-table planning, workspace layout.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -230,6 +231,7 @@ int acc_create(const acc_config* cfg, void* workspace, size_t workspace_bytes, a
   if (e == cudaSuccess) e = prepare_powersgd();
   if (e == cudaSuccess) e = prepare_topk(ctx);
   if (e == cudaSuccess) e = prepare_adamw(ctx);
+  if (e == cudaSuccess) e = prepare_linear();
   int dev = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, dev);
@@ -567,6 +569,104 @@ int acc_embedding_grad(acc_ctx* ctx, int32_t layer, const void* tokens, int32_t 
                                       grads, accumulate != 0, workspace, static_cast<cudaStream_t>(stream)));
 }
 
+static bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+static size_t value_size(int type) { return type == ACC_BF16 ? 2 : 4; }
+static size_t token_size(int type) { return type == ACC_I64 ? 8 : 4; }
+static bool known_value(int type) { return type == ACC_F32 || type == ACC_BF16; }
+static bool known_token(int type) { return type == ACC_I32 || type == ACC_I64; }
+// Rows of `width` elements, `ld` apart, of which a call takes n.
+static bool rows_fit(int64_t n, int64_t width, int64_t ld) {
+  return n >= 0 && n <= ACC_MAX_TOKENS && width >= 1 && width <= 0x7fffffff - 16 && (n <= 1 || ld >= width);
+}
+constexpr int64_t kMostBlocks = 0x7fffffff;
+
+int acc_token_logprobs(acc_ctx* ctx, const void* logits, int32_t logit_type, int64_t n, int32_t vocab, int64_t ld,
+                       const void* tokens, int32_t token_type, float scale, float* logp, float* norm, float* entropy,
+                       int32_t top, int32_t* top_index, float* top_logp, void* stream) {
+  if (!ctx || !known_value(logit_type) || !known_token(token_type) || !rows_fit(n, vocab, ld)) return ACC_EINVAL;
+  if (!(scale > 0.f) || !std::isfinite(scale) || top < 0 || top > ACC_LOGPROBS_MAX_TOP) return ACC_EINVAL;
+  ctx->last_launches = 0;
+  if (n == 0) return ACC_OK;
+  if ((top > 0) != (top_index != nullptr || top_logp != nullptr)) return ACC_EINVAL;
+  if (!logits || (logp && !tokens) || (!logp && !norm && !entropy && top == 0)) return ACC_EINVAL;
+  if (!aligned_to(logits, value_size(logit_type)) || !aligned_to(tokens, token_size(token_type)) || !aligned_to(logp, 4) ||
+      !aligned_to(norm, 8) || !aligned_to(entropy, 4) || !aligned_to(top_index, 4) || !aligned_to(top_logp, 4))
+    return ACC_EALIGN;
+  return finish(launch_token_logprobs(ctx, logits, logit_type == ACC_BF16, n, vocab, ld, tokens, token_type == ACC_I64, scale,
+                                      logp, norm, entropy, top, top_index, top_logp, static_cast<cudaStream_t>(stream)));
+}
+
+int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type, int64_t n, int32_t vocab, int64_t ld,
+                            const void* tokens, int32_t token_type, float scale, const float* norm, const float* g_logp,
+                            int64_t g_logp_count, const float* g_entropy, int64_t g_entropy_count, const float* entropy,
+                            void* dlogits, int32_t out_type, int64_t ld_out, void* stream) {
+  if (!ctx || !known_value(logit_type) || !known_value(out_type) || !known_token(token_type) || !rows_fit(n, vocab, ld) ||
+      !rows_fit(n, vocab, ld_out))
+    return ACC_EINVAL;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return ACC_EINVAL;
+  ctx->last_launches = 0;
+  if (n == 0) return ACC_OK;
+  if (!logits || !norm || !dlogits || (!g_logp && !g_entropy) || (g_logp && !tokens) || (g_entropy && !entropy))
+    return ACC_EINVAL;
+  if ((g_logp && g_logp_count != n && g_logp_count != 1) || (g_entropy && g_entropy_count != n && g_entropy_count != 1))
+    return ACC_EINVAL;
+  // in place, or apart: the same rows under another type or stride would be overwritten before they are read
+  if (logits == dlogits && (logit_type != out_type || (n > 1 && ld != ld_out))) return ACC_EINVAL;
+  if (logprobs_grad_blocks(n, vocab) > kMostBlocks) return ACC_EINVAL;
+  if (!aligned_to(logits, value_size(logit_type)) || !aligned_to(dlogits, value_size(out_type)) ||
+      !aligned_to(tokens, token_size(token_type)) || !aligned_to(norm, 8) || !aligned_to(g_logp, 4) ||
+      !aligned_to(g_entropy, 4) || !aligned_to(entropy, 4))
+    return ACC_EALIGN;
+  return finish(launch_token_logprobs_grad(ctx, logits, logit_type == ACC_BF16, n, vocab, ld, tokens, token_type == ACC_I64,
+                                           scale, norm, g_logp, g_logp_count, g_entropy, g_entropy_count, entropy, dlogits,
+                                           out_type == ACC_BF16, ld_out, static_cast<cudaStream_t>(stream)));
+}
+
+static int checkpoint(acc_ctx* ctx, bool store, void* x, int type, int64_t n, int cols, int64_t ld, const void* tokens,
+                      int token_type, uint8_t* code, uint8_t* scale, void* stream) {
+  if (!ctx || !known_value(type) || !known_token(token_type) || !rows_fit(n, cols, ld)) return ACC_EINVAL;
+  if (n > 0 && (!x || !code || !scale)) return ACC_EINVAL;
+  if (n * ((cols + 31ll) / 32 * 4) / 512 >= kMostBlocks) return ACC_EINVAL;
+  if (!aligned_to(x, value_size(type)) || !aligned_to(tokens, token_size(token_type)) || !aligned16(code)) return ACC_EALIGN;
+  ctx->last_launches = 0;
+  if (n == 0) return ACC_OK;
+  return finish(launch_checkpoint(ctx, store, x, type == ACC_BF16, n, cols, ld, tokens, token_type == ACC_I64, code, scale,
+                                  static_cast<cudaStream_t>(stream)));
+}
+int acc_checkpoint_store(acc_ctx* ctx, const void* x, int32_t x_type, int64_t n, int32_t cols, int64_t ld, const void* tokens,
+                         int32_t token_type, uint8_t* code, uint8_t* code_scale, void* stream) {
+  return checkpoint(ctx, true, const_cast<void*>(x), x_type, n, cols, ld, tokens, token_type, code, code_scale, stream);
+}
+int acc_checkpoint_load(acc_ctx* ctx, const uint8_t* code, const uint8_t* code_scale, int64_t n, int32_t cols, void* out,
+                        int32_t out_type, int64_t ld, void* stream) {
+  return checkpoint(ctx, false, out, out_type, n, cols, ld, nullptr, ACC_I32, const_cast<uint8_t*>(code),
+                    const_cast<uint8_t*>(code_scale), stream);
+}
+
+static int check_linear(const acc_ctx* ctx, int layer, int64_t n) {
+  if (!ctx || layer < 0 || layer >= ctx->cfg.n_layers || ctx->plan.layers[layer].kind != ACC_MATRIX) return ACC_EINVAL;
+  return n < 0 || n > ACC_MAX_TOKENS || n * ctx->cfg.n_workers > ACC_MAX_TOKENS ? ACC_EINVAL : ACC_OK;
+}
+int acc_linear_grad_workspace_bytes(const acc_ctx* ctx, int32_t layer, int64_t n, size_t* bytes) {
+  if (!bytes || check_linear(ctx, layer, n) != ACC_OK) return ACC_EINVAL;
+  *bytes = linear_grad_workspace(ctx, layer, n);
+  return ACC_OK;
+}
+int acc_linear_grad(acc_ctx* ctx, int32_t layer, const void* dy, int32_t dy_type, int64_t n, int64_t ld, int64_t dy_stride,
+                    float scale, const uint8_t* code, const uint8_t* code_scale, float* grads, int32_t accumulate,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  if (check_linear(ctx, layer, n) != ACC_OK || !known_value(dy_type) || !grads) return ACC_EINVAL;
+  const int rows = ctx->plan.layers[layer].rows;
+  if (n > 0 && (!dy || !code || !code_scale || !rows_fit(n, rows, ld))) return ACC_EINVAL;
+  if (n > 0 && ctx->cfg.n_workers > 1 && dy_stride < rows) return ACC_EINVAL;
+  if (!aligned16(grads) || !aligned_to(dy, value_size(dy_type)) || !aligned16(code)) return ACC_EALIGN;
+  if (!workspace || workspace_bytes < linear_grad_workspace(ctx, layer, n)) return ACC_EWORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ACC_EALIGN;
+  ctx->last_launches = 0;
+  return finish(launch_linear_grad(ctx, layer, dy, dy_type == ACC_BF16, n, ld, dy_stride, scale, code, code_scale, grads,
+                                   accumulate != 0, workspace, static_cast<cudaStream_t>(stream)));
+}
+
 int acc_batch_accumulate(acc_ctx* ctx, const float* grads, float* acc, float* delta, int32_t first, void* stream) {
   if (!ctx || !grads || !acc) return ACC_EINVAL;
   if (!aligned16(grads) || !aligned16(acc) || !aligned16(delta)) return ACC_EALIGN;
@@ -688,7 +788,9 @@ const char* acc_profile_kernel_name(int32_t i) {
       "topk_decompress_packed_kernel", "topk_flush_kernel", "moments_partial_kernel", "moments_final_kernel",
       "adamw_coef_kernel", "adamw_kernel", "adamw_8bit_kernel", "clip_factor_kernel",
       "embedding_lookup_kernel", "embedding_small_kernel", "embedding_keys_kernel", "embedding_hist_kernel",
-      "embedding_scan_kernel", "embedding_scatter_kernel", "embedding_sum_kernel", "embedding_join_kernel"};
+      "embedding_scan_kernel", "embedding_scatter_kernel", "embedding_sum_kernel", "embedding_join_kernel",
+      "logprobs_kernel", "logprobs_grad_kernel", "checkpoint_store_kernel", "checkpoint_load_kernel",
+      "linear_grad_kernel", "linear_join_kernel"};
   return (i >= 0 && i < PH_COUNT) ? names[i] : "";
 }
 
@@ -733,7 +835,7 @@ const char* acc_strerror(int status) {
     case ACC_EWORKSPACE: return "workspace missing or too small";
     case ACC_ECUDA: return "CUDA runtime or launch error";
     case ACC_ETIMEOUT: return "a bounded device-side wait gave up (asynchronous copy did not complete)";
-    case ACC_EINDEX: return "a token id beyond the embedding's rows";
+    case ACC_EINDEX: return "a token id beyond the embedding's rows or the vocabulary";
     case ACC_ETOOBIG: return "size exceeds the capacity of the built-in scratch array (ACC_STATIC_NORM_MAX_ELEMS)";
     default: return "unknown status";
   }

@@ -74,6 +74,7 @@ enum Phase {
   PH_MOMENTS_PARTIAL, PH_MOMENTS_FINAL,
   PH_ADAMW_COEF, PH_ADAMW, PH_ADAMW_8BIT, PH_CLIP_FACTOR,
   PH_EMB_LOOKUP, PH_EMB_SMALL, PH_EMB_KEYS, PH_EMB_HIST, PH_EMB_SCAN, PH_EMB_SCATTER, PH_EMB_SUM, PH_EMB_JOIN,
+  PH_LOGPROBS, PH_LOGPROBS_GRAD, PH_CKPT_STORE, PH_CKPT_LOAD, PH_LINEAR_GRAD, PH_LINEAR_JOIN,
   PH_COUNT
 };
 
@@ -212,6 +213,24 @@ cudaError_t launch_embedding_grad(acc_ctx* ctx, int layer, const void* tokens, b
                                   const void* dy, bool bf16, float* grads, int accumulate, void* workspace,
                                   cudaStream_t s);
 
+cudaError_t launch_token_logprobs(acc_ctx* ctx, const void* logits, bool bf16, long long n, int vocab, long long ld,
+                                  const void* tokens, bool tok64, float scale, float* logp, float* norm, float* entropy,
+                                  int top, int* top_index, float* top_logp, cudaStream_t s);
+// Blocks of the gradient's launch.
+long long logprobs_grad_blocks(long long n, int vocab);
+cudaError_t launch_token_logprobs_grad(acc_ctx* ctx, const void* logits, bool bf16, long long n, int vocab, long long ld,
+                                       const void* tokens, bool tok64, float scale, const float* norm, const float* g_logp,
+                                       long long g_count, const float* g_entropy, long long h_count, const float* entropy,
+                                       void* out, bool out_bf16, long long ld_out, cudaStream_t s);
+// A checkpoint written from (store) or read into x.
+cudaError_t launch_checkpoint(acc_ctx* ctx, bool store, void* x, bool bf16, long long n, int cols, long long ld,
+                              const void* tokens, bool tok64, uint8_t* code, uint8_t* scale, cudaStream_t s);
+cudaError_t prepare_linear();
+size_t linear_grad_workspace(const acc_ctx* ctx, int layer, long long n);
+cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf16, long long n, long long ld,
+                               long long dy_stride, float scale, const uint8_t* code, const uint8_t* scales, float* grads,
+                               int accumulate, void* workspace, cudaStream_t s);
+
 // Brackets one kernel launch with CUDA events on its stream when profiling is on; counts the launch.
 struct PhaseTimer {
   acc_ctx* ctx; cudaStream_t s; ProfSlot* slot = nullptr;
@@ -239,19 +258,28 @@ struct PhaseTimer {
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... Params, typename... Args>
-cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, cudaStream_t s, Args... args) {
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+cudaError_t launch_early_as(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, int cluster, cudaStream_t s,
+                            Args... args) {
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   const cudaError_t last = cudaGetLastError();  // also takes back e, which the next call would find there otherwise
   return e != cudaSuccess ? e : last;
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, cudaStream_t s, Args... args) {
+  return launch_early_as(kernel, grid, threads, 0, 1, s, args...);
 }
 
 // ---- small device helpers -------------------------------------------------------------------------
