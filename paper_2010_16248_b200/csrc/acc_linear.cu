@@ -1,5 +1,5 @@
 // Weight gradient of a linear layer from a checkpoint of its input: G_w (+)= scale * sum over the tokens t of dy_wt x_wt^T, a
-// matrix product on the tensor cores that reads the 8-bit codes and writes the workers' fp32 gradients.
+// matrix product on the tensor cores that writes the workers' fp32 gradients.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -11,39 +11,49 @@
 
 namespace acc {
 
-// A tile is 128 rows of the layer (the product's M) by up to 256 columns (N); a step is 64 tokens (K).  Both operands lie in
-// memory with the tokens outermost, so a stage holds them with M (N) contiguous: boxes of 64 elements (128 bytes) x 64 tokens
-// in the 128-byte swizzle, 16-byte chunk c of token k at chunk c ^ (k & 7).
-constexpr int kM = 128, kN = 256, kK = 64;
+// Two blocks on neighbouring SMs work on one tile of 256 rows of the layer (the product's M, 128 a block) by up to 256 columns
+// (N, half of them loaded by each block); a step is 64 tokens (K).  Both operands lie in memory with the tokens outermost, so a
+// stage holds them with M (N) contiguous: boxes of 64 elements (128 bytes) x 64 tokens in the 128-byte swizzle, 16-byte chunk c
+// of token k at chunk c ^ (k & 7).
+constexpr int kM = 128, kK = 64;
 constexpr int kBoxBytes = 64 * 128;
-constexpr int kABytes = kM / 64 * kBoxBytes, kBBytes = kN / 64 * kBoxBytes;
-constexpr int kEpiPitch = 33;
-
-enum { kEpiWarps = 4, kMmaWarp = 4, kTmaWarp = 5, kDecodeWarp = 6, kDecodeGroups = 2, kGroupWarps = 4, kLoadWarp = 14, kLoadWarps = 4 };
+constexpr int kABytes = kM / 64 * kBoxBytes;
+enum { kEpiWarps = 8, kMmaWarp = 8, kDyWarp = 9, kXWarp = 10, kLoadWarp = 12, kLoadWarps = 8 };
 
 // How dy reaches shared memory: bf16 by tensor copies, or (rows that do not start on 16 bytes; fp32) by loads.
 enum DyPath { DY_TMA, DY_BF16, DY_F32 };
 template <DyPath P> struct LinCfg {
   // fp32 values are three bf16 terms each (8 bits of the 24 apiece), so that the products stay those of fp32
   static constexpr int parts = P == DY_F32 ? 3 : 1;
-  static constexpr int stage = kABytes * parts + kBBytes;
-  static constexpr int stages = P == DY_F32 ? 2 : 4;
+  // columns of a tile: each of the eight warps that write it holds half of them for 32 rows, a lane's in registers, which the
+  // loading warps leave fewer of
+  static constexpr int n = P == DY_TMA ? 256 : 128;
+  static constexpr int b_bytes = n / 128 * kBoxBytes;
+  static constexpr int stage = kABytes * parts + b_bytes;
+  static constexpr int stages = P == DY_F32 ? 3 : 6;
   static constexpr int threads = 32 * (P == DY_TMA ? kLoadWarp : kLoadWarp + kLoadWarps);
-  static constexpr int smem = stages * stage + kEpiWarps * 32 * kEpiPitch * 4 + 1024;
+  // Finished sums pass through shared memory, eight rows of each quarter at a time; a pitch that spreads eight rows' 16 bytes over
+  // all banks
+  static constexpr int pitch = n + 4;
+  static constexpr int smem = stages * stage + 4 * 8 * pitch * 4 + 1024;
+  // Registers a thread: the sums' warps take what the others give back, within what the block was launched with.
+  static constexpr int launch_regs = P == DY_TMA ? 168 : 96, epi_regs = P == DY_TMA ? 216 : 128, mma_regs = P == DY_TMA ? 56 : 40, load_regs = 88;
+  static_assert(kEpiWarps * epi_regs + 4 * mma_regs + (threads / 32 - kLoadWarp) * load_regs <= threads / 32 * launch_regs, "");
+  // Most steps whose sum stays in the tensor core.  It cuts its sums where fp32 adds round: 44 products of 16 tokens in one sum
+  // are 8e-7 off, 1024 of them 1e-5.  So a sum ends after 24 products at most (as many of fp32's three terms) and is added to
+  // the others in registers.
+  static constexpr int chunk = P == DY_F32 ? 2 : 6;
 };
 
 struct LinArgs {
   const void* dy;
   long long ld, dy_stride;      // elements between tokens, between workers
   int n, rows, cols;
-  const uint4* code;            // [W][n] rows of code_row pieces of 16 codes
-  const uint8_t* scales;        // [W][n][blocks]
-  int code_row, blocks;
   float* out;                   // worker w's (split s's) layer at out + (s * W + w) * out_stride
   long long out_stride;
   float scale;
   int accumulate;
-  int W, m_tiles, n_tiles, splits, steps, tile_n;  // tile_n: columns of a tile, a multiple of 16
+  int W, m_tiles, n_tiles, splits, steps, tile_n;  // tile_n: columns of a tile, a multiple of 32
   int* status;
 };
 
@@ -59,36 +69,39 @@ __device__ __forceinline__ LinTile lin_tile(const LinArgs& a, int t) {
   return x;
 }
 
-// ---- tensor core, tensor memory ----------------------------------------------------------------------------------
+// The parts of a tile's steps that are summed on their own, as even as they come.
+template <int CHUNK> __device__ __forceinline__ int lin_chunks(const LinTile& x) { return (x.to - x.from + CHUNK - 1) / CHUNK; }
+
+// ---- tensor core, tensor memory, the pair of blocks -----------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(uint32_t* where) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(where)) : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(where)) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
 }
 __device__ __forceinline__ void tmem_free(uint32_t at) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(at));
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at));
 }
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// One arrival on this barrier in both blocks once the products issued so far are done.
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                   smem_u32(bar)), "h"((unsigned short)3)
+               : "memory");
 }
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile(
       "{\n"
       "  .reg .pred p;\n"
       "  setp.ne.u32 p, %4, 0;\n"
-      "  tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      "  tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
       "}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add)
       : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* v) {
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t* v) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
-      "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]),
-        "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]),
-        "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
       : "r"(at));
 }
 __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -99,129 +112,268 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t smem) {
   return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)(kBoxBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
          (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-// fp32 sums of bf16 products, both operands with M (N) contiguous.
+// fp32 sums of bf16 products, both operands with M (N) contiguous, M of the pair.
 __device__ __forceinline__ uint32_t mma_desc(int n) {
-  return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
+  return 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(2 * kM >> 4) << 24;
 }
+// A copy into this block's stage that counts on the first block's barrier.
 __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
-                   "r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-               : "memory");
+  asm volatile(
+      "{\n"
+      "  .reg .b32 there;\n"
+      "  mapa.shared::cluster.u32 there, %5, 0;\n"
+      "  cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [there];\n"
+      "}\n" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
 }
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+// An arrival on the first block's barrier, from either block.
+__device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
+  asm volatile(
+      "{\n"
+      "  .reg .b32 there;\n"
+      "  mapa.shared::cluster.u32 there, %0, 0;\n"
+      "  mbarrier.arrive.shared::cluster.b64 _, [there];\n"
+      "}\n" ::"r"(smem_u32(bar))
+      : "memory");
 }
-__device__ __forceinline__ void store16(char* p, const uint4& v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(smem_u32(p)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// True in one lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  unsigned ok;
+  asm volatile(
+      "{\n"
+      "  .reg .pred p;\n"
+      "  elect.sync _|p, 0xffffffff;\n"
+      "  selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok));
+  return ok != 0;
 }
-
-// ---- codes -> bf16 -----------------------------------------------------------------------------------------------
-__device__ __forceinline__ unsigned mul_bf16x2(unsigned a, unsigned b) {
-  unsigned r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Sixteen codes times their scale, exactly: a code's exponent and mantissa, moved to where bf16 has them, stand for the value
-// times 2^-120 (subnormal codes become subnormal there), and the two factors are powers of two.
-__device__ __forceinline__ void decode16(const uint4& c, unsigned byte, uint4& lo, uint4& hi) {
-  const unsigned s = byte == 0 ? 0x0040u : byte == 255 ? 0x7fffu : byte << 7, s2 = s | s << 16;
-  const unsigned w[4] = {c.x, c.y, c.z, c.w};
-  unsigned o[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const unsigned x = __byte_perm(w[k >> 1], 0, k & 1 ? 0x3424 : 0x1404);
-    o[k] = mul_bf16x2(mul_bf16x2((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), 0x7b807b80u), s2);
-  }
-  lo = make_uint4(o[0], o[1], o[2], o[3]);
-  hi = make_uint4(o[4], o[5], o[6], o[7]);
-}
-
 struct LinShared {
-  uint64_t full[4], empty[4], acc_full[2], acc_empty[2], drain;
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
   uint32_t tmem;
 };
 
 // A wait of a role; when it gives up, the call's status says so and the role ends, and with it, by their own limits, the others.
+// (Waits and remote arrivals of block scope: what they order lies in shared memory, which has no copies; the cluster's scope
+// costs each a fence of the whole memory, four times the time of a step's products.)
 __device__ __forceinline__ bool lin_wait(uint64_t* bar, unsigned parity, int* status) {
   if (mbar_wait_bounded(bar, parity)) return true;
   atomicCAS(status, 0, ACC_ETIMEOUT);
   return false;
 }
 
-// dy's values of one token and 8 rows as bf16 terms.
-template <DyPath P, bool WIDE>
-__device__ __forceinline__ void load_dy8(const LinArgs& a, long long at, int left, uint4* part) {
-  if constexpr (P == DY_BF16) {
-    const unsigned short* p = static_cast<const unsigned short*>(a.dy) + at;
-    unsigned w[4] = {};
-    if (left >= 8) {
+// The two warps that share a quarter of the rows.
+__device__ __forceinline__ void quarter_sync(int quarter) { asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory"); }
+
+__device__ __forceinline__ bool quarter_all(int quarter, bool ok) {
+  unsigned all;
+  asm volatile(
+      "{\n"
+      "  .reg .pred p, q;\n"
+      "  setp.ne.u32 p, %2, 0;\n"
+      "  barrier.red.and.pred q, %1, 64, p;\n"
+      "  selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(all)
+      : "r"(quarter + 1), "r"((unsigned)ok)
+      : "memory");
+  return all != 0;
+}
+
+// Up to four rows of finished sums, `cols` columns each, to or onto rows of the layer.  A lane's columns count from the last
+// multiple of 32 bytes before the row's first, so that a store covers whole sectors of memory whatever the row's start: rows of
+// 650 columns, which start at any multiple of 8 bytes, go out at 4.2 TB/s, and at 2.5 with lanes counted from the first column.
+template <int N, int PITCH, bool ADD>
+__device__ __forceinline__ void write_rows(const float* buf, float* out, int ld, int cols, int rows, int lane) {
+  constexpr int kPlaces = N / 32 + 1;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = WIDE ? reinterpret_cast<const unsigned*>(p)[k] : p[2 * k] | (unsigned)p[2 * k + 1] << 16;
-    } else {
-      for (int k = 0; k < left; ++k) w[k >> 1] |= (unsigned)p[k] << (16 * (k & 1));
-    }
-    part[0] = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-    const float* p = static_cast<const float*>(a.dy) + at;
-    float v[8] = {};
-    if (left >= 8) {
-      if (WIDE) {
-        const float4 x = reinterpret_cast<const float4*>(p)[0], y = reinterpret_cast<const float4*>(p)[1];
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-      } else {
+  for (int r = 0; r < 4; ++r) {
+    if (r >= rows) break;
+    float* const p = out + (long long)r * ld;
+    const int first = lane - (int)((reinterpret_cast<uintptr_t>(p) >> 2) & 7);
+    float v[kPlaces], old[kPlaces];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = p[k];
-      }
-    } else {
-      for (int k = 0; k < left; ++k) v[k] = p[k];
-    }
-    unsigned w[3][4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-#pragma unroll
-      for (int j = 0; j < 3; ++j) w[j][k] = 0;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // cut, not rounded: each term takes the next 8 bits, and the rest is exact; an infinity or NaN is the first term alone
-        const float x = v[2 * k + h];
-        const unsigned b0 = __float_as_uint(x) & 0xffff0000u;
-        const bool fine = (b0 & 0x7f800000u) != 0x7f800000u;
-        const float r0 = fine ? x - __uint_as_float(b0) : 0.f;
-        const unsigned b1 = __float_as_uint(r0) & 0xffff0000u;
-        const unsigned b2 = __float_as_uint(r0 - __uint_as_float(b1)) & 0xffff0000u;
-        const unsigned first = fine ? b0 : (__float_as_uint(x) & 0x7fffffffu) > 0x7f800000u ? 0x7fff0000u : b0;
-        w[0][k] |= h ? first : first >> 16;
-        w[1][k] |= h ? b1 : b1 >> 16;
-        w[2][k] |= h ? b2 : b2 >> 16;
-      }
+    for (int w = 0; w < kPlaces; ++w) {
+      const bool on = (unsigned)(first + 32 * w) < (unsigned)cols;
+      v[w] = on ? buf[r * PITCH + first + 32 * w] : 0.f;
+      if (ADD) old[w] = on ? p[first + 32 * w] : 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < 3; ++j) part[j] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+    for (int w = 0; w < kPlaces; ++w)
+      if ((unsigned)(first + 32 * w) < (unsigned)cols) p[first + 32 * w] = ADD ? old[w] + v[w] : v[w];
   }
 }
 
-// One block per SM walks over the tiles.  Warps 0-3 write finished tiles, warp 4 issues the products, warp 5 the copies of
-// dy, two groups of four warps decode the checkpoint's codes for alternate steps (a group's loads of its next step are under
-// way while the other decodes), and where dy cannot be copied four more warps load it.  Two accumulators in tensor memory: a
-// tile is written while the next is summed.
+// ---- dy by loads --------------------------------------------------------------------------------------------------
+// The steps of a pair, one after another over its tiles.
+struct StepWalk {
+  const LinArgs& a;
+  int t, by, k;
+  LinTile x;
+  __device__ __forceinline__ StepWalk(const LinArgs& a, int pair, int pairs) : a(a), t(pair), by(pairs) {
+    if (on()) x = lin_tile(a, t), k = x.from;
+  }
+  __device__ __forceinline__ bool on() const { return t < a.splits * a.W * a.m_tiles * a.n_tiles; }
+  __device__ __forceinline__ void next() {
+    if (++k < x.to) return;
+    t += by;
+    if (on()) x = lin_tile(a, t), k = x.from;
+  }
+};
+
+// A loading warp's share of a step: its box of 64 rows, two of them a lane, of the tokens token0, token0 + 4, ...: 16 lines of
+// 128 bytes in a stage.
+constexpr int kLines = 16;
+struct DyShare {
+  int box, token0, lane;
+  __device__ __forceinline__ int row(const LinTile& x, int rank) const { return x.m * 2 * kM + rank * kM + box * 64 + 2 * lane; }
+  __device__ __forceinline__ uint32_t place(int line) const {
+    const int token = token0 + 4 * line;
+    return box * kBoxBytes + token * 128 + (((lane >> 2) ^ (token & 7)) << 4) + (lane & 3) * 4;
+  }
+};
+__device__ __forceinline__ void store4(uint32_t at, unsigned v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+
+// bf16 rows on 4 bytes: words copied asynchronously, two steps ahead of the step that is handed on.
+template <typename Wait, typename Done>
+__device__ __forceinline__ void copy_words(const LinArgs& a, StepWalk walk, const DyShare& me, int rank, uint32_t stages, int stage,
+                                           int S, Wait wait, Done done) {
+  constexpr unsigned kAhead = 2;
+  unsigned step = 0, told = 0;
+  for (; walk.on(); walk.next(), ++step) {
+    if (!wait(step)) break;
+    const uint32_t at = stages + step % S * stage;
+    const int row = me.row(walk.x, rank), live = 2 * max(0, min(2, a.rows - row)), token0 = walk.k * kK + me.token0;
+    const __nv_bfloat16* const from = static_cast<const __nv_bfloat16*>(a.dy) + walk.x.w * a.dy_stride + (live ? row : 0);
+#pragma unroll
+    for (int i = 0; i < kLines; ++i) {
+      const int token = token0 + 4 * i;  // (bytes that are not there arrive as zeros)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + me.place(i)),
+                   "l"(__cvta_generic_to_global(token < a.n ? from + token * a.ld : from)), "r"(token < a.n ? live : 0)
+                   : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (step < kAhead) continue;
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+    done(told++);
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  while (told < step) done(told++);
+}
+
+// Loads into registers, a step ahead: single bf16 values, or pairs of fp32 that become three terms each.
+template <bool F32, bool WIDE> struct DyPair;
+template <bool WIDE> struct DyPair<false, WIDE> {
+  unsigned short v[2];
+  __device__ __forceinline__ void load(const void* dy, long long at, int live) {
+    const unsigned short* const p = static_cast<const unsigned short*>(dy) + at;
+    v[0] = live > 0 ? p[0] : 0;
+    v[1] = live > 1 ? p[1] : 0;
+  }
+  static constexpr bool special = false;
+  __device__ __forceinline__ void watch(float&) const {}
+  __device__ __forceinline__ void store(uint32_t at, bool) const { store4(at, v[0] | (unsigned)v[1] << 16); }
+};
+template <bool WIDE> struct DyPair<true, WIDE> {
+  float v[2];
+  __device__ __forceinline__ void load(const void* dy, long long at, int live) {
+    const float* const p = static_cast<const float*>(dy) + at;
+    if (WIDE && live == 2) {
+      const float2 x = *reinterpret_cast<const float2*>(p);
+      v[0] = x.x; v[1] = x.y;
+    } else {
+      v[0] = live > 0 ? p[0] : 0.f;
+      v[1] = live > 1 ? p[1] : 0.f;
+    }
+  }
+  static constexpr bool special = true;
+  __device__ __forceinline__ void watch(float& most) const {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v[k])));
+  }
+  // Cut, not rounded: each term takes the next 8 bits, and the rest is exact.  An infinity or NaN (`odd`) is the first alone.
+  __device__ __forceinline__ void store(uint32_t at, bool odd) const {
+    unsigned w[3] = {};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      unsigned b0 = __float_as_uint(v[k]) & 0xffff0000u;
+      float r = v[k] - __uint_as_float(b0);
+      if (odd && !(fabsf(v[k]) < __builtin_huge_valf())) {
+        r = 0.f;
+        if (v[k] != v[k]) b0 = 0x7fff0000u;
+      }
+      const unsigned b1 = __float_as_uint(r) & 0xffff0000u;
+      const unsigned b2 = __float_as_uint(r - __uint_as_float(b1));
+      w[0] = k ? __byte_perm(w[0], b0, 0x7610) : b0 >> 16;
+      w[1] = k ? __byte_perm(w[1], b1, 0x7610) : b1 >> 16;
+      w[2] = k ? __byte_perm(w[2], b2, 0x7610) : b2 >> 16;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) store4(at + q * kABytes, w[q]);
+  }
+};
+template <bool F32, bool WIDE, typename Wait, typename Done>
+__device__ __forceinline__ void load_pairs(const LinArgs& a, StepWalk walk, const DyShare& me, int rank, uint32_t stages, int stage,
+                                           int S, Wait wait, Done done) {
+  DyPair<F32, WIDE> pair[kLines];
+  auto fetch = [&]() {
+    const int row = me.row(walk.x, rank), live = max(0, min(2, a.rows - row)), token0 = walk.k * kK + me.token0;
+    const long long at = walk.x.w * a.dy_stride + row;
+#pragma unroll
+    for (int i = 0; i < kLines; ++i) {
+      const int token = token0 + 4 * i;
+      pair[i].load(a.dy, at + token * a.ld, token < a.n ? live : 0);
+    }
+  };
+  if (walk.on()) fetch();
+  for (unsigned step = 0; walk.on(); ++step) {
+    if (!wait(step)) break;
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLines; ++i) pair[i].watch(most);
+    const bool odd = DyPair<F32, WIDE>::special && !(most < __builtin_huge_valf());
+    const uint32_t at = stages + step % S * stage;
+    if (__any_sync(0xffffffffu, odd)) {
+#pragma unroll
+      for (int i = 0; i < kLines; ++i) pair[i].store(at + me.place(i), true);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLines; ++i) pair[i].store(at + me.place(i), false);
+    }
+    done(step);
+    walk.next();
+    if (walk.on()) fetch();
+  }
+}
+
+// The blocks of a pair walk over the tiles.  In each, warps 0-7 add up and write the sums of its 128 rows, two warps for each
+// quarter of them, warps 9 and 10 issue the copies of dy and of the checkpoint, and where dy cannot be copied eight more warps
+// load it; the first block's warp 8 issues the products of both.  Two sums in tensor memory: one is read while the other grows.
 template <DyPath P, bool WIDE>
-__global__ void __launch_bounds__(LinCfg<P>::threads, 1) linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(LinCfg<P>::threads, 1)
+linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map) {
   using Cfg = LinCfg<P>;
   constexpr int S = Cfg::stages;
   extern __shared__ char dynamic[];
   __shared__ LinShared sh;
   char* const stages = dynamic + (1024 - (smem_u32(dynamic) & 1023)) % 1024;
-  float* const epi = reinterpret_cast<float*>(stages + S * Cfg::stage);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tiles = a.splits * a.W * a.m_tiles * a.n_tiles;
+  const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int tiles = a.splits * a.W * a.m_tiles * a.n_tiles, half = a.tile_n / 2;
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(&sh.full[s], kGroupWarps + (P == DY_TMA ? 1 : kLoadWarps));
+      mbar_init(&sh.full[s], 1 + (P == DY_TMA ? 0 : 2 * kLoadWarps));
       mbar_init(&sh.empty[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sh.acc_full[s], 1);
-      mbar_init(&sh.acc_empty[s], kEpiWarps);
+      mbar_init(&sh.acc_empty[s], 2 * kEpiWarps);
     }
     mbar_init(&sh.drain, 1);
     fence_mbar_init();
@@ -232,203 +384,144 @@ __global__ void __launch_bounds__(LinCfg<P>::threads, 1) linear_grad_kernel(cons
   if (warp == kMmaWarp) tmem_alloc(&sh.tmem);
   tc_before_sync();
   __syncthreads();
+  cluster_sync();
   tc_after_sync();
   let_next_start();
   const uint32_t tmem = sh.tmem;
 
   if (warp < kEpiWarps) {
-    float* const buf = epi + warp * 32 * kEpiPitch;
-    unsigned i = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++i) {
+    more_registers<Cfg::epi_regs>();
+    constexpr int kHeld = Cfg::n / 2;  // columns of a lane's row
+    const int quarter = warp & 3, side = warp >> 2;
+    float* const buf = reinterpret_cast<float*>(stages + S * Cfg::stage) + quarter * 8 * Cfg::pitch;
+    const uint32_t held_at = tmem + side * half + ((uint32_t)(quarter * 32) << 16);
+    unsigned sum = 0;
+    bool ok = true;
+    for (int t = pair; t < tiles && ok; t += pairs) {
+      float held[kHeld];
+      auto take = [&](auto add) {
+        if (!(ok = lin_wait(&sh.acc_full[sum & 1], (sum >> 1) & 1, a.status))) return;
+        tc_after_sync();
+#pragma unroll
+        for (int c = 0; c < kHeld; c += 32) {  // (the last reads up to 16 columns behind its half, which nobody writes)
+          if (c < half) {
+            uint32_t v[32];
+            tmem_load16(held_at + (sum & 1) * Cfg::n + c, v);
+            tmem_load16(held_at + (sum & 1) * Cfg::n + c + 16, v + 16);
+            tmem_wait_load();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) held[c + j] = decltype(add)::value ? held[c + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+          }
+        }
+        tc_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_first(&sh.acc_empty[sum & 1]);
+        ++sum;
+      };
+      int chunks = lin_chunks<Cfg::chunk>(lin_tile(a, t));
+      take(std::false_type());
+      while (--chunks > 0 && ok) take(std::true_type());
+      // (a quarter's warps give up together: neither waits for the other where it writes)
+      if (!(ok = quarter_all(quarter, ok))) break;
       const LinTile x = lin_tile(a, t);
-      const unsigned acc = i & 1;
-      if (!lin_wait(&sh.acc_full[acc], (i >> 1) & 1, a.status)) break;
-      tc_after_sync();
-      const int row0 = x.m * kM + warp * 32, n0 = x.n * a.tile_n;
+      const int row0 = x.m * 2 * kM + rank * kM + quarter * 32, n0 = x.n * a.tile_n;
       float* const out = a.out + ((long long)x.split * a.W + x.w) * a.out_stride + (long long)row0 * a.cols + n0;
       const int rows = min(32, a.rows - row0), cols = min(a.tile_n, a.cols - n0);
-      for (int c = 0; c < cols; c += 32) {
-        uint32_t v[32];
-        tmem_load32(tmem + acc * kN + c + ((uint32_t)(warp * 32) << 16), v);
-        tmem_wait_load();
+#pragma unroll 1
+      for (int g = 0; g < 32 && g < rows; g += 8) {
+        if ((lane & 24) == g) {
+          float* const line = buf + (lane & 7) * Cfg::pitch + side * half;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) buf[lane * kEpiPitch + k] = __uint_as_float(v[k]) * a.scale;
-        __syncwarp();
-        if (c + lane < cols) {
-          float* const p = out + c + lane;
-          if (a.accumulate) {
-            for (int r = 0; r < rows; r += 8) {  // loads of a batch first
-              float old[8];
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (r + k < rows) old[k] = p[(long long)(r + k) * a.cols];
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (r + k < rows) p[(long long)(r + k) * a.cols] = old[k] + buf[(r + k) * kEpiPitch + lane];
-            }
-          } else {
-#pragma unroll 8
-            for (int r = 0; r < rows; ++r) p[(long long)r * a.cols] = buf[r * kEpiPitch + lane];
-          }
+          for (int c = 0; c < kHeld; c += 4)
+            if (c < half)
+              *reinterpret_cast<float4*>(line + c) =
+                  make_float4(held[c] * a.scale, held[c + 1] * a.scale, held[c + 2] * a.scale, held[c + 3] * a.scale);
         }
-        __syncwarp();
+        quarter_sync(quarter);
+        const float* const from = buf + 4 * side * Cfg::pitch;
+        float* const to = out + (long long)(g + 4 * side) * a.cols;
+        if (a.accumulate) write_rows<Cfg::n, Cfg::pitch, true>(from, to, a.cols, cols, rows - g - 4 * side, lane);
+        else write_rows<Cfg::n, Cfg::pitch, false>(from, to, a.cols, cols, rows - g - 4 * side, lane);
+        quarter_sync(quarter);
       }
-      tc_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
     }
-  } else if (warp == kMmaWarp) {
-    if (lane == 0) {
-      unsigned step = 0, i = 0;
+  } else if (warp < kLoadWarp) {
+    fewer_registers<Cfg::mma_regs>();
+    unsigned step = 0;
+    bool ok = true;
+    if (warp == kMmaWarp && rank == 0) {
+      unsigned sum = 0;
       const uint32_t idesc = mma_desc(a.tile_n);
-      bool ok = true;
-      for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++i) {
+      const bool issuer = elect_one();
+      for (int t = pair; t < tiles && ok; t += pairs) {
         const LinTile x = lin_tile(a, t);
-        const unsigned acc = i & 1;
-        if (!(ok = lin_wait(&sh.acc_empty[acc], ((i >> 1) & 1) ^ 1, a.status))) break;
-        tc_after_sync();
+        const int chunks = lin_chunks<Cfg::chunk>(x);
+        int begin = x.from, end = begin, chunk = 0;
         for (int k = x.from; k < x.to; ++k, ++step) {
-          const unsigned s = step % S;
+          if (k == end) begin = k, end = x.from + (x.to - x.from) * ++chunk / chunks;
+          const unsigned s = step % S, acc = sum & 1;
+          const bool first = k == begin, last = k + 1 == end;
+          if (first && !(ok = lin_wait(&sh.acc_empty[acc], ((sum >> 1) & 1) ^ 1, a.status))) break;
           if (!(ok = lin_wait(&sh.full[s], (step / S) & 1, a.status))) break;
           tc_after_sync();
-          const uint32_t at = smem_u32(stages + s * Cfg::stage);
-          const uint64_t b = operand_desc(at + Cfg::parts * kABytes);
+          if (issuer) {
+            const uint32_t at = smem_u32(stages + s * Cfg::stage);
+            const uint64_t b = operand_desc(at + Cfg::parts * kABytes);
 #pragma unroll
-          for (int part = 0; part < Cfg::parts; ++part) {
-            const uint64_t am = operand_desc(at + part * kABytes);
+            for (int part = 0; part < Cfg::parts; ++part) {
+              const uint64_t am = operand_desc(at + part * kABytes);
 #pragma unroll
-            for (int j = 0; j < kK / 16; ++j)
-              tc_mma(tmem + acc * kN, am + j * (2048 >> 4), b + j * (2048 >> 4), idesc, k > x.from || part > 0 || j > 0);
+              for (int j = 0; j < kK / 16; ++j)
+                tc_mma(tmem + acc * Cfg::n, am + j * (2048 >> 4), b + j * (2048 >> 4), idesc, !first || part > 0 || j > 0);
+            }
+            tc_commit(&sh.empty[s]);
+            if (last) tc_commit(&sh.acc_full[acc]);
           }
-          tc_commit(&sh.empty[s]);
+          sum += last;
         }
-        if (ok) tc_commit(&sh.acc_full[acc]);
       }
-      if (!ok) {  // nothing of this block's may be in flight when it frees its tensor memory
+      if (!ok && issuer) {  // no product may be under way when the blocks free their tensor memory
         tc_commit(&sh.drain);
         mbar_wait_bounded(&sh.drain, 0);
       }
-    }
-    __syncwarp();
-  } else if (warp == kTmaWarp) {
-    if (P == DY_TMA && lane == 0) {
-      unsigned step = 0;
-      bool ok = true;
-      for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+    } else if ((warp == kDyWarp || warp == kXWarp) && elect_one()) {
+      const int boxes = warp == kXWarp ? (half + 63) / 64 : P == DY_TMA ? kM / 64 : 0;
+      const unsigned bytes = 2 * ((P == DY_TMA ? kABytes : 0) + (half + 63) / 64 * kBoxBytes);  // of a step, in both blocks
+      const CUtensorMap* const map = warp == kXWarp ? &x_map : &dy_map;
+      for (int t = pair; t < tiles && ok; t += pairs) {
         const LinTile x = lin_tile(a, t);
+        const int at0 = warp == kXWarp ? x.n * a.tile_n + rank * half : x.m * 2 * kM + rank * kM;
         for (int k = x.from; k < x.to; ++k, ++step) {
           const unsigned s = step % S;
           if (!(ok = lin_wait(&sh.empty[s], ((step / S) & 1) ^ 1, a.status))) break;
-          char* const at = stages + s * Cfg::stage;
-          mbar_arrive_expect_tx(&sh.full[s], kABytes);
-          for (int b = 0; b < kM / 64; ++b) tma_load(at + b * kBoxBytes, &map, x.m * kM + b * 64, k * kK, x.w, &sh.full[s]);
+          if (warp == kDyWarp && rank == 0) mbar_arrive_expect_tx(&sh.full[s], bytes);
+          char* const to = stages + s * Cfg::stage + (warp == kXWarp ? Cfg::parts * kABytes : 0);
+          for (int b = 0; b < boxes; ++b) tma_load(to + b * kBoxBytes, map, at0 + b * 64, k * kK, x.w, &sh.full[s]);
         }
       }
-      if (!ok)  // copies under way end before the block does
+      if (!ok && warp == kDyWarp && rank == 0)  // both blocks' copies under way end before the blocks do
         for (unsigned j = step < S ? 0 : step - S; j < step; ++j) mbar_wait_bounded(&sh.full[j % S], (j / S) & 1);
     }
-    __syncwarp();
-  } else if (warp < kLoadWarp) {
-    const int group = (warp - kDecodeWarp) / kGroupWarps, tid = threadIdx.x - 32 * (kDecodeWarp + group * kGroupWarps);
-    const int piece = tid & 15, token0 = tid >> 4;  // 16 codes; tokens token0, token0 + 8, ... of a step
-    uint4 code[8];
-    unsigned byte[8];
-    // this group's next step: tile, step inside it, number among all
-    int t = blockIdx.x, k = 0;
-    unsigned step = 0;
-    LinTile x{};
-    auto settle = [&]() {  // moves on to the next tile until step k lies inside one
-      while (t < tiles) {
-        x = lin_tile(a, t);
-        if (x.from + k < x.to) return;
-        k -= x.to - x.from;
-        t += gridDim.x;
-      }
-    };
-    auto fetch = [&]() {
-      const int col = x.n * a.tile_n + piece * 16;  // pieces behind the tile or the row are zeros
-      const bool on = piece * 16 < a.tile_n && (col >> 4) < a.code_row;
-      const int token = (x.from + k) * kK + token0;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        code[u] = make_uint4(0, 0, 0, 0);
-        byte[u] = 0;
-        if (on && token + 8 * u < a.n) {
-          const long long row = (long long)x.w * a.n + token + 8 * u;
-          code[u] = a.code[row * a.code_row + (col >> 4)];
-          byte[u] = a.scales[row * a.blocks + (col >> 5)];
-        }
-      }
-    };
-    k = group;
-    step = group;
-    settle();
-    if (t < tiles) fetch();
-    while (t < tiles) {
-      const unsigned s = step % S;
-      if (!lin_wait(&sh.empty[s], ((step / S) & 1) ^ 1, a.status)) break;
-      char* const at = stages + s * Cfg::stage + Cfg::parts * kABytes + (piece >> 2) * kBoxBytes;
-      if (piece * 16 < a.tile_n) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          uint4 lo, hi;
-          decode16(code[u], byte[u], lo, hi);
-          const int token = token0 + 8 * u, chunk = 2 * (piece & 3);
-          char* const line = at + token * 128;
-          // (neighbouring boxes' lanes begin with opposite halves: their chunks lie in the same banks)
-          const bool swap = piece & 4;
-          store16(line + (((chunk + swap) ^ (token & 7)) << 4), swap ? hi : lo);
-          store16(line + (((chunk + !swap) ^ (token & 7)) << 4), swap ? lo : hi);
-        }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.full[s]);
-      k += kDecodeGroups;
-      step += kDecodeGroups;
-      settle();
-      if (t < tiles) fetch();
-    }
   } else {
-    const int tid = threadIdx.x - 32 * kLoadWarp, chunk = tid & 15, token0 = tid >> 4;
-    unsigned step = 0;
-    bool ok = true;
-    for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-      const LinTile x = lin_tile(a, t);
-      const int row = x.m * kM + chunk * 8, left = a.rows - row;
-      for (int k = x.from; k < x.to; ++k, ++step) {
-        const unsigned s = step % S;
-        if (!(ok = lin_wait(&sh.empty[s], ((step / S) & 1) ^ 1, a.status))) break;
-        char* const at = stages + s * Cfg::stage + (chunk >> 3) * kBoxBytes;
-#pragma unroll 1
-        for (int u = 0; u < 8; u += 4) {
-          uint4 part[4][Cfg::parts];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int token = k * kK + token0 + 8 * (u + j);
-            if (token < a.n && left > 0) {
-              load_dy8<P, WIDE>(a, x.w * a.dy_stride + token * a.ld + row, left, part[j]);
-            } else {
-              for (int q = 0; q < Cfg::parts; ++q) part[j][q] = make_uint4(0, 0, 0, 0);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int token = token0 + 8 * (u + j);
-#pragma unroll
-            for (int q = 0; q < Cfg::parts; ++q)
-              store16(at + q * kABytes + token * 128 + (((chunk & 7) ^ (token & 7)) << 4), part[j][q]);
-          }
-        }
+    fewer_registers<Cfg::load_regs>();
+    if constexpr (P != DY_TMA) {
+      const int loader = warp - kLoadWarp;
+      const DyShare me{loader & 1, loader >> 1, lane};
+      const uint32_t at = smem_u32(stages);
+      auto wait = [&](unsigned step) { return lin_wait(&sh.empty[step % S], ((step / S) & 1) ^ 1, a.status); };
+      auto done = [&](unsigned step) {
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.full[s]);
-      }
+        if (lane == 0) mbar_arrive_first(&sh.full[step % S]);
+      };
+      if constexpr (P == DY_BF16 && WIDE) copy_words(a, StepWalk(a, pair, pairs), me, rank, at, Cfg::stage, S, wait, done);
+      else load_pairs<P == DY_F32, WIDE>(a, StepWalk(a, pair, pairs), me, rank, at, Cfg::stage, S, wait, done);
     }
   }
   __syncwarp();
   tc_before_sync();
   __syncthreads();
+  cluster_sync();  // the other block may still read this one's stages and arrive on its barriers
   tc_after_sync();
   if (warp == kMmaWarp) tmem_free(tmem);
 }
@@ -464,33 +557,56 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* part, lon
 struct LinPlan {
   int m_tiles, n_tiles, tile_n, steps, splits;
   long long slab;  // floats of a split's sums of one worker
-  size_t bytes;
+  size_t x_bytes, bytes;  // of the decoded checkpoint; of it and the splits' sums
 };
-static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n) {
+static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n, int most_n, int parts) {
   const DevLayer& L = ctx->plan.layers[layer];
   const int W = ctx->cfg.n_workers;
   LinPlan p{};
-  p.m_tiles = (L.rows + kM - 1) / kM;
-  p.n_tiles = (L.cols + kN - 1) / kN;
-  p.tile_n = ((L.cols + p.n_tiles - 1) / p.n_tiles + 15) / 16 * 16;
+  p.m_tiles = (L.rows + 2 * kM - 1) / (2 * kM);
   p.steps = (int)((n + kK - 1) / kK);
   p.slab = ((long long)L.rows * L.cols + 3) / 4 * 4;
-  // Few tiles leave SMs idle: the tokens are then cut into splits, whose sums a second kernel joins.  Costs in steps of 64
-  // tokens (a quarter of a microsecond): a tile's start and end 6, the second launch 8, its traffic at the memory's rate.
-  const long long tiles = (long long)W * p.m_tiles * p.n_tiles, sms = ctx->sm_count;
-  double best = 0;
-  for (int s = 1; s <= 32 && (s == 1 || p.steps / s >= 4); ++s) {
-    const double waves = (double)((tiles * s + sms - 1) / sms), traffic = (s + 1.0) * W * p.slab * 4.0 / 1.6e6;
-    const double cost = waves * ((p.steps + s - 1) / s + 6) + (s > 1 ? 8 + traffic : 0.0);
-    if (s == 1 || cost < best) { best = cost; p.splits = s; }
+  // Few tiles leave SMs idle: then the tiles get narrower, or the tokens are cut into splits whose sums a second kernel joins.
+  // Costs in products of 64 tokens by 256 columns (a quarter of a microsecond): a step of a narrow tile costs what
+  // dy's copies take, that of 224 columns; a tile's start and end are 6 of its width and 2, the second launch 8 and its traffic.
+  const long long pairs = ctx->sm_count / 2;
+  const int least = (L.cols + most_n - 1) / most_n;
+  double best = -1.0;
+  for (int nt = least; nt <= 4 * least && (nt == least || L.cols / nt >= 32); ++nt) {
+    const int tile_n = ((L.cols + nt - 1) / nt + 31) / 32 * 32, n_tiles = (L.cols + tile_n - 1) / tile_n;
+    const long long tiles = (long long)W * p.m_tiles * n_tiles;
+    const double each = tile_n / 256.0, step = std::max(each, most_n * 0.875 / 256.0);
+    for (int s = 1; s <= 32 && (s == 1 || p.steps / s >= 4); ++s) {
+      const double waves = (double)((tiles * s + pairs - 1) / pairs), traffic = (s + 1.0) * W * p.slab * 4.0 / 1.6e6;
+      const double cost = waves * ((p.steps + s - 1) / s * step * parts + 6 * each + 2) + (s > 1 ? 8 + traffic : 0.0);
+      if (best < 0 || cost < best) {
+        best = cost;
+        p.splits = s;
+        p.tile_n = tile_n;
+        p.n_tiles = n_tiles;
+      }
+    }
   }
-  p.bytes = p.splits > 1 ? sizeof(float) * (size_t)p.splits * W * p.slab : 0;
+  const long long row = (L.cols + ACC_CHECKPOINT_BLOCK - 1) / ACC_CHECKPOINT_BLOCK * ACC_CHECKPOINT_BLOCK;
+  p.x_bytes = ((size_t)(2 * row * n * W) + 255) / 256 * 256;
+  p.bytes = p.x_bytes + (p.splits > 1 ? sizeof(float) * (size_t)p.splits * W * p.slab : 0);
   if (p.bytes < 256) p.bytes = 256;
   return p;
 }
-size_t linear_grad_workspace(const acc_ctx* ctx, int layer, long long n) { return lin_plan(ctx, layer, n).bytes; }
+template <DyPath P> static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n) {
+  return lin_plan(ctx, layer, n, LinCfg<P>::n, LinCfg<P>::parts);
+}
+size_t linear_grad_workspace(const acc_ctx* ctx, int layer, long long n) {
+  return std::max(lin_plan<DY_TMA>(ctx, layer, n).bytes,
+                  std::max(lin_plan<DY_BF16>(ctx, layer, n).bytes, lin_plan<DY_F32>(ctx, layer, n).bytes));
+}
 
 template <DyPath P, bool WIDE> static cudaError_t lin_prepare() {
+  // (a block launched with fewer registers than it deals out would wait for them for good)
+  cudaFuncAttributes f;
+  cudaError_t e = cudaFuncGetAttributes(&f, linear_grad_kernel<P, WIDE>);
+  if (e == cudaSuccess && f.numRegs < LinCfg<P>::launch_regs) e = cudaErrorInvalidConfiguration;
+  if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(linear_grad_kernel<P, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, LinCfg<P>::smem);
 }
 cudaError_t prepare_linear() {
@@ -520,6 +636,18 @@ static EncodeTiled encode_tiled() {
   return f;
 }
 
+// Map of [W][n] rows of `width` bf16 values, ld apart, workers `stride` apart (each a multiple of 8 where there are several;
+// a dimension of one has no stride of its own, and any that spans it does); false for strides beyond a map's range.
+static bool bf16_map(CUtensorMap* map, const void* p, long long width, long long n, long long W, long long ld, long long stride) {
+  const long long row = n == 1 ? (width + 7) / 8 * 8 : ld, worker = W == 1 ? row * n : stride;
+  const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)n, (cuuint64_t)W};
+  const cuuint64_t strides[2] = {(cuuint64_t)row * 2, (cuuint64_t)worker * 2};
+  const cuuint32_t box[3] = {64, kK, 1}, one[3] = {1, 1, 1};
+  return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, one,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf16, long long n, long long ld,
                                long long dy_stride, float scale, const uint8_t* code, const uint8_t* scales, float* grads,
                                int accumulate, void* workspace, cudaStream_t s) {
@@ -533,51 +661,45 @@ cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf1
     for (int w = 0; w < W && e == cudaSuccess; ++w) e = cudaMemsetAsync(layer0 + w * stride, 0, sizeof(float) * size, s);
     return e;
   }
-  const LinPlan p = lin_plan(ctx, layer, n);
+  if (encode_tiled() == nullptr) return cudaErrorNotSupported;
+  // The checkpoint as bf16, exactly, once for all tiles: a tile's own decoding costs the SM more than its products do (64 tokens
+  // x 224 columns: 2400 warp instructions for 448 cycles of the tensor core).
+  const int row = (L.cols + ACC_CHECKPOINT_BLOCK - 1) / ACC_CHECKPOINT_BLOCK * ACC_CHECKPOINT_BLOCK;
+  const uintptr_t address = reinterpret_cast<uintptr_t>(dy);
+  CUtensorMap x_map{}, dy_map{};
+  if (!bf16_map(&x_map, workspace, row, n, W, row, row * n)) return cudaErrorInvalidValue;
+  const bool tma = bf16 && address % 16 == 0 && (n == 1 || ld % 8 == 0) && (W == 1 || dy_stride % 8 == 0) &&
+                   bf16_map(&dy_map, dy, L.rows, n, W, ld, dy_stride);
+  cudaError_t e = launch_checkpoint(ctx, false, workspace, true, n * W, row, row, nullptr, false, const_cast<uint8_t*>(code),
+                                    const_cast<uint8_t*>(scales), s);
+  if (e != cudaSuccess) return e;
+  const LinPlan p = tma ? lin_plan<DY_TMA>(ctx, layer, n) : bf16 ? lin_plan<DY_BF16>(ctx, layer, n) : lin_plan<DY_F32>(ctx, layer, n);
   const bool split = p.splits > 1;
-  const int blocks = (L.cols + ACC_CHECKPOINT_BLOCK - 1) / ACC_CHECKPOINT_BLOCK;
+  float* const sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.x_bytes);
   LinArgs a{};
   a.dy = dy; a.ld = ld; a.dy_stride = dy_stride;
   a.n = (int)n; a.rows = L.rows; a.cols = L.cols;
-  a.code = reinterpret_cast<const uint4*>(code); a.scales = scales;
-  a.code_row = blocks * 2; a.blocks = blocks;
-  a.out = split ? static_cast<float*>(workspace) : layer0;
+  a.out = split ? sums : layer0;
   a.out_stride = split ? p.slab : stride;
   a.scale = split ? 1.f : scale;
   a.accumulate = split ? 0 : accumulate;
   a.W = W; a.m_tiles = p.m_tiles; a.n_tiles = p.n_tiles; a.splits = p.splits; a.steps = p.steps; a.tile_n = p.tile_n;
   a.status = ctx->d_status;
-  const uintptr_t address = reinterpret_cast<uintptr_t>(dy);
-  CUtensorMap map{};
-  bool tma = bf16 && address % 16 == 0 && (n == 1 || ld % 8 == 0) && (W == 1 || dy_stride % 8 == 0);
-  if (tma) {
-    // (a dimension of one has no stride of its own: any multiple of 16 bytes that spans it)
-    const long long row = n == 1 ? (L.rows + 7) / 8 * 8 : ld, worker = W == 1 ? row * n : dy_stride;
-    const cuuint64_t dims[3] = {(cuuint64_t)L.rows, (cuuint64_t)n, (cuuint64_t)W};
-    const cuuint64_t strides[2] = {(cuuint64_t)row * 2, (cuuint64_t)worker * 2};
-    const cuuint32_t box[3] = {64, kK, 1}, one[3] = {1, 1, 1};
-    const EncodeTiled encode = encode_tiled();
-    if (encode == nullptr) return cudaErrorNotSupported;
-    if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(dy), dims, strides, box, one,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      tma = false;  // strides beyond a map's range take the other way
-  }
   const long long tiles = (long long)p.splits * W * p.m_tiles * p.n_tiles;
-  const unsigned grid = (unsigned)std::min<long long>(tiles, ctx->sm_count);
-  cudaError_t e;
+  const unsigned grid = 2 * (unsigned)std::min<long long>(tiles, ctx->sm_count / 2);
   {
     PhaseTimer pt(ctx, PH_LINEAR_GRAD, s);
     auto go = [&](auto path, auto wide) {
       constexpr DyPath P = decltype(path)::value;
-      return launch_early_as(linear_grad_kernel<P, decltype(wide)::value>, grid, LinCfg<P>::threads, LinCfg<P>::smem, 1, s, a, map);
+      return launch_early_as(linear_grad_kernel<P, decltype(wide)::value>, grid, LinCfg<P>::threads, LinCfg<P>::smem, 2, s, a,
+                             dy_map, x_map);
     };
     using Tma = std::integral_constant<DyPath, DY_TMA>;
     using Bf16 = std::integral_constant<DyPath, DY_BF16>;
     using F32 = std::integral_constant<DyPath, DY_F32>;
-    // words of two bf16, vectors of four floats, where every row starts on one
+    // words of two bf16, pairs of floats, where every row starts on one
     const uintptr_t each = address | (uintptr_t)(n > 1 ? ld : 0) * (bf16 ? 2 : 4) | (uintptr_t)(W > 1 ? dy_stride : 0) * (bf16 ? 2 : 4);
-    const bool wide = each % (bf16 ? 4 : 16) == 0;
+    const bool wide = each % (bf16 ? 4 : 8) == 0;
     if (tma) e = go(Tma(), std::true_type());
     else if (bf16) e = wide ? go(Bf16(), std::true_type()) : go(Bf16(), std::false_type());
     else e = wide ? go(F32(), std::true_type()) : go(F32(), std::false_type());
@@ -585,7 +707,7 @@ cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf1
   if (e != cudaSuccess || !split) return e;
   PhaseTimer pt(ctx, PH_LINEAR_JOIN, s);
   return launch_early(linear_join_kernel, dim3((unsigned)((size + 1023) / 1024), (unsigned)W), 256, s,
-                      static_cast<const float*>(workspace), p.slab, p.splits, W, size, layer0, stride, scale, accumulate);
+                      static_cast<const float*>(sums), p.slab, p.splits, W, size, layer0, stride, scale, accumulate);
 }
 
 }  // namespace acc
