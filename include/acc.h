@@ -377,7 +377,7 @@ int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type
  *   bytes of DEVICE memory, 256-byte aligned, caller-owned, for one call at a time; contents before and after do not matter.
  * Device pointers: x, out, dy (element-aligned), code [n][ceil(cols/32)*32] (16-byte aligned), code_scale
  * [n][ceil(cols/32)] (no alignment), tokens [n], grads (16-byte aligned).  n = 0 is allowed; n (gradient: W * n) is at most
- * ACC_MAX_TOKENS, otherwise ACC_EINVAL.  bf16 rows of dy that start on 16 bytes (ld and dy_stride multiples of 8) are the
+ * ACC_MAX_TOKENS, cols at most 2^30, otherwise ACC_EINVAL.  bf16 rows of dy that start on 16 bytes (ld and dy_stride multiples of 8) are the
  * fast way: they are copied to the tensor cores by the copy engine, others by loads.                              */
 #define ACC_CHECKPOINT_BLOCK 32
 int acc_checkpoint_store(acc_ctx* ctx, const void* x, int32_t x_type, int64_t n, int32_t cols, int64_t ld, const void* tokens,

@@ -9,76 +9,32 @@
 
 namespace acc {
 
-constexpr int kBlock = ACC_CHECKPOINT_BLOCK;  // columns that share a scale: four threads of eight
-static_assert(kBlock == 32, "four neighbouring lanes hold a block");
+constexpr int kBlock = ACC_CHECKPOINT_BLOCK;  // columns that share a scale
+static_assert(kBlock == 32, "lanes of a warp hold whole blocks");
 
-// VEC neighbouring elements of a row whose start is aligned to VEC elements (or to 16 bytes), as fp32.
-template <int VEC> __device__ __forceinline__ void load_eight(const float* p, float* v) {
-  if constexpr (VEC == 8) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else if constexpr (VEC >= 2) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 a = *reinterpret_cast<const float2*>(p + 2 * k);
-      v[2 * k] = a.x; v[2 * k + 1] = a.y;
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = p[k];
-  }
-}
-template <int VEC> __device__ __forceinline__ void load_eight(const __nv_bfloat16* p, float* v) {
-  unsigned w[4];
-  if constexpr (VEC == 8) {
-    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
-    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-  } else if constexpr (VEC >= 2) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = reinterpret_cast<const unsigned*>(p)[k];
-  } else {
-    const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = q[2 * k] | (unsigned)q[2 * k + 1] << 16;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[2 * k] = __uint_as_float(w[k] << 16);
-    v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-  }
-}
-template <int VEC> __device__ __forceinline__ void store_eight(float* p, const float* v) {
-  if constexpr (VEC == 8) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-  } else if constexpr (VEC >= 2) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) *reinterpret_cast<float2*>(p + 2 * k) = make_float2(v[2 * k], v[2 * k + 1]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) p[k] = v[k];
-  }
-}
-template <int VEC> __device__ __forceinline__ void store_eight(__nv_bfloat16* p, const float* v) {
-  unsigned w[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-    w[k] = *reinterpret_cast<const unsigned*>(&h);
-  }
-  if constexpr (VEC == 8) {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
-  } else if constexpr (VEC >= 2) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) reinterpret_cast<unsigned*>(p)[k] = w[k];
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      reinterpret_cast<unsigned short*>(p)[2 * k] = (unsigned short)w[k];
-      reinterpret_cast<unsigned short*>(p)[2 * k + 1] = (unsigned short)(w[k] >> 16);
-    }
-  }
-}
+// VEC neighbouring values as loaded and stored: 16 bytes where every row starts on 16, else two, else one.
+template <typename T, int VEC> struct Some;
+template <> struct Some<float, 4> { using type = float4; };
+template <> struct Some<float, 2> { using type = float2; };
+template <> struct Some<float, 1> { using type = float; };
+template <> struct Some<__nv_bfloat16, 8> { using type = uint4; };
+template <> struct Some<__nv_bfloat16, 2> { using type = unsigned; };
+template <> struct Some<__nv_bfloat16, 1> { using type = unsigned short; };
+template <int VEC> struct Codes;
+template <> struct Codes<8> { using type = uint2; };
+template <> struct Codes<4> { using type = unsigned; };
+template <> struct Codes<2> { using type = unsigned short; };
+template <> struct Codes<1> { using type = unsigned char; };
+
+template <typename T, int VEC> union Values {
+  typename Some<T, VEC>::type raw;
+  T each[VEC];
+  __device__ __forceinline__ Values() {}
+};
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_float(float& y, float x) { y = x; }
+__device__ __forceinline__ void from_float(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }
 
 struct CkptArgs {
   void* x;              // [n] rows of ld elements
@@ -86,24 +42,41 @@ struct CkptArgs {
   int cols;
   const void* tokens;   // nullptr, or one per row: rows of negative tokens are zeros and not read
   int token64;
-  uint2* code;          // [n][eights]
+  uint8_t* code;        // [n][32 blocks]
   uint8_t* scale;       // [n][blocks]
-  int eights, blocks;   // of a row: eight columns each, thirty-two each
+  int blocks;           // of a row
+  int units;            // of VEC columns, of a row
+  float inv_units;
 };
 
-// Place of this thread's eight columns; false behind the last row.
-struct CkptPlace { long long row; int eight; };
-__device__ __forceinline__ bool ckpt_place(const CkptArgs& a, int per_block, int k, CkptPlace& p) {
-  // (a block's first place in 64 bits, the rest of the way in 32)
-  const long long base = (long long)blockIdx.x * per_block;
-  const long long row0 = base / a.eights;
-  const unsigned at = (unsigned)(base - row0 * a.eights) + k * blockDim.x + threadIdx.x;
-  p.row = row0 + at / (unsigned)a.eights;
-  p.eight = (int)(at % (unsigned)a.eights);
-  return p.row < a.n;
-}
+// Where a thread's k-th unit lies: units count through the rows, a block of threads takes a stretch of them.  The first of the
+// stretch in 64 bits, the way from there in fp32 (below 2^22, and half a unit away from the next whole number).
+struct CkptPlace {
+  long long row;
+  int unit;
+  template <int UNITS> __device__ __forceinline__ static CkptPlace of(const CkptArgs& a, int k) {
+    const long long base = (long long)blockIdx.x * (blockDim.x * UNITS);
+    const long long row0 = base / a.units;
+    const int from = (int)(base - row0 * a.units), way = k * (int)blockDim.x + (int)threadIdx.x;
+    int at = from + way;
+    CkptPlace p;
+    p.row = row0;
+    if (a.units < (1 << 20)) {
+      const int rows = (int)(((float)at + 0.5f) * a.inv_units);
+      p.row += rows;
+      at -= rows * a.units;
+    } else if (at >= a.units) {  // (a stretch is shorter than such a row)
+      p.row += 1;
+      at -= a.units;
+    }
+    p.unit = at;
+    return p;
+  }
+};
 
-constexpr int kCkptThreads = 256, kCkptUnits = 2;  // units of eight columns a thread
+constexpr int kCkptThreads = 256;
+// Units a thread has under way: 64 bytes and more of x.
+template <int VEC> constexpr int kCkptUnits = VEC == 8 ? 4 : 8;
 
 // Codes and scales of a row.  The scale's byte is the exponent that brings the largest magnitude of the block into [128, 256);
 // values are then exact multiples of a power of two away from x, and rounding to the nearest e4m3 is the only one.
@@ -111,54 +84,63 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(kCkptThreads) checkpoint_store_kernel(const CkptArgs a) {
   await_previous();
   let_next_start();
-  float v[kCkptUnits][8];
-  CkptPlace at[kCkptUnits];
-  bool on[kCkptUnits];
+  constexpr int U = kCkptUnits<VEC>;
+  Values<T, VEC> x[U];
+  CkptPlace at[U];
+  bool live[U];
 #pragma unroll
-  for (int u = 0; u < kCkptUnits; ++u) {
-    on[u] = ckpt_place(a, kCkptThreads * kCkptUnits, u, at[u]);
+  for (int u = 0; u < U; ++u) {
+    at[u] = CkptPlace::of<U>(a, u);
+    live[u] = at[u].row < a.n;
+  }
+  if (a.tokens != nullptr) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[u][k] = 0.f;
-    if (!on[u]) continue;
-    if (a.tokens != nullptr) {
-      const long long t = a.token64 ? static_cast<const long long*>(a.tokens)[at[u].row]
-                                    : static_cast<const int*>(a.tokens)[at[u].row];
-      if (t < 0) continue;
-    }
-    const int c = 8 * at[u].eight;
-    const T* p = static_cast<const T*>(a.x) + at[u].row * a.ld + c;
-    if (c + 8 <= a.cols) {
-      load_eight<VEC>(p, v[u]);
-    } else {
-      for (int k = 0; k < a.cols - c; ++k) {
-        if constexpr (sizeof(T) == 2) v[u][k] = __bfloat162float(p[k]);
-        else v[u][k] = p[k];
-      }
+    for (int u = 0; u < U; ++u)
+      if (live[u]) live[u] = (a.token64 ? static_cast<const long long*>(a.tokens)[at[u].row] : static_cast<const int*>(a.tokens)[at[u].row]) >= 0;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) from_float(x[u].each[k], 0.f);
+    const int c = VEC * at[u].unit;
+    const T* const p = static_cast<const T*>(a.x) + at[u].row * a.ld + c;
+    if (live[u] && c + VEC <= a.cols) {
+      x[u].raw = __ldcs(reinterpret_cast<const typename Some<T, VEC>::type*>(p));
+    } else if (live[u]) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k)
+        if (c + k < a.cols) x[u].each[k] = p[k];
     }
   }
 #pragma unroll
-  for (int u = 0; u < kCkptUnits; ++u) {
+  for (int u = 0; u < U; ++u) {
     // magnitudes compare as integers, NaN and infinity above all
     unsigned top = 0;
+    if constexpr (sizeof(T) == 2 && VEC == 8) {
+      const uint4 w = x[u].raw;
+      const unsigned two = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+      top = max(two << 16, two & 0xffff0000u);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[u][k]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // floor(log2 of the largest) - 7 + 127; 1 where that is less (its factor 2^126 is the largest there is a use for)
-    int byte = top >= 0x7f800000u ? 255 : top == 0 ? 0 : max((int)(top >> 23) - 7, 1);
-    const float factor = __int_as_float((254 - min(byte, 254)) << 23);
-    unsigned w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      unsigned short h;
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(v[u][2 * k + 1] * factor), "f"(v[u][2 * k] * factor));
-      w[k] = h;
+      for (int k = 0; k < VEC; ++k) top = max(top, __float_as_uint(as_float(x[u].each[k])) & 0x7fffffffu);
     }
-    if (!on[u]) continue;
-    uint2 code = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-    if (byte == 255) code = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
-    a.code[at[u].row * a.eights + at[u].eight] = code;
-    if ((at[u].eight & 3) == 0) a.scale[at[u].row * a.blocks + (at[u].eight >> 2)] = (uint8_t)byte;
+#pragma unroll
+    for (int o = 1; o < kBlock / VEC; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    // floor(log2 of the largest) - 7 + 127; 1 where that is less (its factor 2^126 is the largest there is a use for)
+    const int byte = top >= 0x7f800000u ? 255 : top == 0 ? 0 : max((int)(top >> 23) - 7, 1);
+    const float factor = __int_as_float((254 - min(byte, 254)) << 23);
+    union { unsigned char each[VEC]; typename Codes<VEC>::type raw; } code;
+#pragma unroll
+    for (int k = 0; k < VEC; k += 2) {
+      unsigned short h;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(as_float(x[u].each[VEC > 1 ? k + 1 : k]) * factor), "f"(as_float(x[u].each[k]) * factor));
+      if (byte == 255) h = 0x7f7f;
+      code.each[k] = (unsigned char)h;
+      if (VEC > 1) code.each[k + 1] = (unsigned char)(h >> 8);
+    }
+    if (at[u].row >= a.n) continue;
+    *reinterpret_cast<typename Codes<VEC>::type*>(a.code + at[u].row * (a.blocks * kBlock) + VEC * at[u].unit) = code.raw;
+    if (at[u].unit % (kBlock / VEC) == 0) a.scale[at[u].row * a.blocks + at[u].unit / (kBlock / VEC)] = (uint8_t)byte;
   }
 }
 
@@ -171,65 +153,67 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(kCkptThreads) checkpoint_load_kernel(const CkptArgs a) {
   await_previous();
   let_next_start();
-  CkptPlace at[kCkptUnits];
-  bool on[kCkptUnits];
-  uint2 code[kCkptUnits];
-  unsigned byte[kCkptUnits];
+  constexpr int U = kCkptUnits<VEC>;
+  CkptPlace at[U];
+  bool on[U];
+  union { unsigned char each[VEC]; typename Codes<VEC>::type raw; } code[U];
+  unsigned byte[U];
 #pragma unroll
-  for (int u = 0; u < kCkptUnits; ++u) {
-    on[u] = ckpt_place(a, kCkptThreads * kCkptUnits, u, at[u]) && 8 * at[u].eight < a.cols;
+  for (int u = 0; u < U; ++u) {
+    at[u] = CkptPlace::of<U>(a, u);
+    on[u] = at[u].row < a.n && VEC * at[u].unit < a.cols;
     if (!on[u]) continue;
-    code[u] = __ldcs(a.code + at[u].row * a.eights + at[u].eight);
-    byte[u] = a.scale[at[u].row * a.blocks + (at[u].eight >> 2)];
+    code[u].raw = *reinterpret_cast<const typename Codes<VEC>::type*>(a.code + at[u].row * (a.blocks * kBlock) + VEC * at[u].unit);
+    byte[u] = a.scale[at[u].row * a.blocks + at[u].unit / (kBlock / VEC)];
   }
 #pragma unroll
-  for (int u = 0; u < kCkptUnits; ++u) {
+  for (int u = 0; u < U; ++u) {
     if (!on[u]) continue;
     const float s = scale_value(byte[u]);
-    float v[8];
+    Values<T, VEC> y;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const unsigned short h = (unsigned short)((k < 2 ? code[u].x : code[u].y) >> (16 * (k & 1)));
+    for (int k = 0; k < VEC; k += 2) {
+      unsigned short h = code[u].each[k];
+      if (VEC > 1) h |= (unsigned short)(code[u].each[VEC > 1 ? k + 1 : k] << 8);
       unsigned f;
       asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(h));
       const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&f));
-      v[2 * k] = p.x * s;
-      v[2 * k + 1] = p.y * s;
+      from_float(y.each[k], p.x * s);
+      if (VEC > 1) from_float(y.each[VEC > 1 ? k + 1 : k], p.y * s);
     }
-    const int c = 8 * at[u].eight;
-    T* p = static_cast<T*>(a.x) + at[u].row * a.ld + c;
-    if (c + 8 <= a.cols) {
-      store_eight<VEC>(p, v);
+    const int c = VEC * at[u].unit;
+    T* const p = static_cast<T*>(a.x) + at[u].row * a.ld + c;
+    if (c + VEC <= a.cols) {
+      *reinterpret_cast<typename Some<T, VEC>::type*>(p) = y.raw;
     } else {
-      for (int k = 0; k < a.cols - c; ++k) {
-        if constexpr (sizeof(T) == 2) p[k] = __float2bfloat16_rn(v[k]);
-        else p[k] = v[k];
-      }
+#pragma unroll
+      for (int k = 0; k < VEC; ++k)
+        if (c + k < a.cols) p[k] = y.each[k];
     }
   }
-}
-
-// Widest access at which every eight columns of every row start aligned: 8 elements (16 bytes at least), 2, or 1.
-static int ckpt_vec(const void* x, long long n, long long ld, int size) {
-  const uintptr_t at = reinterpret_cast<uintptr_t>(x) | (n > 1 ? (uintptr_t)(ld * size) : 0);
-  return at % 16 == 0 ? 8 : at % (2 * size) == 0 ? 2 : 1;
 }
 
 cudaError_t launch_checkpoint(acc_ctx* ctx, bool store, void* x, bool bf16, long long n, int cols, long long ld,
                               const void* tokens, bool tok64, uint8_t* code, uint8_t* scale, cudaStream_t s) {
   const int blocks = (cols + kBlock - 1) / kBlock;
-  const CkptArgs a{x, n, ld, cols, tokens, tok64, reinterpret_cast<uint2*>(code), scale, 4 * blocks, blocks};
-  const long long units = n * a.eights, per = kCkptThreads * kCkptUnits;
-  const int vec = ckpt_vec(x, n, ld, bf16 ? 2 : 4);
+  CkptArgs a{x, n, ld, cols, tokens, tok64, code, scale, blocks, 0, 0.f};
+  // 16 bytes where every row starts on 16 (and no row's last vector is read or written whole unless it is), two elements, or one
+  const int size = bf16 ? 2 : 4;
+  const uintptr_t each = reinterpret_cast<uintptr_t>(x) | (n > 1 ? (uintptr_t)(ld * size) : 0);
+  const int vec = each % 16 == 0 ? 16 / size : each % (2 * size) == 0 ? 2 : 1;
+  a.units = blocks * (kBlock / vec);
+  a.inv_units = 1.f / (float)a.units;
   PhaseTimer pt(ctx, store ? PH_CKPT_STORE : PH_CKPT_LOAD, s);
   auto go = [&](auto t, auto v) {
     using T = decltype(t);
     constexpr int VEC = decltype(v)::value;
+    const long long per = kCkptThreads * kCkptUnits<VEC>, all = n * a.units;
     return launch_early(store ? checkpoint_store_kernel<T, VEC> : checkpoint_load_kernel<T, VEC>,
-                        (unsigned)((units + per - 1) / per), kCkptThreads, s, a);
+                        (unsigned)((all + per - 1) / per), kCkptThreads, s, a);
   };
   auto typed = [&](auto t) {
-    if (vec == 8) return go(t, std::integral_constant<int, 8>());
+    using T = decltype(t);
+    if (vec > 2) return go(t, std::integral_constant<int, 16 / (int)sizeof(T)>());
     return vec == 2 ? go(t, std::integral_constant<int, 2>()) : go(t, std::integral_constant<int, 1>());
   };
   return bf16 ? typed(__nv_bfloat16()) : typed(0.f);

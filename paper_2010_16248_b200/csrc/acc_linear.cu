@@ -18,6 +18,7 @@ namespace acc {
 constexpr int kM = 128, kK = 64;
 constexpr int kBoxBytes = 64 * 128;
 constexpr int kABytes = kM / 64 * kBoxBytes;
+constexpr int kEpiPitch = 41;  // floats of a row of 8 + 32 finished sums, odd: a column's 32 rows lie in 32 banks
 enum { kEpiWarps = 8, kMmaWarp = 8, kDyWarp = 9, kXWarp = 10, kLoadWarp = 12, kLoadWarps = 8 };
 
 // How dy reaches shared memory: bf16 by tensor copies, or (rows that do not start on 16 bytes; fp32) by loads.
@@ -30,12 +31,9 @@ template <DyPath P> struct LinCfg {
   static constexpr int n = P == DY_TMA ? 256 : 128;
   static constexpr int b_bytes = n / 128 * kBoxBytes;
   static constexpr int stage = kABytes * parts + b_bytes;
-  static constexpr int stages = P == DY_F32 ? 3 : 6;
+  static constexpr int stages = P == DY_F32 ? 3 : P == DY_BF16 ? 6 : 5;
   static constexpr int threads = 32 * (P == DY_TMA ? kLoadWarp : kLoadWarp + kLoadWarps);
-  // Finished sums pass through shared memory, eight rows of each quarter at a time; a pitch that spreads eight rows' 16 bytes over
-  // all banks
-  static constexpr int pitch = n + 4;
-  static constexpr int smem = stages * stage + 4 * 8 * pitch * 4 + 1024;
+  static constexpr int smem = stages * stage + kEpiWarps * 32 * kEpiPitch * 4 + 1024;
   // Registers a thread: the sums' warps take what the others give back, within what the block was launched with.
   static constexpr int launch_regs = P == DY_TMA ? 168 : 96, epi_regs = P == DY_TMA ? 216 : 128, mma_regs = P == DY_TMA ? 56 : 40, load_regs = 88;
   static_assert(kEpiWarps * epi_regs + 4 * mma_regs + (threads / 32 - kLoadWarp) * load_regs <= threads / 32 * launch_regs, "");
@@ -168,45 +166,57 @@ __device__ __forceinline__ bool lin_wait(uint64_t* bar, unsigned parity, int* st
   return false;
 }
 
-// The two warps that share a quarter of the rows.
-__device__ __forceinline__ void quarter_sync(int quarter) { asm volatile("bar.sync %0, 64;" ::"r"(quarter + 1) : "memory"); }
-
-__device__ __forceinline__ bool quarter_all(int quarter, bool ok) {
-  unsigned all;
-  asm volatile(
-      "{\n"
-      "  .reg .pred p, q;\n"
-      "  setp.ne.u32 p, %2, 0;\n"
-      "  barrier.red.and.pred q, %1, 64, p;\n"
-      "  selp.u32 %0, 1, 0, q;\n"
-      "}\n"
-      : "=r"(all)
-      : "r"(quarter + 1), "r"((unsigned)ok)
-      : "memory");
-  return all != 0;
-}
-
-// Up to four rows of finished sums, `cols` columns each, to or onto rows of the layer.  A lane's columns count from the last
-// multiple of 32 bytes before the row's first, so that a store covers whole sectors of memory whatever the row's start: rows of
-// 650 columns, which start at any multiple of 8 bytes, go out at 4.2 TB/s, and at 2.5 with lanes counted from the first column.
-template <int N, int PITCH, bool ADD>
-__device__ __forceinline__ void write_rows(const float* buf, float* out, int ld, int cols, int rows, int lane) {
-  constexpr int kPlaces = N / 32 + 1;
+// A warp's 32 rows of finished sums, `cols` columns of each lane's row held[], times scale, to or onto rows of the layer.  Blocks of
+// 32 columns turn in shared memory.  A row may start at any element, and a store that ends inside 32 bytes of memory costs as
+// much as two: so a row's block begins up to seven columns early, where 32 bytes do, and the block before leaves those to it.
+// Rows eight apart start at the same place within 32 bytes and go together, one address for four of them.  (Rows of 650 columns,
+// the writing alone: 2.5 TB/s with blocks from the first column, 3.9 with an address each, 5.2 so.)
+// The code stays small -- one copy of the part that writes, for all blocks --: unrolled, it cost 30 us of 300 in instruction fetches.
+template <bool ADD, bool WHOLE>
+__device__ __forceinline__ void write_block(uint32_t at, float* out, int start, int ld, int c, int cols, int rows, int lane) {
+  const long long step = 8ll * ld;
+#pragma unroll WHOLE ? 8 : 1
+  for (int k = 0; k < 8; ++k) {
+    const int early = (start + k * ld) & 7, col = c - early + lane;
+    if ((unsigned)col >= (unsigned)cols) continue;
+    const uint32_t from = at + 4 * (k * kEpiPitch + 8 - early + lane);
+    float* p = out + (long long)k * ld + col;
+    float v[4], old[4];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (r >= rows) break;
-    float* const p = out + (long long)r * ld;
-    const int first = lane - (int)((reinterpret_cast<uintptr_t>(p) >> 2) & 7);
-    float v[kPlaces], old[kPlaces];
-#pragma unroll
-    for (int w = 0; w < kPlaces; ++w) {
-      const bool on = (unsigned)(first + 32 * w) < (unsigned)cols;
-      v[w] = on ? buf[r * PITCH + first + 32 * w] : 0.f;
-      if (ADD) old[w] = on ? p[first + 32 * w] : 0.f;
+    for (int r = 0; r < 4; ++r) {
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[r]) : "r"(from + 4 * 8 * r * kEpiPitch));
+      if (ADD && (WHOLE || k + 8 * r < rows)) old[r] = p[r * step];
     }
 #pragma unroll
-    for (int w = 0; w < kPlaces; ++w)
-      if ((unsigned)(first + 32 * w) < (unsigned)cols) p[first + 32 * w] = ADD ? old[w] + v[w] : v[w];
+    for (int r = 0; r < 4; ++r) {
+      if (WHOLE || k + 8 * r < rows) *p = ADD ? old[r] + v[r] : v[r];
+      p += step;
+    }
+  }
+}
+template <int HELD>
+__device__ __forceinline__ void write_rows(const float (&held)[HELD], float scale, bool add, float* buf, float* out, int ld, int cols,
+                                           int rows, int lane) {
+  const int start = (int)(reinterpret_cast<uintptr_t>(out) >> 2);
+  const uint32_t at = smem_u32(buf);
+#pragma unroll 1
+  for (int c = 0; c <= HELD && c - 7 < cols; c += 32) {
+#pragma unroll
+    for (int b = 0; b <= HELD; b += 32) {
+      if (b != c) continue;
+#pragma unroll
+      for (int j = b > 0 ? 0 : 8; j < (b < HELD ? 40 : 8); ++j)
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * (lane * kEpiPitch + j)), "f"(held[b - 8 + j] * scale) : "memory");
+    }
+    __syncwarp();
+    if (rows == 32) {
+      if (add) write_block<true, true>(at, out, start, ld, c, cols, rows, lane);
+      else write_block<false, true>(at, out, start, ld, c, cols, rows, lane);
+    } else {
+      if (add) write_block<true, false>(at, out, start, ld, c, cols, rows, lane);
+      else write_block<false, false>(at, out, start, ld, c, cols, rows, lane);
+    }
+    __syncwarp();
   }
 }
 
@@ -352,8 +362,8 @@ __device__ __forceinline__ void load_pairs(const LinArgs& a, StepWalk walk, cons
   }
 }
 
-// The blocks of a pair walk over the tiles.  In each, warps 0-7 add up and write the sums of its 128 rows, two warps for each
-// quarter of them, warps 9 and 10 issue the copies of dy and of the checkpoint, and where dy cannot be copied eight more warps
+// The blocks of a pair walk over the tiles.  In each, warps 0-7 add up and write the sums of its 128 rows, two warps (half of
+// the columns each) for each quarter of them, warps 9 and 10 issue the copies of dy and of the checkpoint, and where dy cannot be copied eight more warps
 // load it; the first block's warp 8 issues the products of both.  Two sums in tensor memory: one is read while the other grows.
 template <DyPath P, bool WIDE>
 __global__ void __launch_bounds__(LinCfg<P>::threads, 1)
@@ -393,7 +403,7 @@ linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, 
     more_registers<Cfg::epi_regs>();
     constexpr int kHeld = Cfg::n / 2;  // columns of a lane's row
     const int quarter = warp & 3, side = warp >> 2;
-    float* const buf = reinterpret_cast<float*>(stages + S * Cfg::stage) + quarter * 8 * Cfg::pitch;
+    float* const buf = reinterpret_cast<float*>(stages + S * Cfg::stage) + warp * 32 * kEpiPitch;
     const uint32_t held_at = tmem + side * half + ((uint32_t)(quarter * 32) << 16);
     unsigned sum = 0;
     bool ok = true;
@@ -421,29 +431,13 @@ linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, 
       int chunks = lin_chunks<Cfg::chunk>(lin_tile(a, t));
       take(std::false_type());
       while (--chunks > 0 && ok) take(std::true_type());
-      // (a quarter's warps give up together: neither waits for the other where it writes)
-      if (!(ok = quarter_all(quarter, ok))) break;
+      if (!ok) break;
       const LinTile x = lin_tile(a, t);
-      const int row0 = x.m * 2 * kM + rank * kM + quarter * 32, n0 = x.n * a.tile_n;
+      const int row0 = x.m * 2 * kM + rank * kM + quarter * 32, n0 = x.n * a.tile_n + side * half;
       float* const out = a.out + ((long long)x.split * a.W + x.w) * a.out_stride + (long long)row0 * a.cols + n0;
-      const int rows = min(32, a.rows - row0), cols = min(a.tile_n, a.cols - n0);
-#pragma unroll 1
-      for (int g = 0; g < 32 && g < rows; g += 8) {
-        if ((lane & 24) == g) {
-          float* const line = buf + (lane & 7) * Cfg::pitch + side * half;
-#pragma unroll
-          for (int c = 0; c < kHeld; c += 4)
-            if (c < half)
-              *reinterpret_cast<float4*>(line + c) =
-                  make_float4(held[c] * a.scale, held[c + 1] * a.scale, held[c + 2] * a.scale, held[c + 3] * a.scale);
-        }
-        quarter_sync(quarter);
-        const float* const from = buf + 4 * side * Cfg::pitch;
-        float* const to = out + (long long)(g + 4 * side) * a.cols;
-        if (a.accumulate) write_rows<Cfg::n, Cfg::pitch, true>(from, to, a.cols, cols, rows - g - 4 * side, lane);
-        else write_rows<Cfg::n, Cfg::pitch, false>(from, to, a.cols, cols, rows - g - 4 * side, lane);
-        quarter_sync(quarter);
-      }
+      const int rows = min(32, a.rows - row0), cols = min(half, a.cols - n0);
+      if (rows <= 0 || cols <= 0) continue;  // (a tile may end inside the other warp's half)
+      write_rows<kHeld>(held, a.scale, a.accumulate, buf, out, a.cols, cols, rows, lane);
     }
   } else if (warp < kLoadWarp) {
     fewer_registers<Cfg::mma_regs>();
