@@ -626,7 +626,7 @@ static int checkpoint(acc_ctx* ctx, bool store, void* x, int type, int64_t n, in
                       int token_type, uint8_t* code, uint8_t* scale, void* stream) {
   if (!ctx || !known_value(type) || !known_token(token_type) || !rows_fit(n, cols, ld)) return ACC_EINVAL;
   if (n > 0 && (!x || !code || !scale)) return ACC_EINVAL;
-  if (cols > (1 << 30) || n * ((cols + 31ll) / 32 * 32) / 2048 >= kMostBlocks) return ACC_EINVAL;
+  if (cols > (1 << 30) || n * ((cols + 31ll) / 32 * 8 + 1) / 1024 >= kMostBlocks - 1) return ACC_EINVAL;
   if (!aligned_to(x, value_size(type)) || !aligned_to(tokens, token_size(token_type)) || !aligned16(code)) return ACC_EALIGN;
   ctx->last_launches = 0;
   if (n == 0) return ACC_OK;

@@ -10,31 +10,12 @@
 namespace acc {
 
 constexpr int kBlock = ACC_CHECKPOINT_BLOCK;  // columns that share a scale
-static_assert(kBlock == 32, "lanes of a warp hold whole blocks");
+static_assert(kBlock == 32, "two lanes of sixteen columns hold a block");
 
-// VEC neighbouring values as loaded and stored: 16 bytes where every row starts on 16, else two, else one.
-template <typename T, int VEC> struct Some;
-template <> struct Some<float, 4> { using type = float4; };
-template <> struct Some<float, 2> { using type = float2; };
-template <> struct Some<float, 1> { using type = float; };
-template <> struct Some<__nv_bfloat16, 8> { using type = uint4; };
-template <> struct Some<__nv_bfloat16, 2> { using type = unsigned; };
-template <> struct Some<__nv_bfloat16, 1> { using type = unsigned short; };
-template <int VEC> struct Codes;
-template <> struct Codes<8> { using type = uint2; };
-template <> struct Codes<4> { using type = unsigned; };
-template <> struct Codes<2> { using type = unsigned short; };
-template <> struct Codes<1> { using type = unsigned char; };
-
-template <typename T, int VEC> union Values {
-  typename Some<T, VEC>::type raw;
-  T each[VEC];
-  __device__ __forceinline__ Values() {}
-};
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_float(float& y, float x) { y = x; }
-__device__ __forceinline__ void from_float(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }
+__device__ __forceinline__ unsigned as_bits(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ unsigned as_bits(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
 
 struct CkptArgs {
   void* x;              // [n] rows of ld elements
@@ -45,8 +26,9 @@ struct CkptArgs {
   uint8_t* code;        // [n][32 blocks]
   uint8_t* scale;       // [n][blocks]
   int blocks;           // of a row
-  int units;            // of VEC columns, of a row
+  int units;            // of a row
   float inv_units;
+  const char *first, *end;  // the rows' bytes
 };
 
 // Where a thread's k-th unit lies: units count through the rows, a block of threads takes a stretch of them.  The first of the
@@ -75,17 +57,59 @@ struct CkptPlace {
 };
 
 constexpr int kCkptThreads = 256;
-// Units a thread has under way: 64 bytes and more of x.
-template <int VEC> constexpr int kCkptUnits = VEC == 8 ? 4 : 8;
+// Units a thread has under way, at least 64 bytes of x.
+template <typename T> constexpr int kStoreUnits = 4 / (int)sizeof(T);
+constexpr int kLoadUnits = 4;
 
-// Codes and scales of a row.  The scale's byte is the exponent that brings the largest magnitude of the block into [128, 256);
-// values are then exact multiples of a power of two away from x, and rounding to the nearest e4m3 is the only one.
-template <typename T, int VEC>
+// The bits of sixteen neighbouring values of a row, columns behind the row zeros: WORDS words.  ROWS16: every row starts on 16
+// bytes.  Otherwise the 16-byte pieces around the values are loaded -- inside the rows' bytes, so at their first and last the values
+// come one by one -- and moved by whole words, then by half of one.
+template <typename T> constexpr int kWords = 16 * (int)sizeof(T) / 4;
+template <typename T, bool ROWS16>
+__device__ __forceinline__ void load_sixteen(const CkptArgs& a, long long row, int c, unsigned* w) {
+  constexpr int N = kWords<T>;
+  const T* const p = static_cast<const T*>(a.x) + row * a.ld + c;
+  const char* const at = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+  const int by = ROWS16 ? 0 : (int)(reinterpret_cast<uintptr_t>(p) & 15);
+  if (c + 16 <= a.cols && (by == 0 || (at >= a.first && at + 4 * N + 16 <= a.end))) {
+    unsigned v[N + 4];
+#pragma unroll
+    for (int k = 0; k < N / 4 + 1; ++k) {
+      if (k == N / 4 && by == 0) break;
+      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(at) + k);
+      v[4 * k] = x.x; v[4 * k + 1] = x.y; v[4 * k + 2] = x.z; v[4 * k + 3] = x.w;
+    }
+    if (!ROWS16 && by != 0) {
+#pragma unroll
+      for (int k = 0; k < N + 3; ++k) v[k] = by & 4 ? v[k + 1] : v[k];
+#pragma unroll
+      for (int k = 0; k < N + 1; ++k) v[k] = by & 8 ? v[k + 2] : v[k];
+      if (sizeof(T) == 2) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = by & 2 ? __funnelshift_r(v[k], v[k + 1], 16) : v[k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[k] = v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const unsigned b = c + k < a.cols ? as_bits(p[k]) : 0u;
+      if (sizeof(T) == 4) w[k] = b;
+      else w[k / 2] = k & 1 ? w[k / 2] | b << 16 : b;
+    }
+  }
+}
+
+// Codes and scales of a row, sixteen columns a thread.  The scale's byte is the exponent that brings the largest magnitude of the
+// block into [128, 256); values are then exact multiples of a power of two away from x, and rounding to the nearest e4m3 is the
+// only one.
+template <typename T, bool ROWS16>
 __global__ void __launch_bounds__(kCkptThreads) checkpoint_store_kernel(const CkptArgs a) {
   await_previous();
   let_next_start();
-  constexpr int U = kCkptUnits<VEC>;
-  Values<T, VEC> x[U];
+  constexpr int U = kStoreUnits<T>, N = kWords<T>;
+  unsigned w[U][N];
   CkptPlace at[U];
   bool live[U];
 #pragma unroll
@@ -101,46 +125,38 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_store_kernel(const Ck
 #pragma unroll
   for (int u = 0; u < U; ++u) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) from_float(x[u].each[k], 0.f);
-    const int c = VEC * at[u].unit;
-    const T* const p = static_cast<const T*>(a.x) + at[u].row * a.ld + c;
-    if (live[u] && c + VEC <= a.cols) {
-      x[u].raw = __ldcs(reinterpret_cast<const typename Some<T, VEC>::type*>(p));
-    } else if (live[u]) {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k)
-        if (c + k < a.cols) x[u].each[k] = p[k];
-    }
+    for (int k = 0; k < N; ++k) w[u][k] = 0;
+    if (live[u]) load_sixteen<T, ROWS16>(a, at[u].row, 16 * at[u].unit, w[u]);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     // magnitudes compare as integers, NaN and infinity above all
     unsigned top = 0;
-    if constexpr (sizeof(T) == 2 && VEC == 8) {
-      const uint4 w = x[u].raw;
-      const unsigned two = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
-      top = max(two << 16, two & 0xffff0000u);
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) top = __vmaxu2(top, w[u][k] & 0x7fff7fffu);
+      top = max(top << 16, top & 0xffff0000u);
     } else {
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) top = max(top, __float_as_uint(as_float(x[u].each[k])) & 0x7fffffffu);
+      for (int k = 0; k < N; ++k) top = max(top, w[u][k] & 0x7fffffffu);
     }
-#pragma unroll
-    for (int o = 1; o < kBlock / VEC; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     // floor(log2 of the largest) - 7 + 127; 1 where that is less (its factor 2^126 is the largest there is a use for)
-    const int byte = top >= 0x7f800000u ? 255 : top == 0 ? 0 : max((int)(top >> 23) - 7, 1);
-    const float factor = __int_as_float((254 - min(byte, 254)) << 23);
-    union { unsigned char each[VEC]; typename Codes<VEC>::type raw; } code;
+    const bool odd = top >= 0x7f800000u;
+    const int byte = odd ? 255 : top == 0 ? 0 : max((int)(top >> 23) - 7, 1);
+    const float factor = __uint_as_float(odd ? 0x7fffffffu : (unsigned)(254 - byte) << 23);  // (NaN makes every code NaN)
+    unsigned code[4];
 #pragma unroll
-    for (int k = 0; k < VEC; k += 2) {
+    for (int k = 0; k < 8; ++k) {
+      const float lo = sizeof(T) == 2 ? __uint_as_float(w[u][k % N] << 16) : __uint_as_float(w[u][(2 * k) % N]);
+      const float hi = sizeof(T) == 2 ? __uint_as_float(w[u][k % N] & 0xffff0000u) : __uint_as_float(w[u][(2 * k + 1) % N]);
       unsigned short h;
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(as_float(x[u].each[VEC > 1 ? k + 1 : k]) * factor), "f"(as_float(x[u].each[k]) * factor));
-      if (byte == 255) h = 0x7f7f;
-      code.each[k] = (unsigned char)h;
-      if (VEC > 1) code.each[k + 1] = (unsigned char)(h >> 8);
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(hi * factor), "f"(lo * factor));
+      code[k / 2] = k & 1 ? code[k / 2] | (unsigned)h << 16 : h;
     }
     if (at[u].row >= a.n) continue;
-    *reinterpret_cast<typename Codes<VEC>::type*>(a.code + at[u].row * (a.blocks * kBlock) + VEC * at[u].unit) = code.raw;
-    if (at[u].unit % (kBlock / VEC) == 0) a.scale[at[u].row * a.blocks + at[u].unit / (kBlock / VEC)] = (uint8_t)byte;
+    *reinterpret_cast<uint4*>(a.code + at[u].row * (a.blocks * kBlock) + 16 * at[u].unit) = make_uint4(code[0], code[1], code[2], code[3]);
+    if ((at[u].unit & 1) == 0) a.scale[at[u].row * a.blocks + (at[u].unit >> 1)] = (uint8_t)byte;
   }
 }
 
@@ -149,74 +165,105 @@ __device__ __forceinline__ float scale_value(unsigned byte) {
   return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fffffffu : byte << 23);
 }
 
-template <typename T, int VEC>
+// The values, 16 bytes of them a thread: V columns from column V * unit, or (rows that start anywhere) those that lie in one
+// 16-byte piece of memory, whose codes start at any byte and may belong to two blocks.
+template <typename T, bool ROWS16>
 __global__ void __launch_bounds__(kCkptThreads) checkpoint_load_kernel(const CkptArgs a) {
   await_previous();
   let_next_start();
-  constexpr int U = kCkptUnits<VEC>;
+  constexpr int U = kLoadUnits, V = 16 / (int)sizeof(T);
   CkptPlace at[U];
-  bool on[U];
-  union { unsigned char each[VEC]; typename Codes<VEC>::type raw; } code[U];
-  unsigned byte[U];
+  int c[U];              // first column, negative where the piece begins before the row
+  unsigned code[U][2], byte[U][2];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     at[u] = CkptPlace::of<U>(a, u);
-    on[u] = at[u].row < a.n && VEC * at[u].unit < a.cols;
-    if (!on[u]) continue;
-    code[u].raw = *reinterpret_cast<const typename Codes<VEC>::type*>(a.code + at[u].row * (a.blocks * kBlock) + VEC * at[u].unit);
-    byte[u] = a.scale[at[u].row * a.blocks + at[u].unit / (kBlock / VEC)];
+    c[u] = V * at[u].unit;
+    if (!ROWS16) c[u] -= (int)(reinterpret_cast<uintptr_t>(static_cast<const T*>(a.x) + at[u].row * a.ld) % 16 / sizeof(T));
+    if (at[u].row >= a.n) c[u] = a.cols;
+    if (c[u] >= a.cols) continue;
+    const uint8_t* const codes = a.code + at[u].row * (a.blocks * kBlock);
+    const uint8_t* const scales = a.scale + at[u].row * a.blocks;
+    if (ROWS16) {
+      if (V == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(codes + c[u]);
+        code[u][0] = x.x;
+        code[u][1] = x.y;
+      } else {
+        code[u][0] = *reinterpret_cast<const unsigned*>(codes + c[u]);
+      }
+      byte[u][0] = byte[u][1] = scales[c[u] / kBlock];
+    } else {
+      const int from = c[u] & ~3, by = 8 * (c[u] & 3);  // (columns below 0 or behind the codes: anything)
+      unsigned w[V / 4 + 1];
+#pragma unroll
+      for (int k = 0; k < V / 4 + 1; ++k)
+        w[k] = from + 4 * k >= 0 && from + 4 * k < a.blocks * kBlock ? *reinterpret_cast<const unsigned*>(codes + from + 4 * k) : 0u;
+#pragma unroll
+      for (int k = 0; k < V / 4; ++k) code[u][k] = __funnelshift_r(w[k], w[k + 1], by);
+      byte[u][0] = scales[max(c[u], 0) / kBlock];
+      byte[u][1] = scales[min(c[u] + V - 1, a.cols - 1) / kBlock];
+    }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (!on[u]) continue;
-    const float s = scale_value(byte[u]);
-    Values<T, VEC> y;
+    if (c[u] >= a.cols) continue;
+    const float s0 = scale_value(byte[u][0]), s1 = scale_value(byte[u][1]);
+    const int turn = ROWS16 ? V : kBlock - (c[u] & (kBlock - 1));  // values before the second block
+    float v[V];
 #pragma unroll
-    for (int k = 0; k < VEC; k += 2) {
-      unsigned short h = code[u].each[k];
-      if (VEC > 1) h |= (unsigned short)(code[u].each[VEC > 1 ? k + 1 : k] << 8);
+    for (int k = 0; k < V; k += 2) {
+      const unsigned short h = (unsigned short)(code[u][k / 4] >> (8 * (k & 2)));
       unsigned f;
       asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"(h));
       const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&f));
-      from_float(y.each[k], p.x * s);
-      if (VEC > 1) from_float(y.each[VEC > 1 ? k + 1 : k], p.y * s);
+      v[k] = p.x * (k < turn ? s0 : s1);
+      v[k + 1] = p.y * (k + 1 < turn ? s0 : s1);
     }
-    const int c = VEC * at[u].unit;
-    T* const p = static_cast<T*>(a.x) + at[u].row * a.ld + c;
-    if (c + VEC <= a.cols) {
-      *reinterpret_cast<typename Some<T, VEC>::type*>(p) = y.raw;
+    T* const p = static_cast<T*>(a.x) + at[u].row * a.ld + c[u];
+    if (c[u] >= 0 && c[u] + V <= a.cols) {
+      uint4 y;
+      if constexpr (V == 8) {
+        unsigned w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+          w[k] = *reinterpret_cast<const unsigned*>(&h);
+        }
+        y = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        y = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      }
+      *reinterpret_cast<uint4*>(p) = y;
     } else {
 #pragma unroll
-      for (int k = 0; k < VEC; ++k)
-        if (c + k < a.cols) p[k] = y.each[k];
+      for (int k = 0; k < V; ++k) {
+        if (c[u] + k < 0 || c[u] + k >= a.cols) continue;
+        if constexpr (V == 8) p[k] = __float2bfloat16_rn(v[k]);
+        else p[k] = v[k];
+      }
     }
   }
 }
 
 cudaError_t launch_checkpoint(acc_ctx* ctx, bool store, void* x, bool bf16, long long n, int cols, long long ld,
                               const void* tokens, bool tok64, uint8_t* code, uint8_t* scale, cudaStream_t s) {
-  const int blocks = (cols + kBlock - 1) / kBlock;
-  CkptArgs a{x, n, ld, cols, tokens, tok64, code, scale, blocks, 0, 0.f};
-  // 16 bytes where every row starts on 16 (and no row's last vector is read or written whole unless it is), two elements, or one
-  const int size = bf16 ? 2 : 4;
-  const uintptr_t each = reinterpret_cast<uintptr_t>(x) | (n > 1 ? (uintptr_t)(ld * size) : 0);
-  const int vec = each % 16 == 0 ? 16 / size : each % (2 * size) == 0 ? 2 : 1;
-  a.units = blocks * (kBlock / vec);
+  const int blocks = (cols + kBlock - 1) / kBlock, size = bf16 ? 2 : 4;
+  const char* const first = static_cast<const char*>(x);
+  CkptArgs a{x, n, ld, cols, tokens, tok64, code, scale, blocks, 0, 0.f, first, first + ((n - 1) * ld + cols) * size};
+  const bool rows16 = (reinterpret_cast<uintptr_t>(x) | (n > 1 ? (uintptr_t)(ld * size) : 0)) % 16 == 0;
+  // a row's pieces of 16 bytes of output are one more where it starts inside one
+  a.units = store ? 2 * blocks : (cols + 16 / size - 1) / (16 / size) + !rows16;
   a.inv_units = 1.f / (float)a.units;
   PhaseTimer pt(ctx, store ? PH_CKPT_STORE : PH_CKPT_LOAD, s);
-  auto go = [&](auto t, auto v) {
+  auto go = [&](auto t) {
     using T = decltype(t);
-    constexpr int VEC = decltype(v)::value;
-    const long long per = kCkptThreads * kCkptUnits<VEC>, all = n * a.units;
-    return launch_early(store ? checkpoint_store_kernel<T, VEC> : checkpoint_load_kernel<T, VEC>,
-                        (unsigned)((all + per - 1) / per), kCkptThreads, s, a);
+    const long long per = kCkptThreads * (store ? kStoreUnits<T> : kLoadUnits), all = n * a.units;
+    auto* kernel = store ? (rows16 ? checkpoint_store_kernel<T, true> : checkpoint_store_kernel<T, false>)
+                         : (rows16 ? checkpoint_load_kernel<T, true> : checkpoint_load_kernel<T, false>);
+    return launch_early(kernel, (unsigned)((all + per - 1) / per), kCkptThreads, s, a);
   };
-  auto typed = [&](auto t) {
-    using T = decltype(t);
-    if (vec > 2) return go(t, std::integral_constant<int, 16 / (int)sizeof(T)>());
-    return vec == 2 ? go(t, std::integral_constant<int, 2>()) : go(t, std::integral_constant<int, 1>());
-  };
-  return bf16 ? typed(__nv_bfloat16()) : typed(0.f);
+  return bf16 ? go(__nv_bfloat16()) : go(0.f);
 }
 
 }  // namespace acc
