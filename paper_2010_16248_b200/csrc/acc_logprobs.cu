@@ -23,6 +23,31 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
+// The same of two pairs of bf16, of the lanes of a warp.
+__device__ __forceinline__ unsigned max2(unsigned a, unsigned b) {
+  unsigned y;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+__device__ __forceinline__ float max_warp(float a) {
+  float y;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(a));
+  return y;
+}
+// Two fp32 operations at once.
+union Pair { float2 f; unsigned long long u; };
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  Pair x, y, z, r;
+  x.f = a; y.f = b; z.f = c;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(x.u), "l"(y.u), "l"(z.u));
+  return r.f;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  Pair x, y, r;
+  x.f = a; y.f = b;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(x.u), "l"(y.u));
+  return r.f;
+}
 constexpr float kMinusInf = -__builtin_huge_valf();
 __device__ __forceinline__ float not_a_number() { return __int_as_float(0x7fffffff); }
 
@@ -35,6 +60,16 @@ template <> struct Eight<__nv_bfloat16> {
   uint4 a;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void fill_minus_inf() { a = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+  // The largest of the eight, NaN when one of them is; and the eight as pairs, none below `least`.
+  __device__ __forceinline__ float largest() const {
+    const unsigned m = max2(max2(a.x, a.y), max2(a.z, a.w));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+  __device__ __forceinline__ void pairs(float2* v, float least) const {
+    const unsigned l = __float_as_uint(least) >> 16, l2 = l | l << 16, w[4] = {max2(a.x, l2), max2(a.y, l2), max2(a.z, l2), max2(a.w, l2)};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+  }
   __device__ __forceinline__ void get(float* v) const {
     const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -61,6 +96,13 @@ template <> struct Eight<float> {
     b = *reinterpret_cast<const float4*>(p + 4);
   }
   __device__ __forceinline__ void fill_minus_inf() { a = b = make_float4(kMinusInf, kMinusInf, kMinusInf, kMinusInf); }
+  __device__ __forceinline__ float largest() const {
+    return max_nan(max_nan(max_nan(a.x, a.y), max_nan(a.z, a.w)), max_nan(max_nan(b.x, b.y), max_nan(b.z, b.w)));
+  }
+  __device__ __forceinline__ void pairs(float2* v, float least) const {
+    v[0] = make_float2(max_nan(a.x, least), max_nan(a.y, least)); v[1] = make_float2(max_nan(a.z, least), max_nan(a.w, least));
+    v[2] = make_float2(max_nan(b.x, least), max_nan(b.y, least)); v[3] = make_float2(max_nan(b.z, least), max_nan(b.w, least));
+  }
   __device__ __forceinline__ void get(float* v) const {
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
   }
@@ -91,73 +133,116 @@ struct RowSpan {
   }
 };
 
-// The running statistics of a set of logits z: m = max z, s = sum 2^d, t = sum 2^d d with d = (z - m) * scale * log2(e).  A
-// distance below -200 counts as -200, where 2^d is 0: -inf and the type's lowest value then add nothing, not 0 * inf.
+// The running statistics of a set of logits z with largest m: s = sum 2^d, t = sum 2^d d.  d = z c2 - ref(m), one rounding, with
+// c2 = scale log2(e) and ref(m) = m c2 rounded, which the row's end puts right: 2^(m c2 - ref(m)) is known to all its bits.
+// Where m c2 nears fp32's range (a row of the type's lowest value) d = (z - m) c2 instead.  A distance below -200 counts as
+// -200, where 2^d is 0: -inf and the type's lowest value then add nothing, not 0 * inf.
+struct Scale {
+  float c2, limit, least;  // |m| below limit has a ref; a logit below `least` counts as `least`: its 2^d is 0, and d finite
+  static Scale of(float scale) {
+    const float c2 = scale * kLog2e;
+    return {c2, 0x1p100f / c2, -0x1p120f / c2};
+  }
+  __device__ __forceinline__ bool near(float m) const { return fabsf(m) < limit; }
+  __device__ __forceinline__ float ref(float m) const { return __fmul_rn(m, c2); }  // (never part of an fma)
+  __device__ __forceinline__ float distance(float z, float m) const {
+    return fmaxf(near(z) && near(m) ? ref(z) - ref(m) : (z - m) * c2, -200.f);
+  }
+};
 struct Stats { float m, s, t; };
 
-__device__ __forceinline__ float distance(float z, float m, float c2) { return fmaxf((z - m) * c2, -200.f); }
-
-__device__ __forceinline__ Stats merge(const Stats& a, const Stats& b, float c2) {
-  const float m = max_nan(a.m, b.m);
-  const float da = distance(a.m, m, c2), db = distance(b.m, m, c2);
+// The sum of s and t over a warp, from the lanes' own m to the largest.
+__device__ __forceinline__ Stats merge_warp(const Stats& a, const Scale& k) {
+  const float m = max_warp(a.m), d = k.distance(a.m, m), f = exp2_fast(d);
+  return {m, warp_sum(f * a.s), warp_sum(f * fmaf(a.s, d, a.t))};
+}
+__device__ __forceinline__ Stats merge(const Stats& a, const Stats& b, const Scale& k) {
+  const float m = max_nan(a.m, b.m), da = k.distance(a.m, m), db = k.distance(b.m, m);
   const float fa = exp2_fast(da), fb = exp2_fast(db);
   return {m, fa * a.s + fb * b.s, fa * fmaf(a.s, da, a.t) + fb * fmaf(b.s, db, b.t)};
 }
-__device__ __forceinline__ Stats merge_warp(Stats a, float c2) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const Stats b{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o),
-                  __shfl_xor_sync(0xffffffffu, a.t, o)};
-    a = merge(a, b, c2);
-  }
-  return a;
-}
 
-// Adds N values whose largest is `top` (NaN when one of them is).
-template <bool ENT, int N> __device__ __forceinline__ void add_values(Stats& a, const float* z, float top, float c2) {
-  if (!(top <= a.m)) {
-    const float m = max_nan(a.m, top), d = distance(a.m, m, c2), f = exp2_fast(d);
-    if (ENT) a.t = f * fmaf(a.s, d, a.t);
-    a.s *= f;
-    a.m = m;
+// The same while a thread adds to it: two sums of each, for two fp32 operations at once.
+template <bool ENT> struct Running {
+  float m = kMinusInf;
+  float2 s = {0.f, 0.f}, t = {0.f, 0.f};
+  // To a largest of at least `top` (NaN when something in the row is).
+  __device__ __forceinline__ void raise(float top, const Scale& k) {
+    if (top <= m) return;
+    const float next = max_nan(m, top), d = k.distance(m, next), f = exp2_fast(d);
+    if (ENT) t = {f * fmaf(s.x, d, t.x), f * fmaf(s.y, d, t.y)};
+    s = {f * s.x, f * s.y};
+    m = next;
   }
+  __device__ __forceinline__ void add_far(float z, const Scale& k) {
+    const float d = fmaxf((z - m) * k.c2, -200.f), e = exp2_fast(d);
+    s.x += e;
+    if (ENT) t.x = fmaf(e, d, t.x);
+  }
+  __device__ __forceinline__ void add_one(float z, const Scale& k) {
+    raise(z, k);
+    if (!k.near(m)) return add_far(z, k);
+    const float d = fmaf(fmaxf(z, k.least), k.c2, -k.ref(m)), e = exp2_fast(d);
+    s.x += e;
+    if (ENT) t.x = fmaf(e, d, t.x);
+  }
+  // N groups of eight values, of which the first `count` are there and the others -inf.
+  template <int N, typename T> __device__ __forceinline__ void add(const Eight<T> (&x)[N], int count, const Scale& k) {
+    float top = x[0].largest();
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const float d = distance(z[k], a.m, c2), e = exp2_fast(d);
-    a.s += e;
-    if (ENT) a.t = fmaf(e, d, a.t);
+    for (int i = 1; i < N; ++i) top = max_nan(top, x[i].largest());
+    raise(top, k);
+    if (k.near(m)) {
+      const float2 c = {k.c2, k.c2}, r = {-k.ref(m), -k.ref(m)};
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (i >= count) break;
+        float2 z[4];
+        x[i].pairs(z, k.least);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 d = fma2(z[j], c, r), e = {exp2_fast(d.x), exp2_fast(d.y)};
+          s = add2(s, e);
+          if (ENT) t = fma2(e, d, t);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float z[8];
+        x[i].get(z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) add_far(z[j], k);
+      }
+    }
   }
-}
+};
 
 // Statistics of this thread's share of a row: groups first + own, first + own + stride, ... below last, and single elements.
 template <typename T, bool ENT>
 __device__ __forceinline__ Stats row_share(const T* row, const RowSpan& r, int first, int last, int own, int stride,
-                                           int single, float c2) {
+                                           int single, const Scale& c) {
   constexpr int kBatch = 4;
-  Stats a{kMinusInf, 0.f, 0.f};
-  const T* p = row + r.head;
-  for (int g = first + own; g < last; g += kBatch * stride) {
-    Eight<T> x[kBatch];
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k)
-      if (g + k * stride < last) x[k].load(p + 8ll * (g + k * stride));
+  Running<ENT> a;
+  const T* p = row + r.head + 8ll * (first + own);
+  int left = (last - first - own + stride - 1) / stride;  // groups of this thread that are not loaded
+  auto load = [&](Eight<T> (&x)[kBatch]) {
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      if (g + k * stride >= last) break;
-      float z[8];
-      x[k].get(z);
-      float top = z[0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) top = max_nan(top, z[j]);
-      add_values<ENT, 8>(a, z, top, c2);
+      if (k < left) x[k].load(p + 8 * k * stride);
+      else x[k].fill_minus_inf();
     }
+    p += 8ll * kBatch * stride;
+    left -= kBatch;
+  };
+  while (left > 0) {
+    Eight<T> x[kBatch];
+    load(x);
+    a.add(x, left >= 0 ? kBatch : left + kBatch, c);
   }
   const int i = r.single(single);
-  if (i >= 0) {
-    const float z = to_float(row[i]);
-    add_values<ENT, 1>(a, &z, z, c2);
-  }
-  return a;
+  if (i >= 0) a.add_one(to_float(row[i]), c);
+  return {a.m, a.s.x + a.s.y, a.t.x + a.t.y};
 }
 
 // ---- the likeliest tokens ---------------------------------------------------------------------------------------
@@ -180,6 +265,7 @@ struct LogArgs {
   long long n, ld;
   int vocab;
   float scale;          // of the logits
+  Scale c;
   float* logp;          // each output may be nullptr
   float2* norm;
   float* entropy;
@@ -187,7 +273,7 @@ struct LogArgs {
   int* top_index;
   float* top_logp;
   int* status;
-  int parts;            // blocks per row
+  int parts_log2;       // blocks per row
 };
 
 // The given token of a row: its index; -1 where none was asked for; -2 for a row that is not to be read (a negative token
@@ -205,7 +291,10 @@ __device__ __forceinline__ int given_token(const void* tokens, int token64, long
 
 // What a row's owner writes once it has the row's statistics; returns log S, NaN for a row with a NaN or +inf.
 __device__ __forceinline__ float finish_row(const LogArgs& a, long long row, const Stats& s, int token, float given) {
+  const Scale& k = a.c;
+  // (s and t count from ref(m): the distance of m from it enters log S, and cancels in the entropy)
   float log_s = logf(s.s), entropy = log_s - s.t / s.s * kLn2;
+  if (k.near(s.m)) log_s -= fmaf(s.m, k.c2, -k.ref(s.m)) * kLn2;
   if (s.m == kMinusInf) log_s = entropy = 0.f;  // nothing to choose from
   if (!(s.m < -kMinusInf)) log_s = entropy = not_a_number();
   if (a.norm != nullptr) a.norm[row] = make_float2(s.m, log_s);
@@ -231,25 +320,28 @@ __device__ __forceinline__ void write_top(const LogArgs& a, long long row, int k
     a.top_logp[row * a.top + k] = some ? (key_logit(key) - m) * a.scale - log_s : fine ? kMinusInf : not_a_number();
 }
 
-constexpr int kRowThreads = 256, kGroupMaxima = kRowThreads / 4, kCandidates = 1024;
+constexpr int kGroupMaxima = 64, kCandidates = 1024;
+static_assert(kGroupMaxima >= ACC_LOGPROBS_MAX_TOP, "as many maxima as alternatives");
 
-struct RowShared {
-  Stats stats[kRowThreads / 32];
+template <int THREADS> struct RowShared {
+  Stats stats[THREADS / 32];
   Stats all;
   float maxima[kGroupMaxima];
   float bar;                     // a bound that at least `top` logits of the share reach
   int count;
+  unsigned char owner[THREADS / 32][32];  // of each warp: the lanes whose shares are read again
   Key best[ACC_LOGPROBS_MAX_TOP];
   Key list[kCandidates];
 };
 
 // list[0 .. count) -> best[0 .. top), in order; keys are distinct, so the order in which the list was filled does not matter.
-__device__ __forceinline__ void rank_list(RowShared& sh, int count, int top) {
+template <int THREADS> __device__ __forceinline__ void rank_list(RowShared<THREADS>& sh, int count, int top) {
   if ((int)threadIdx.x < top) sh.best[threadIdx.x] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < count; i += kRowThreads) {
+  for (int i = threadIdx.x; i < count; i += THREADS) {
     const Key own = sh.list[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < count; ++j) rank += sh.list[j] > own;
     if (rank < top) sh.best[rank] = own;
   }
@@ -273,22 +365,24 @@ __device__ __forceinline__ void each_value(const T* row, const RowSpan& r, int f
 }
 
 // The `top` largest keys of a block's share of a row into sh.best.  Every thread knows the largest logit of its own share; the
-// `top`-th largest of 64 such maxima, four threads each, is a bar that at least `top` logits reach, and only the shares of
-// threads whose maximum reaches it are read again, by whole warps: for top = 20 about 25 of 256.  Ties at the bar may be many
+// `top`-th largest of 64 such maxima, of neighbouring threads, is a bar that at least `top` logits reach, and only the shares of
+// threads whose maximum reaches it are read again, by whole warps: for top = 20 about 25.  Ties at the bar may be many
 // (a mask of the type's lowest value leaves them): then those above it are taken and those at it searched in order of index.
-template <typename T>
-__device__ __forceinline__ void select_top(RowShared& sh, const T* row, const RowSpan& r, int first, int last, int single,
+template <typename T, int THREADS>
+__device__ __forceinline__ void select_top(RowShared<THREADS>& sh, const T* row, const RowSpan& r, int first, int last, int single,
                                            float own_max, int top) {
+  constexpr int kMaximumOf = THREADS / kGroupMaxima;
   const int tid = threadIdx.x, lane = tid & 31;
   float m = own_max;
-  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  if ((tid & 3) == 0) sh.maxima[tid >> 2] = m;
+#pragma unroll
+  for (int o = 1; o < kMaximumOf; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (tid % kMaximumOf == 0) sh.maxima[tid / kMaximumOf] = m;
   if (tid == 0) { sh.bar = kMinusInf; sh.count = 0; }
   __syncthreads();
   if (tid < kGroupMaxima) {
     const float own = sh.maxima[tid];
     int rank = 0;
+#pragma unroll 16
     for (int j = 0; j < kGroupMaxima; ++j) rank += sh.maxima[j] > own || (sh.maxima[j] == own && j < tid);
     if (rank == top - 1) sh.bar = own;
   }
@@ -301,12 +395,30 @@ __device__ __forceinline__ void select_top(RowShared& sh, const T* row, const Ro
   // (-inf is no alternative, whatever the bar)
   auto gather = [&](bool above) {
     auto take = [&](float z) { return above ? z > bar : z >= bar && z > kMinusInf; };
-    unsigned todo = __ballot_sync(0xffffffffu, take(own_max));
-    while (todo != 0) {
-      const int owner = (tid & ~31) + __ffs(todo) - 1;
-      todo &= todo - 1;
-      each_value(row, r, first + owner, last, lane * kRowThreads, 32 * kRowThreads, -1,
-                 [&](float z, int i) { if (take(z)) push(z, i); });
+    const unsigned owners = __ballot_sync(0xffffffffu, take(own_max));
+    if (take(own_max)) sh.owner[tid >> 5][__popc(owners & ((1u << lane) - 1))] = (unsigned char)lane;
+    __syncwarp();
+    // the owners' groups as one list, a lane each, four at a time
+    const int each = (last - first + THREADS - 1) / THREADS, items = __popc(owners) * each;
+    constexpr int kTogether = 4;
+    for (int i = lane; i < items; i += 32 * kTogether) {
+      Eight<T> x[kTogether];
+      int group[kTogether];
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        const int item = i + 32 * k, owner = item < items ? item / each : 0;
+        group[k] = item < items ? first + (tid & ~31) + sh.owner[tid >> 5][owner] + (item - owner * each) * THREADS : last;
+        if (group[k] < last) x[k].load(row + r.head + 8ll * group[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        if (group[k] >= last || !take(x[k].largest())) continue;
+        float z[8];
+        x[k].get(z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (take(z[j])) push(z[j], r.head + 8 * group[k] + j);
+      }
     }
     const int i = r.single(single);
     if (i >= 0) {
@@ -327,7 +439,7 @@ __device__ __forceinline__ void select_top(RowShared& sh, const T* row, const Ro
       // at the bar, in order of index: the singles before the groups, the groups, the singles behind them
       for (int g = first; count < top && g < last; g += kSearch) {
         __syncthreads();
-        each_value(row, r, g, min(last, g + kSearch), tid, kRowThreads, g == first && tid < 7 ? single : -1,
+        each_value(row, r, g, min(last, g + kSearch), tid, THREADS, g == first && tid < 7 ? single : -1,
                    [&](float z, int i) { if (z == bar) push(z, i); });
         __syncthreads();
         count = sh.count;
@@ -344,7 +456,7 @@ __device__ __forceinline__ void select_top(RowShared& sh, const T* row, const Ro
       Key below = ~0ull;
       for (int k = 0; k < top; ++k) {
         Key best = 0;
-        each_value(row, r, first, last, tid, kRowThreads, single, [&](float z, int i) {
+        each_value(row, r, first, last, tid, THREADS, single, [&](float z, int i) {
           const Key key = make_key(z, i);
           if (z > kMinusInf && key < below && key > best) best = key;
         });
@@ -354,7 +466,7 @@ __device__ __forceinline__ void select_top(RowShared& sh, const T* row, const Ro
         if (lane == 0) sh.list[tid >> 5] = best;
         __syncthreads();
         best = 0;
-        for (int j = 0; j < kRowThreads / 32; ++j) best = max(best, sh.list[j]);
+        for (int j = 0; j < THREADS / 32; ++j) best = max(best, sh.list[j]);
         if (tid == 0) sh.best[k] = best;
         below = best;
       }
@@ -367,35 +479,35 @@ __device__ __forceinline__ void select_top(RowShared& sh, const T* row, const Ro
 
 // A row per cluster of `parts` blocks: each takes a stretch of its groups, and the first joins them over the cluster's shared
 // memory.  One pass over the logits; the alternatives cost a second look at a tenth of them, which the L2 cache still holds.
-template <typename T, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kRowThreads) logprobs_kernel(const LogArgs a) {
+template <typename T, bool ENT, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, TOP ? 1280 / THREADS : 1) logprobs_kernel(const LogArgs a) {
   namespace cg = cooperative_groups;
-  __shared__ RowShared sh;
+  __shared__ __align__(16) RowShared<THREADS> sh;
   await_previous();
   let_next_start();
-  const int parts = a.parts, tid = threadIdx.x;
-  const long long row = blockIdx.x / parts;
-  const int part = blockIdx.x % parts;
+  const int parts = 1 << a.parts_log2, tid = threadIdx.x;
+  const long long row = blockIdx.x >> a.parts_log2;
+  const int part = blockIdx.x & (parts - 1);
   const int token = given_token(a.tokens, a.token64, row, a.vocab, tid == 0 && part == 0 ? a.status : nullptr);
   if (token == -2) {
-    if (part == 0) skip_row(a, row, tid, kRowThreads);
+    if (part == 0) skip_row(a, row, tid, THREADS);
     return;
   }
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   const RowSpan r = RowSpan::of(z, a.vocab);
-  const int first = (int)((long long)r.groups * part / parts), last = (int)((long long)r.groups * (part + 1) / parts);
+  const int first = (int)((long long)r.groups * part >> a.parts_log2), last = (int)((long long)r.groups * (part + 1) >> a.parts_log2);
   // the singles before the groups belong to the first part, those behind them to the last
   const int single = tid < 7 ? (part == 0 ? tid : -1) : tid < 14 && part == parts - 1 ? tid : -1;
-  const float c2 = a.scale * kLog2e;
-  const Stats own = row_share<T, ENT>(z, r, first, last, tid, kRowThreads, single < 0 ? 14 : single, c2);
+  const Scale& c = a.c;
+  const Stats own = row_share<T, ENT>(z, r, first, last, tid, THREADS, single < 0 ? 14 : single, c);
   {
-    const Stats w = merge_warp(own, c2);
+    const Stats w = merge_warp(own, c);
     if ((tid & 31) == 0) sh.stats[tid >> 5] = w;
   }
   __syncthreads();
   if (tid < 32) {
-    Stats w = tid < kRowThreads / 32 ? sh.stats[tid] : Stats{kMinusInf, 0.f, 0.f};
-    w = merge_warp(w, c2);
+    Stats w = tid < THREADS / 32 ? sh.stats[tid] : Stats{kMinusInf, 0.f, 0.f};
+    w = merge_warp(w, c);
     if (tid == 0) sh.all = w;
   }
   if (TOP) select_top(sh, z, r, first, last, single < 0 ? 14 : single, own.m, a.top);
@@ -405,9 +517,9 @@ __global__ void __launch_bounds__(kRowThreads) logprobs_kernel(const LogArgs a) 
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
     if (part == 0) {
-      for (int p = 1; p < parts; ++p) all = merge(all, *cluster.map_shared_rank(&sh.all, p), c2);
+      for (int p = 1; p < parts; ++p) all = merge(all, *cluster.map_shared_rank(&sh.all, p), c);
       if (TOP) {
-        for (int i = tid; i < parts * a.top; i += kRowThreads) sh.list[i] = cluster.map_shared_rank(sh.best, i / a.top)[i % a.top];
+        for (int i = tid; i < parts * a.top; i += THREADS) sh.list[i] = cluster.map_shared_rank(sh.best, i / a.top)[i % a.top];
         __syncthreads();
         // (empty places are zeros: behind every key, and equal, so none of them is ranked below `top` in place of a key)
         rank_list(sh, parts * a.top, a.top);
@@ -424,13 +536,17 @@ __global__ void __launch_bounds__(kRowThreads) logprobs_kernel(const LogArgs a) 
   }
 }
 
-// A row per warp, for vocabularies of which a lane's share is a few vectors; the alternatives one after another.
+// A row per warp.  The alternatives as above, with a bar from the 32 lanes' maxima, below which two logits in three stay.
+constexpr int kWarpList = 192;
 template <typename T, bool ENT, bool TOP>
 __global__ void __launch_bounds__(256) logprobs_warp_kernel(const LogArgs a) {
+  __shared__ __align__(16) Key lists[TOP ? 8 : 1][kWarpList];
+  __shared__ Key bests[TOP ? 8 : 1][ACC_LOGPROBS_MAX_TOP];
+  __shared__ int counts[8];
   await_previous();
   let_next_start();
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * 8 + warp;
   if (row >= a.n) return;
   const int token = given_token(a.tokens, a.token64, row, a.vocab, lane == 0 ? a.status : nullptr);
   if (token == -2) {
@@ -439,61 +555,111 @@ __global__ void __launch_bounds__(256) logprobs_warp_kernel(const LogArgs a) {
   }
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   const RowSpan r = RowSpan::of(z, a.vocab);
-  const float c2 = a.scale * kLog2e;
-  const Stats all = merge_warp(row_share<T, ENT>(z, r, 0, r.groups, lane, 32, lane, c2), c2);
+  const Scale& c = a.c;
+  const Stats own = row_share<T, ENT>(z, r, 0, r.groups, lane, 32, lane, c), all = merge_warp(own, c);
   float log_s = 0.f;
   if (lane == 0) log_s = finish_row(a, row, all, token, token >= 0 ? to_float(z[token]) : 0.f);
   if (!TOP) return;
   log_s = __shfl_sync(0xffffffffu, log_s, 0);
-  // a lane's best key below its last; only the lane whose key was taken looks again
-  auto next = [&](Key below) {
-    Key best = 0;
-    each_value(z, r, 0, r.groups, lane, 32, lane, [&](float v, int i) {
-      const Key key = make_key(v, i);
-      if (v > kMinusInf && key < below && key > best) best = key;
-    });
-    return best;
-  };
-  Key mine = next(~0ull), kept = 0;
-  for (int k = 0; k < a.top; ++k) {
-    Key best = mine;
+  int above = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (lane == k) kept = best;
-    if (best == 0) break;
-    if (mine == best) mine = next(best);
+  for (int j = 0; j < 32; ++j) {
+    const float m = __shfl_sync(0xffffffffu, own.m, j);
+    above += m > own.m || (m == own.m && j < lane);
   }
-  if (lane < a.top) write_top(a, row, lane, kept, all.m, log_s);
+  const unsigned at_bar = __ballot_sync(0xffffffffu, above == a.top - 1);
+  const float bar = __shfl_sync(0xffffffffu, own.m, at_bar != 0 ? __ffs(at_bar) - 1 : 0);  // (a row with NaN may have none)
+  if (lane == 0) counts[warp] = 0;
+  bests[warp][lane] = 0;
+  __syncwarp();
+  auto take = [&](float v) { return v >= bar && v > kMinusInf; };
+  auto push = [&](float v, int i) {
+    const int at = atomicAdd(&counts[warp], 1);
+    if (at < kWarpList) lists[warp][at] = make_key(v, i);
+  };
+  for (int g = lane; g < r.groups; g += 32) {
+    Eight<T> x;
+    x.load(z + r.head + 8ll * g);
+    if (!take(x.largest())) continue;
+    float v[8];
+    x.get(v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (take(v[k])) push(v[k], r.head + 8 * g + k);
+  }
+  const int single = r.single(lane);
+  if (single >= 0 && take(to_float(z[single]))) push(to_float(z[single]), single);
+  __syncwarp();
+  const int count = counts[warp];
+  if (count <= kWarpList) {
+    for (int i = lane; i < count; i += 32) {
+      const Key key = lists[warp][i];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < count; ++j) rank += lists[warp][j] > key;
+      if (rank < a.top) bests[warp][rank] = key;
+    }
+  } else {
+    // one after another: a lane's best key below its last; only the lane whose key was taken looks again
+    auto next = [&](Key below) {
+      Key best = 0;
+      each_value(z, r, 0, r.groups, lane, 32, lane, [&](float v, int i) {
+        const Key key = make_key(v, i);
+        if (v > kMinusInf && key < below && key > best) best = key;
+      });
+      return best;
+    };
+    Key mine = next(~0ull);
+    for (int k = 0; k < a.top; ++k) {
+      Key best = mine;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+      if (lane == 0) bests[warp][k] = best;
+      if (best != 0 && mine == best) mine = next(best);
+    }
+  }
+  __syncwarp();
+  if (lane < a.top) write_top(a, row, lane, bests[warp][lane], all.m, log_s);
 }
 
-// Vocabularies up to this length take a warp per row.
-constexpr int kWarpVocab = 1024;
+// Rows up to the first length take a warp each, and up to the second where that leaves every SM its warps (65536 rows of 2000 in
+// bf16: 105 us with a block of 128 threads each).
+constexpr int kWarpVocab = 1024, kWarpVocabMany = 4096;
+static bool warp_rows(const acc_ctx* ctx, long long n, int vocab) {
+  return vocab <= kWarpVocab || (vocab <= kWarpVocabMany && n >= 32ll * ctx->sm_count);
+}
 
 // Blocks per row: as many as keep the GPU busy when there are few rows, each with a stretch worth a block's start.
-static int row_parts(const acc_ctx* ctx, long long n, int vocab) {
-  int parts = 1;
-  while (parts < 8 && n * parts * 2 <= 4ll * ctx->sm_count && vocab / (parts * 2) >= 2048) parts *= 2;
-  return parts;
+static int row_parts_log2(const acc_ctx* ctx, long long n, int vocab) {
+  int p = 0;
+  while (p < 3 && (n << (p + 1)) <= 4ll * ctx->sm_count && vocab >> (p + 1) >= 2048) ++p;
+  return p;
 }
 
 cudaError_t launch_token_logprobs(acc_ctx* ctx, const void* logits, bool bf16, long long n, int vocab, long long ld,
                                   const void* tokens, bool tok64, float scale, float* logp, float* norm, float* entropy,
                                   int top, int* top_index, float* top_logp, cudaStream_t s) {
-  LogArgs a{logits, tokens, tok64, n, ld, vocab, scale, logp, reinterpret_cast<float2*>(norm), entropy, top, top_index,
-            top_logp, ctx->d_status, 1};
+  LogArgs a{logits, tokens, tok64, n, ld, vocab, scale, Scale::of(scale), logp, reinterpret_cast<float2*>(norm), entropy, top,
+            top_index, top_logp, ctx->d_status, 0};
   PhaseTimer pt(ctx, PH_LOGPROBS, s);
   auto go = [&](auto t) {
     using T = decltype(t);
     const bool ent = entropy != nullptr;
-    if (vocab <= kWarpVocab) {
+    if (warp_rows(ctx, n, vocab)) {
       auto* kernel = top > 0 ? (ent ? logprobs_warp_kernel<T, true, true> : logprobs_warp_kernel<T, false, true>)
                              : (ent ? logprobs_warp_kernel<T, true, false> : logprobs_warp_kernel<T, false, false>);
       return launch_early(kernel, (unsigned)((n + 7) / 8), 256, s, a);
     }
-    a.parts = row_parts(ctx, n, vocab);
-    auto* kernel = top > 0 ? (ent ? logprobs_kernel<T, true, true> : logprobs_kernel<T, false, true>)
-                           : (ent ? logprobs_kernel<T, true, false> : logprobs_kernel<T, false, false>);
-    return launch_early_as(kernel, (unsigned)(n * a.parts), kRowThreads, 0, a.parts, s, a);
+    a.parts_log2 = row_parts_log2(ctx, n, vocab);
+    auto block = [&](auto threads) {
+      constexpr int N = decltype(threads)::value;
+      auto* kernel = top > 0 ? (ent ? logprobs_kernel<T, true, true, N> : logprobs_kernel<T, false, true, N>)
+                             : (ent ? logprobs_kernel<T, true, false, N> : logprobs_kernel<T, false, false, N>);
+      return launch_early_as(kernel, (unsigned)(n << a.parts_log2), N, 0, 1 << a.parts_log2, s, a);
+    };
+    // Rows of 33278 in bf16, 5040 of them: 64 us with 128 threads a row and 68 with 256 (more rows' ends overlap); 2048 rows of 131071:
+    // 99 us and 88 (fewer rows are left for the last wave).
+    return vocab < 65536 ? block(std::integral_constant<int, 128>()) : block(std::integral_constant<int, 256>());
   };
   return bf16 ? go(__nv_bfloat16()) : go(0.f);
 }
