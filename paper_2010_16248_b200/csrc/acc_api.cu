@@ -612,7 +612,7 @@ int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type
     return ACC_EINVAL;
   // in place, or apart: the same rows under another type or stride would be overwritten before they are read
   if (logits == dlogits && (logit_type != out_type || (n > 1 && ld != ld_out))) return ACC_EINVAL;
-  if (logprobs_grad_blocks(n, vocab) > kMostBlocks) return ACC_EINVAL;
+  if (logprobs_grad_blocks(ctx, n, vocab) > kMostBlocks) return ACC_EINVAL;
   if (!aligned_to(logits, value_size(logit_type)) || !aligned_to(dlogits, value_size(out_type)) ||
       !aligned_to(tokens, token_size(token_type)) || !aligned_to(norm, 8) || !aligned_to(g_logp, 4) ||
       !aligned_to(g_entropy, 4) || !aligned_to(entropy, 4))

@@ -217,7 +217,7 @@ cudaError_t launch_token_logprobs(acc_ctx* ctx, const void* logits, bool bf16, l
                                   const void* tokens, bool tok64, float scale, float* logp, float* norm, float* entropy,
                                   int top, int* top_index, float* top_logp, cudaStream_t s);
 // Blocks of the gradient's launch.
-long long logprobs_grad_blocks(long long n, int vocab);
+long long logprobs_grad_blocks(const acc_ctx* ctx, long long n, int vocab);
 cudaError_t launch_token_logprobs_grad(acc_ctx* ctx, const void* logits, bool bf16, long long n, int vocab, long long ld,
                                        const void* tokens, bool tok64, float scale, const float* norm, const float* g_logp,
                                        long long g_count, const float* g_entropy, long long h_count, const float* entropy,

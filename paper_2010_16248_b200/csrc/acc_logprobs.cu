@@ -48,6 +48,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(x.u), "l"(y.u));
   return r.f;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  Pair x, y, r;
+  x.f = a; y.f = b;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(x.u), "l"(y.u));
+  return r.f;
+}
 constexpr float kMinusInf = -__builtin_huge_valf();
 __device__ __forceinline__ float not_a_number() { return __int_as_float(0x7fffffff); }
 
@@ -624,7 +630,7 @@ __global__ void __launch_bounds__(256) logprobs_warp_kernel(const LogArgs a) {
 
 // Rows up to the first length take a warp each, and up to the second where that leaves every SM its warps (65536 rows of 2000 in
 // bf16: 105 us with a block of 128 threads each).
-constexpr int kWarpVocab = 1024, kWarpVocabMany = 4096;
+constexpr int kWarpVocab = 1024, kWarpVocabMany = 8192;
 static bool warp_rows(const acc_ctx* ctx, long long n, int vocab) {
   return vocab <= kWarpVocab || (vocab <= kWarpVocabMany && n >= 32ll * ctx->sm_count);
 }
@@ -682,24 +688,24 @@ struct LogGradArgs {
   int h_step;
   void* out;
   int* status;
-  int segments;            // blocks per row
+  int segments, stretch;   // blocks per row, groups of eight (elements, on the narrow way) of a block
 };
 
-// What one row's elements need.
+// What one row's elements need: dz = p (w0 + w1 log2 p), with log2 p = (z - m) c2 - log2_s.
 struct RowGrad {
-  float m, c2, log2_s;     // log2 p = (z - m) c2 - log2_s
-  float g, h, h_entropy;   // times scale; h_entropy = h H
-  int token;
-  template <bool ENT> __device__ __forceinline__ float at(float z, int index) const {
+  float m, c2, log2_s, w0, w1, g;
+  template <bool ENT> __device__ __forceinline__ float at(float z) const {
     float l = fmaf(z - m, c2, -log2_s);
     if (ENT) l = fmaxf(l, -200.f);  // 2^-200 is 0, and so is its product
-    const float p = exp2_fast(l);
-    const float w = ENT ? fmaf(h * kLn2, l, g + h_entropy) : g;
-    return index == token ? g - p * w : -p * w;
+    return exp2_fast(l) * (ENT ? fmaf(w1, l, w0) : w0);
+  }
+  template <bool ENT> __device__ __forceinline__ float2 at(float2 z) const {
+    float2 l = fma2(add2(z, {-m, -m}), {c2, c2}, {-log2_s, -log2_s});
+    if (ENT) l = {fmaxf(l.x, -200.f), fmaxf(l.y, -200.f)};
+    const float2 p = {exp2_fast(l.x), exp2_fast(l.y)};
+    return mul2(p, ENT ? fma2({w1, w1}, l, {w0, w0}) : float2{w0, w0});
   }
 };
-
-constexpr int kGradBatch = 4;  // groups of eight elements that a thread loads together
 
 // ROW_THREADS threads share a row: a block with `segments` blocks per row, or a warp.  SAME: input and output rows start at
 // the same place within eight elements, so that both take wide accesses; otherwise elements one at a time.
@@ -708,59 +714,66 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const LogGradArgs a)
   await_previous();
   let_next_start();
   const int lane = threadIdx.x % ROW_THREADS;
-  const long long unit = ROW_THREADS == 256 ? blockIdx.x : (long long)blockIdx.x * (256 / ROW_THREADS) + threadIdx.x / ROW_THREADS;
-  const long long row = ROW_THREADS == 256 ? unit / a.segments : unit;
-  const int segment = ROW_THREADS == 256 ? (int)(unit - row * a.segments) : 0;
+  const unsigned unit = ROW_THREADS == 256 ? blockIdx.x : blockIdx.x * (256 / ROW_THREADS) + threadIdx.x / ROW_THREADS;
+  const long long row = ROW_THREADS == 256 && a.segments > 1 ? unit / (unsigned)a.segments : unit;
+  const int segment = ROW_THREADS == 256 ? (int)(unit - (unsigned)row * a.segments) : 0;
   if (row >= a.n) return;
   const int token = given_token(a.tokens, a.token64, row, a.vocab, lane == 0 && segment == 0 ? a.status : nullptr);
   const In* z = static_cast<const In*>(a.logits) + row * a.ld;
   Out* out = static_cast<Out*>(a.out) + row * a.ld_out;
   const RowSpan r = SAME ? RowSpan::of(z, a.vocab) : RowSpan{0, 0, a.vocab};
   RowGrad f{};
-  f.token = token;
   bool zero = token == -2;
   if (!zero) {
     const float2 norm = a.norm[row];
     f.m = norm.x;
     f.c2 = a.scale * kLog2e;
     f.log2_s = norm.y * kLog2e;
-    f.g = a.g_logp != nullptr ? a.g_logp[row * a.g_step] * a.scale : 0.f;
+    f.g = a.g_logp != nullptr && token >= 0 ? a.g_logp[row * a.g_step] * a.scale : 0.f;
+    f.w0 = -f.g;
     if (ENT) {
-      f.h = a.g_entropy[row * a.h_step] * a.scale;
-      f.h_entropy = f.h * a.entropy[row];
+      const float h = a.g_entropy[row * a.h_step] * a.scale;
+      f.w0 = -fmaf(h, a.entropy[row], f.g);
+      f.w1 = -h * kLn2;
     }
-    if (token < 0) f.g = 0.f;  // no token was given
     zero = f.m == kMinusInf;
-    if (norm.y != norm.y || f.m != f.m) f.g = f.h_entropy = not_a_number();
+    if (norm.y != norm.y || f.m != f.m) f.w0 = not_a_number();
   }
   auto single = [&](int i) {
     float v = 0.f;
-    if (!zero) v = f.template at<ENT>(to_float(z[i]), i);
+    if (!zero) v = f.template at<ENT>(to_float(z[i])) + (i == token ? f.g : 0.f);
     if constexpr (sizeof(Out) == 2) out[i] = __float2bfloat16_rn(v);
     else out[i] = v;
   };
   if (!SAME) {
-    const int from = segment * 256 * kGradBatch * 8;
-    const int to = ROW_THREADS == 256 ? min(a.vocab, from + 256 * kGradBatch * 8) : a.vocab;
+    const int from = segment * a.stretch, to = ROW_THREADS == 256 ? min(a.vocab, from + a.stretch) : a.vocab;
     for (int i = from + lane; i < to; i += ROW_THREADS) single(i);
     return;
   }
-  const int g0 = segment * ROW_THREADS * kGradBatch + lane;
-  const int last = ROW_THREADS == 256 ? min(r.groups, (segment + 1) * ROW_THREADS * kGradBatch) : r.groups;
-  for (int g = g0; g < last; g += ROW_THREADS * kGradBatch) {
-    Eight<In> x[kGradBatch];
+  const int first = segment * a.stretch, last = ROW_THREADS == 256 ? min(r.groups, first + a.stretch) : r.groups;
+  constexpr int kTogether = 4;
+  for (int g = first + lane; g < last; g += ROW_THREADS * kTogether) {
+    Eight<In> x[kTogether];
 #pragma unroll
-    for (int k = 0; k < kGradBatch; ++k)
+    for (int k = 0; k < kTogether; ++k)
       if (!zero && g + k * ROW_THREADS < last) x[k].load(z + r.head + 8ll * (g + k * ROW_THREADS));
 #pragma unroll
-    for (int k = 0; k < kGradBatch; ++k) {
+    for (int k = 0; k < kTogether; ++k) {
       if (g + k * ROW_THREADS >= last) break;
       const int i = r.head + 8 * (g + k * ROW_THREADS);
       float v[8] = {};
       if (!zero) {
         x[k].get(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = f.template at<ENT>(v[j], i + j);
+        for (int j = 0; j < 8; j += 2) {
+          const float2 y = f.template at<ENT>(float2{v[j], v[j + 1]});
+          v[j] = y.x;
+          v[j + 1] = y.y;
+        }
+        if ((unsigned)(token - i) < 8u) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += i + j == token ? f.g : 0.f;
+        }
       }
       Eight<Out> y;
       y.put(v);
@@ -773,10 +786,14 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const LogGradArgs a)
   }
 }
 
-// Blocks of a row, for rows of more than a warp's share.
-static int grad_segments(int vocab) { return (vocab + 256 * kGradBatch * 8 - 1) / (256 * kGradBatch * 8); }
-long long logprobs_grad_blocks(long long n, int vocab) {
-  return vocab <= kWarpVocab ? (n + 7) / 8 : n * grad_segments(vocab);
+// Blocks of a row: one where there are rows enough (its start, a chain of loads, is then paid once), more where there are few.
+static int grad_segments(const acc_ctx* ctx, long long n, int vocab) {
+  const long long some = (16ll * ctx->sm_count + n - 1) / n, most = (vocab + 2047) / 2048;
+  return (int)std::max<long long>(1, std::min(some, most));
+}
+static bool grad_warp_rows(const acc_ctx* ctx, long long n, int vocab) { return warp_rows(ctx, n, vocab); }
+long long logprobs_grad_blocks(const acc_ctx* ctx, long long n, int vocab) {
+  return grad_warp_rows(ctx, n, vocab) ? (n + 7) / 8 : n * grad_segments(ctx, n, vocab);
 }
 
 cudaError_t launch_token_logprobs_grad(acc_ctx* ctx, const void* logits, bool bf16, long long n, int vocab, long long ld,
@@ -784,12 +801,15 @@ cudaError_t launch_token_logprobs_grad(acc_ctx* ctx, const void* logits, bool bf
                                        long long g_count, const float* g_entropy, long long h_count, const float* entropy,
                                        void* out, bool out_bf16, long long ld_out, cudaStream_t s) {
   LogGradArgs a{logits, tokens, tok64, n, ld, ld_out, vocab, scale, reinterpret_cast<const float2*>(norm), g_logp, g_entropy,
-                entropy, g_count > 1, h_count > 1, out, ctx->d_status, 1};
+                entropy, g_count > 1, h_count > 1, out, ctx->d_status, 1, 0};
   const size_t in_size = bf16 ? 2 : 4, out_size = out_bf16 ? 2 : 4;
   const bool same = (reinterpret_cast<uintptr_t>(logits) / in_size) % 8 == (reinterpret_cast<uintptr_t>(out) / out_size) % 8 &&
                     (n == 1 || (ld - ld_out) % 8 == 0);
-  const bool warp = vocab <= kWarpVocab;
-  if (!warp) a.segments = grad_segments(vocab);
+  const bool warp = grad_warp_rows(ctx, n, vocab);
+  if (!warp) {
+    a.segments = grad_segments(ctx, n, vocab);
+    a.stretch = ((same ? vocab / 8 : vocab) + a.segments - 1) / a.segments;
+  }
   PhaseTimer pt(ctx, PH_LOGPROBS_GRAD, s);
   auto go = [&](auto in, auto o, auto ent) {
     using In = decltype(in);
@@ -797,7 +817,7 @@ cudaError_t launch_token_logprobs_grad(acc_ctx* ctx, const void* logits, bool bf
     constexpr bool ENT = decltype(ent)::value;
     auto* kernel = warp ? (same ? logprobs_grad_kernel<In, Out, ENT, 32, true> : logprobs_grad_kernel<In, Out, ENT, 32, false>)
                         : (same ? logprobs_grad_kernel<In, Out, ENT, 256, true> : logprobs_grad_kernel<In, Out, ENT, 256, false>);
-    return launch_early(kernel, (unsigned)logprobs_grad_blocks(n, vocab), 256, s, a);
+    return launch_early(kernel, (unsigned)logprobs_grad_blocks(ctx, n, vocab), 256, s, a);
   };
   auto typed = [&](auto ent) {
     if (bf16) return out_bf16 ? go(__nv_bfloat16(), __nv_bfloat16(), ent) : go(__nv_bfloat16(), 0.f, ent);
