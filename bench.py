@@ -271,6 +271,9 @@ def main():
     ap.add_argument("--tokens", type=int, default=0,
                     help="config 5: the encoder's gradient is made in the step from that many tokens per worker "
                          "(embedding gradient of a Zipf-distributed batch), in place of the stream's")
+    ap.add_argument("--head", type=int, default=0,
+                    help="config 5: the decoder's gradient is made in the step from the logits of that many tokens per worker "
+                         "(log probabilities, their gradient, the input kept in 8 bits), in place of the stream's")
     ap.add_argument("--batch-mode", action="store_true",
                     help="batch-size mode instead of compression: a step is n_accum micro-batch accumulations, the "
                          "uncompressed average with the fused Nesterov update, and (every check_every steps) the "
@@ -335,10 +338,15 @@ def main():
     if args.tokens:
         assert args.config == 5, "--tokens needs config 5 (the language model's encoder)"
         embedding = wl.token_batch(w, args.tokens, device=dev, rank=rank)
+    head = None
+    if args.head:
+        assert args.config == 5, "--head needs config 5 (the language model's decoder)"
+        head = wl.head_batch(w, args.head, device=dev, rank=rank)
     eng = pipeline.AccordionStep(table, W, w.compressors, w.rank_low, w.rank_high, w.topk_low_bp, w.topk_high_bp,
                                  w.eta, 1e-8, w.check_every, device=dev, lazy_residual=not args.eager,
                                  optimizer=optimizer, extra_flags={"auto": 0, "always": 2, "never": 4}[args.pipeline],
-                                 overlap=not args.no_overlap, share_sms=args.share_sms, embedding=embedding)
+                                 overlap=not args.no_overlap, share_sms=args.share_sms, embedding=embedding,
+                                 head=head)
     n_mat = table.n_matrix_params
     grad_bytes_step = n_comp * 4.0 * W * table.n_params
 
@@ -438,7 +446,7 @@ def main():
     by_regime = {}
     # the stored per-step traffic belongs to the default path (lazy residual, no optimiser tail, the library's choice
     # of first PowerSGD pass, the config's own worker count)
-    default_path = not (args.eager or args.sgd_tail or args.adamw or args.tokens or args.share_sms or args.pipeline != "auto")
+    default_path = not (args.eager or args.sgd_tail or args.adamw or args.tokens or args.head or args.share_sms or args.pipeline != "auto")
     for name in ("low", "high", "mixed"):
         ts = per_step[[r == name for r in regime]]
         if len(ts):
@@ -530,6 +538,8 @@ def main():
                                               f"AdamW after the step, states in {args.adamw} bits, clipped"
                                               if args.adamw else "none"),
                            "encoder_gradient": (f"from {args.tokens} tokens per worker, in the step" if args.tokens
+                                                else "part of the gradient batch"),
+                           "decoder_gradient": (f"from the logits of {args.head} tokens per worker, in the step" if args.head
                                                 else "part of the gradient batch"),
                            "gradient_bytes_per_step": grad_bytes_step,
                            "l2_policy": f"inputs larger than L2: {RING} gradient batches of "

@@ -81,6 +81,71 @@ class TokenEmbedding:
         return self.ctx.last_launch_count()
 
 
+class CheckpointedLinear:
+    """A linear layer ``y = x W^T`` of one MATRIX layer (by name) for ``n`` tokens per worker: keeps its input ``x`` in 8 bits
+    during the forward pass, and makes the weight's gradient from that in the backward pass."""
+
+    def __init__(self, ctx: "binding.Context", layer: str, n: int, scale=1.0, accumulate=False):
+        self.ctx, self.layer, self.n = ctx, ctx.table.names.index(layer), int(n)
+        self.rows, self.cols = int(ctx.table.rows[self.layer]), int(ctx.table.cols[self.layer])
+        self.scale, self.accumulate = float(scale), accumulate
+        self.code, self.code_scale = ctx.new_checkpoint(ctx.n_workers * self.n, self.cols)
+        self.workspace = ctx.new_linear_grad_workspace(self.layer, self.n)
+
+    def keep(self, x: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None) -> int:
+        """``x`` ``[W, n, cols]``; rows of negative ``tokens`` ``[W, n]`` are kept as zeros.  Returns the kernels launched."""
+        self.ctx.acc_checkpoint_store(x.reshape(-1, self.cols), self.code, self.code_scale, tokens, stream)
+        return self.ctx.last_launch_count()
+
+    def kept(self, out: torch.Tensor, stream=None) -> torch.Tensor:
+        """The input as it was kept, into ``out`` ``[W, n, cols]``."""
+        self.ctx.acc_checkpoint_load(self.code, self.code_scale, out.view(-1, self.cols), stream)
+        return out
+
+    def backward(self, dy: torch.Tensor, grads: torch.Tensor, stream=None) -> int:
+        """The layer's slice of every worker's ``grads`` ``[W, stride]`` from ``dy`` ``[W, n, rows]``."""
+        self.ctx.acc_linear_grad(self.layer, dy, self.code, self.code_scale, grads, self.scale, self.accumulate,
+                                 self.workspace, stream)
+        return self.ctx.last_launch_count()
+
+
+class TokenHead(CheckpointedLinear):
+    """A language model's decoder: the log probabilities of given tokens under its logits, their gradient, and the decoder's
+    weight gradient from its input kept in 8 bits.  The caller makes the logits (a matrix product) and the input's gradient
+    (another, from ``dlogits``)."""
+
+    def __init__(self, ctx: "binding.Context", layer: str, n: int, temperature=1.0, top=0, scale=1.0, accumulate=False,
+                 dtype=torch.bfloat16):
+        super().__init__(ctx, layer, n, scale, accumulate)
+        W, dev = ctx.n_workers, ctx.device
+        self.logit_scale = 1.0 / float(temperature)
+        self.logp, self.entropy = torch.zeros(W, self.n, device=dev), torch.zeros(W, self.n, device=dev)
+        self.norm = torch.zeros(W, self.n, 2, device=dev)
+        self.top_index = torch.zeros(W * self.n, top, dtype=torch.int32, device=dev) if top else None
+        self.top_logp = torch.zeros(W * self.n, top, device=dev) if top else None
+        # rows on 16 bytes, which the gradient's copies want
+        self.dlogits = torch.zeros(W, self.n, (self.rows + 7) // 8 * 8, dtype=dtype, device=dev)[:, :, :self.rows]
+
+    def new_logits(self) -> torch.Tensor:
+        """A buffer ``[W, n, rows]`` for the logits, whose rows start on 16 bytes."""
+        return self.dlogits.new_zeros(self.ctx.n_workers, self.n, self.dlogits.stride(1))[:, :, :self.rows]
+
+    def _flat(self, t):
+        return t.view(-1, self.rows) if t.is_contiguous() else t.flatten(0, 1)
+
+    def forward(self, logits: torch.Tensor, tokens: torch.Tensor, stream=None) -> int:
+        """Fills ``logp``, ``entropy``, ``norm`` (and the alternatives) from ``logits`` ``[W, n, rows]`` and ``tokens``."""
+        self.ctx.acc_token_logprobs(self._flat(logits), tokens, self.logp, self.norm, self.entropy, self.top_index, self.top_logp,
+                                    self.logit_scale, stream)
+        return self.ctx.last_launch_count()
+
+    def backward_logits(self, logits: torch.Tensor, tokens: torch.Tensor, g_logp=None, g_entropy=None, stream=None) -> int:
+        """``dlogits`` from the loss's derivatives by ``logp`` and ``entropy`` (``[W, n]``, or one element)."""
+        self.ctx.acc_token_logprobs_grad(self._flat(logits), tokens, self.norm, self._flat(self.dlogits), g_logp, g_entropy,
+                                         self.entropy, self.logit_scale, stream)
+        return self.ctx.last_launch_count()
+
+
 def _make_optimizer(optimizer, ctx, stride, dev):
     """``(params, mom, hyper, adamw)`` of an optimizer dict: the Nesterov tail's tensors, or an ``AdamW`` and its hyper-
     parameters (``params`` and ``mom`` are then None: nothing is fused into the step)."""
@@ -101,7 +166,7 @@ class AccordionStep:
     def __init__(self, table: wl.LayerTable, n_workers: int, compressors: Sequence[str] = ("powersgd",),
                  rank_low=2, rank_high=1, topk_low_bp=1000, topk_high_bp=100, eta=0.5, gs_eps=1e-8,
                  check_every=10, decider=0, q_init=None, device="cuda", lazy_residual=False, optimizer=None,
-                 extra_flags=0, overlap=True, share_sms=False, embedding=None):
+                 extra_flags=0, overlap=True, share_sms=False, embedding=None, head=None):
         """``overlap``: with two compressors, the TopK step runs on a second stream beside the PowerSGD step
         (they share only the gradients and the level array, both read-only), so that the short, latency-bound
         kernels of one hide behind the streaming kernels of the other; the results are the same bits.
@@ -115,7 +180,10 @@ class AccordionStep:
         ``adamw``; its own ``params`` and ``mom`` belong to the fused update and are then None).
         ``embedding``: None, or a dict ``{"layer": name, "tokens": [W, n], "dy": [W, n, cols], "scale": 1.0,
         "accumulate": False}`` of fixed device buffers: every step first writes (or adds) the embedding's gradient of the
-        tokens into that layer of the gradients it is given."""
+        tokens into that layer of the gradients it is given.  ``head``: None, or a dict ``{"layer": name, "hidden": [W, n,
+        cols], "logits": [W, n, rows], "tokens": [W, n], "g_logp": tensor}`` of fixed device buffers (and, if wanted,
+        ``TokenHead``'s ``temperature``, ``scale``, ``accumulate``): every step first keeps the decoder's input in 8 bits,
+        takes the log probabilities and their gradient, and writes (or adds) the decoder's gradient."""
         self.table, self.W = table, n_workers
         self.compressors = tuple(compressors)
         if optimizer is not None and len(self.compressors) != 1:
@@ -150,6 +218,11 @@ class AccordionStep:
             self.tokens, self.dy = embedding["tokens"], embedding["dy"]
             self.embedding = TokenEmbedding(self.ctx, embedding["layer"], self.tokens.shape[1], embedding.get("scale", 1.0),
                                             embedding.get("accumulate", False))
+        self.head = None
+        if head is not None:
+            self.head_batch = [head[k] for k in ("hidden", "logits", "tokens", "g_logp")]
+            self.head = TokenHead(self.ctx, head["layer"], head["hidden"].shape[1], head.get("temperature", 1.0), 0,
+                                  head.get("scale", 1.0), head.get("accumulate", False), head["logits"].dtype)
         if "powersgd" in self.compressors:
             self.err_psgd = torch.zeros(n_workers, stride, device=dev)
             self.q = self.ctx.new_q(q_init if q_init is not None else wl.initial_q(table, rank_low, device=dev))
@@ -165,6 +238,12 @@ class AccordionStep:
         c = self.ctx
         if self.embedding is not None:
             self.launches += self.embedding.backward(self.tokens, self.dy, grads, stream)
+        if self.head is not None:
+            hidden, logits, tokens, g_logp = self.head_batch
+            self.launches += self.head.keep(hidden, tokens, stream)
+            self.launches += self.head.forward(logits, tokens, stream)
+            self.launches += self.head.backward_logits(logits, tokens, g_logp, stream=stream)
+            self.launches += self.head.backward(self.head.dlogits, grads, stream)
         delta: Optional[torch.Tensor] = self.delta  # accumulated once per iteration, by the first compressor
         if self.overlap and len(self.compressors) == 2:
             main = stream if stream is not None else torch.cuda.current_stream(self.device)

@@ -325,3 +325,20 @@ def token_batch(wl: Workload, n: int, device="cpu", rank: int = 0):
     tokens = torch.multinomial(weights, wl.n_workers * n, replacement=True, generator=g).view(wl.n_workers, n)
     dy = torch.randn(wl.n_workers, n, cols, generator=g, device=device) * 1e-3
     return {"layer": wl.table.names[layer], "tokens": tokens, "dy": dy}
+
+
+def head_batch(wl: Workload, n: int, device="cpu", rank: int = 0):
+    """One batch for the decoder of the language-model workload: ``{"layer", "hidden" [W, n, cols] bf16, "logits" [W, n,
+    rows] bf16 (rows on 16 bytes), "tokens" [W, n] int64, "g_logp": one element}``: hidden states of unit size, logits of a
+    trained model's spread with the given token well above most, the mean loss's derivative."""
+    layer = next(l for l, name in enumerate(wl.table.names) if name.startswith("decoder") and wl.table.kind[l] == MATRIX)
+    rows, cols = int(wl.table.rows[layer]), int(wl.table.cols[layer])
+    g = _gen(device, wl.config_id, 3, rank)
+    hidden = torch.randn(wl.n_workers, n, cols, generator=g, device=device).bfloat16()
+    tokens = torch.randint(0, rows, (wl.n_workers, n), generator=g, device=device)
+    logits = torch.zeros(wl.n_workers, n, (rows + 7) // 8 * 8, dtype=torch.bfloat16, device=device)[:, :, :rows]
+    for k in range(wl.n_workers):
+        z = torch.randn(n, rows, generator=g, device=device) * 2.0
+        logits[k] = z.scatter_(1, tokens[k][:, None], 6.0)
+    return {"layer": wl.table.names[layer], "hidden": hidden, "logits": logits, "tokens": tokens,
+            "g_logp": torch.full((1,), -1.0 / n, device=device)}
