@@ -234,25 +234,27 @@ def _refuse(device, items):
 
 def _rows(t, dtypes, what, device, dims=2):
     """Checks a tensor whose rows (its last dimension) are contiguous and may lie apart; returns its address, its type's
-    number and its shape and strides but the last."""
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{what}: expected a torch tensor")
-    if t.dtype not in dtypes:
+    number and its shape and strides."""
+    try:
+        strides, kind = t.stride(), dtypes.get(t.dtype)
+        if kind is not None and len(strides) == dims and (strides[-1] == 1 or t.shape[-1] <= 1) and t.get_device() == device.index:
+            return t.data_ptr() or None, kind, t.shape, strides
+    except AttributeError:
+        raise ValueError(f"{what}: expected a torch tensor") from None
+    if kind is None:
         raise ValueError(f"{what}: expected one of {list(dtypes)}, got {t.dtype}")
-    if t.dim() != dims:
+    if len(strides) != dims:
         raise ValueError(f"{what}: expected {dims} dimensions, got {tuple(t.shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{what}: expected contiguous rows")
     if not t.is_cuda:
         raise ValueError(f"{what}: expected a CUDA tensor (the library has no CPU path)")
-    if device.index is not None and t.get_device() != device.index:
+    if t.get_device() != device.index:
         raise ValueError(f"{what}: lives on {t.device}, the context on {device}")
-    return t.data_ptr() or None, dtypes[t.dtype], t.shape, t.stride()
+    raise ValueError(f"{what}: expected contiguous rows")
 
 
 def _sized(t, numel, what):
-    """Checks the number of elements of a tensor that may be missing."""
-    if t is not None and isinstance(t, torch.Tensor) and t.numel() != numel:
+    """Checks the number of elements of a tensor that may be missing (what is no tensor is refused with the others)."""
+    if t is not None and getattr(t, "numel", int)() != numel and isinstance(t, torch.Tensor):
         raise ValueError(f"{what}: {t.numel()} elements, expected {numel}")
 
 
@@ -267,6 +269,7 @@ def _stream(stream, index=None) -> Optional[int]:
 class Context:
     """Owns the workspace tensor and the ``acc_ctx``; methods mirror the C entry points."""
 
+    _matrix_shapes = None   # (rows, columns) of each layer, None for VECTOR layers (built by the first call that needs them)
     _embedding_cols = None  # columns of each layer, 0 for VECTOR layers (built by the first embedding call)
 
     def __init__(self, table, n_workers, device="cuda", **cfg_kwargs):
@@ -507,12 +510,14 @@ class Context:
         """Token type of one token per row (None: no tokens)."""
         if tokens is None:
             return 0
-        if not isinstance(tokens, torch.Tensor):
-            raise ValueError("tokens: expected a torch tensor")
-        if tokens.dtype not in _TOKEN_TYPES:
+        kind = _TOKEN_TYPES.get(getattr(tokens, "dtype", None))
+        if kind is None:
+            if not isinstance(tokens, torch.Tensor):
+                raise ValueError("tokens: expected a torch tensor")
             raise ValueError(f"tokens: expected one of {list(_TOKEN_TYPES)}, got {tokens.dtype}")
-        _sized(tokens, n, "tokens")
-        return _TOKEN_TYPES[tokens.dtype]
+        if tokens.numel() != n:
+            raise ValueError(f"tokens: {tokens.numel()} elements, expected {n}")
+        return kind
 
     def acc_token_logprobs(self, logits, tokens=None, logp=None, norm=None, entropy=None, top_index=None, top_logp=None,
                            scale=1.0, stream=None):
@@ -578,10 +583,13 @@ class Context:
         """Weight gradient of layer ``layer`` (its index) from its output's gradient ``dy`` ``[W, n, rows]`` (float32 / bfloat16;
         rows and workers may lie apart) and the checkpoint ``code, scales`` of its input ``[W * n, cols]``, into ``grads``
         ``[W, stride]``; ``workspace`` from ``new_linear_grad_workspace(layer, n)``."""
+        if self._matrix_shapes is None:
+            self._matrix_shapes = [(int(r), int(c)) if q >= 0 else None
+                                   for r, c, q in zip(self.table.rows, self.table.cols, self.q_row)]
         layer = int(layer)
-        if not 0 <= layer < self.n_layers or self.q_row[layer] < 0:
+        if not 0 <= layer < self.n_layers or self._matrix_shapes[layer] is None:
             raise ValueError(f"layer {layer}: expected the index of a MATRIX layer")
-        rows, cols = int(self.table.rows[layer]), int(self.table.cols[layer])
+        rows, cols = self._matrix_shapes[layer]
         at, dt, shape, (dy_stride, ld, _) = _rows(dy, _VALUE_TYPES, "dy", self.device, dims=3)
         n = shape[1]
         if shape[0] != self.n_workers or shape[2] != rows:

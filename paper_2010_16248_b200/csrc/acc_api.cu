@@ -790,7 +790,7 @@ const char* acc_profile_kernel_name(int32_t i) {
       "embedding_lookup_kernel", "embedding_small_kernel", "embedding_keys_kernel", "embedding_hist_kernel",
       "embedding_scan_kernel", "embedding_scatter_kernel", "embedding_sum_kernel", "embedding_join_kernel",
       "logprobs_kernel", "logprobs_grad_kernel", "checkpoint_store_kernel", "checkpoint_load_kernel",
-      "linear_grad_kernel", "linear_join_kernel"};
+      "linear_grad_kernel", "linear_join_kernel", "linear_grad_few_kernel"};
   return (i >= 0 && i < PH_COUNT) ? names[i] : "";
 }
 

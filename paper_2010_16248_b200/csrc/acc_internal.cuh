@@ -74,11 +74,14 @@ enum Phase {
   PH_MOMENTS_PARTIAL, PH_MOMENTS_FINAL,
   PH_ADAMW_COEF, PH_ADAMW, PH_ADAMW_8BIT, PH_CLIP_FACTOR,
   PH_EMB_LOOKUP, PH_EMB_SMALL, PH_EMB_KEYS, PH_EMB_HIST, PH_EMB_SCAN, PH_EMB_SCATTER, PH_EMB_SUM, PH_EMB_JOIN,
-  PH_LOGPROBS, PH_LOGPROBS_GRAD, PH_CKPT_STORE, PH_CKPT_LOAD, PH_LINEAR_GRAD, PH_LINEAR_JOIN,
+  PH_LOGPROBS, PH_LOGPROBS_GRAD, PH_CKPT_STORE, PH_CKPT_LOAD, PH_LINEAR_GRAD, PH_LINEAR_JOIN, PH_LINEAR_FEW,
   PH_COUNT
 };
 
 struct ProfSlot { int phase; cudaEvent_t a, b; };
+
+// What acc_linear_grad's workspace came to for the last layer and number of tokens that were asked about.
+struct LinWorkspace { int layer; long long n; size_t bytes; };
 
 struct Plan {
   std::vector<DevLayer> layers;
@@ -112,6 +115,7 @@ struct acc_ctx {
   int occ_topk_first_pass = 3;       // resident blocks per SM of topk_ef_hist1_kernel (queried at creation)
   int occ_adamw = 1, occ_adamw_8bit = 1;  // resident blocks per SM of the AdamW kernels, likewise
   int last_launches = 0;
+  mutable acc::LinWorkspace linear_workspace{-1, -1, 0};
   bool prof = false;                 // per-kernel event timing on
   std::vector<acc::ProfSlot> prof_slots;
   size_t prof_used = 0;

@@ -2,6 +2,7 @@
 // matrix product on the tensor cores that writes the workers' fp32 gradients.
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -520,6 +521,88 @@ linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, 
   if (warp == kMmaWarp) tmem_free(tmem);
 }
 
+// Few tokens and small layers, where starting the tensor cores is most of the time: a block of 64 rows by 64 columns in fp32,
+// dy and the decoded columns in shared memory, eight rows by two columns a thread.
+constexpr int kFewTokens = 64, kFewTile = 64;
+template <typename T>
+__global__ void __launch_bounds__(256) linear_grad_few_kernel(const LinArgs a, const uint8_t* code, const uint8_t* scales) {
+  __shared__ __align__(16) float sy[kFewTokens][kFewTile];
+  __shared__ __align__(16) float sx[kFewTokens][kFewTile];
+  await_previous();
+  let_next_start();
+  const int tid = threadIdx.x, w = blockIdx.z, row0 = blockIdx.y * kFewTile, col0 = blockIdx.x * kFewTile;
+  const int blocks = (a.cols + ACC_CHECKPOINT_BLOCK - 1) / ACC_CHECKPOINT_BLOCK, code_row = blocks * ACC_CHECKPOINT_BLOCK;
+  // all loads of a thread go out before the first is waited for
+  constexpr int kY = kFewTokens / 4, kX = kFewTokens / 16;
+  T y[kY];
+  unsigned x[kX], byte[kX];
+  const int i = tid & 63, u = 4 * (tid & 15);
+#pragma unroll
+  for (int k = 0; k < kX; ++k) {
+    const int t = (tid >> 4) + 16 * k, c = col0 + u;
+    const bool on = t < a.n && c < code_row;
+    const long long row = (long long)w * a.n + t;
+    x[k] = on ? *reinterpret_cast<const unsigned*>(code + row * code_row + c) : 0u;
+    byte[k] = on ? scales[row * blocks + c / ACC_CHECKPOINT_BLOCK] : 0u;
+  }
+  const T* const dy = static_cast<const T*>(a.dy) + w * a.dy_stride + row0 + i;
+#pragma unroll
+  for (int k = 0; k < kY; ++k) {
+    const int t = (tid >> 6) + 4 * k;
+    y[k] = t < a.n && row0 + i < a.rows ? dy[t * a.ld] : T(0.f);
+  }
+#pragma unroll
+  for (int k = 0; k < kX; ++k) {
+    const float s = __uint_as_float(byte[k] == 0 ? 0x00400000u : byte[k] == 255 ? 0x7fffffffu : byte[k] << 23);
+    float v[4];
+#pragma unroll
+    for (int h = 0; h < 4; h += 2) {
+      unsigned f;
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f) : "h"((unsigned short)(x[k] >> (8 * h))));
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&f));
+      v[h] = p.x * s;
+      v[h + 1] = p.y * s;
+    }
+    *reinterpret_cast<float4*>(&sx[(tid >> 4) + 16 * k][u]) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+#pragma unroll
+  for (int k = 0; k < kY; ++k) {
+    if constexpr (sizeof(T) == 2) sy[(tid >> 6) + 4 * k][i] = __bfloat162float(y[k]);
+    else sy[(tid >> 6) + 4 * k][i] = y[k];
+  }
+  __syncthreads();
+  const int lane = tid & 31, r = 8 * (tid >> 5);
+  float sum[8][2] = {};
+#pragma unroll 8
+  for (int t = 0; t < a.n; ++t) {
+    const float4 y0 = *reinterpret_cast<const float4*>(&sy[t][r]), y1 = *reinterpret_cast<const float4*>(&sy[t][r + 4]);
+    const float yv[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+    const float x0 = sx[t][lane], x1 = sx[t][lane + 32];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      sum[k][0] = fmaf(yv[k], x0, sum[k][0]);
+      sum[k][1] = fmaf(yv[k], x1, sum[k][1]);
+    }
+  }
+  float* const out = a.out + w * a.out_stride + (long long)(row0 + r) * a.cols + col0 + lane;
+  float old[8][2];
+  if (a.accumulate) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        old[k][j] = row0 + r + k < a.rows && col0 + lane + 32 * j < a.cols ? out[(long long)k * a.cols + 32 * j] : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float v = sum[k][j] * a.scale;
+      if (row0 + r + k < a.rows && col0 + lane + 32 * j < a.cols) out[(long long)k * a.cols + 32 * j] = a.accumulate ? old[k][j] + v : v;
+    }
+  }
+}
+
 // G (+)= scale * the splits' sums, in order.
 __global__ void __launch_bounds__(256) linear_join_kernel(const float* part, long long slab, int splits, int W, long long size,
                                                           float* grads, long long stride, float scale, int accumulate) {
@@ -587,12 +670,22 @@ static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n, int most_n, 
   if (p.bytes < 256) p.bytes = 256;
   return p;
 }
+// Whether the kernel for few tokens takes the call: its sums cost 2 W n rows cols operations at the fp32 units' rate, and the
+// tensor cores' way some 8 us more of start.
+static bool few_way(const acc_ctx* ctx, int layer, long long n) {
+  const DevLayer& L = ctx->plan.layers[layer];
+  return n <= kFewTokens && (double)ctx->cfg.n_workers * n * L.rows * L.cols <= 1e8 && L.rows <= 65535 * kFewTile;
+}
 template <DyPath P> static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n) {
   return lin_plan(ctx, layer, n, LinCfg<P>::n, LinCfg<P>::parts);
 }
 size_t linear_grad_workspace(const acc_ctx* ctx, int layer, long long n) {
-  return std::max(lin_plan<DY_TMA>(ctx, layer, n).bytes,
-                  std::max(lin_plan<DY_BF16>(ctx, layer, n).bytes, lin_plan<DY_F32>(ctx, layer, n).bytes));
+  LinWorkspace& last = ctx->linear_workspace;  // (the same question from call to call: 400 plans to weigh for many tokens)
+  if (last.layer != layer || last.n != n)
+    last = {layer, n, few_way(ctx, layer, n) ? 256 :
+            std::max(lin_plan<DY_TMA>(ctx, layer, n).bytes,
+                     std::max(lin_plan<DY_BF16>(ctx, layer, n).bytes, lin_plan<DY_F32>(ctx, layer, n).bytes))};
+  return last.bytes;
 }
 
 template <DyPath P, bool WIDE> static cudaError_t lin_prepare() {
@@ -654,6 +747,15 @@ cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf1
     cudaError_t e = cudaSuccess;
     for (int w = 0; w < W && e == cudaSuccess; ++w) e = cudaMemsetAsync(layer0 + w * stride, 0, sizeof(float) * size, s);
     return e;
+  }
+  if (few_way(ctx, layer, n)) {
+    LinArgs a{};
+    a.dy = dy; a.ld = ld; a.dy_stride = dy_stride;
+    a.n = (int)n; a.rows = L.rows; a.cols = L.cols;
+    a.out = layer0; a.out_stride = stride; a.scale = scale; a.accumulate = accumulate;
+    PhaseTimer pt(ctx, PH_LINEAR_FEW, s);
+    return launch_early(bf16 ? linear_grad_few_kernel<__nv_bfloat16> : linear_grad_few_kernel<float>,
+                        dim3((L.cols + kFewTile - 1) / kFewTile, (L.rows + kFewTile - 1) / kFewTile, W), 256, s, a, code, scales);
   }
   if (encode_tiled() == nullptr) return cudaErrorNotSupported;
   // The checkpoint as bf16, exactly, once for all tiles: a tile's own decoding costs the SM more than its products do (64 tokens

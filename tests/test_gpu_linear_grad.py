@@ -75,7 +75,9 @@ def _check(table, ctx, layer, dy, x, scale=1.0, accumulate=False):
 # (W, n, rows, cols): tiles and steps that end anywhere, several tiles a block, sums split over the tokens
 SIZES = [(1, 1, 1, 1), (1, 64, 128, 256), (1, 16, 8, 16), (2, 3, 5, 7), (1, 65, 129, 257), (3, 100, 130, 33), (2, 35, 300, 650),
          (1, 128, 257, 1030), (1, 4000, 64, 16), (2, 1000, 33, 520), (1, 35, 2600, 650), (8, 200, 700, 130), (1, 2049, 600, 300),
-         (3, 777, 1111, 97)]
+         (3, 777, 1111, 97),
+         # few tokens of layers too large for the kernel of few tokens; just within it; 65 tokens of a small one
+         (8, 40, 2000, 650), (3, 1, 8000, 5000), (1, 64, 1250, 1250), (1, 65, 70, 90), (2, 64, 513, 67)]
 
 
 @pytest.mark.parametrize("W,n,rows,cols", SIZES)
