@@ -486,7 +486,7 @@ __device__ __forceinline__ void select_top(RowShared<THREADS>& sh, const T* row,
 // A row per cluster of `parts` blocks: each takes a stretch of its groups, and the first joins them over the cluster's shared
 // memory.  One pass over the logits; the alternatives cost a second look at a tenth of them, which the L2 cache still holds.
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS, TOP ? 1280 / THREADS : 1) logprobs_kernel(const LogArgs a) {
+__global__ void __launch_bounds__(THREADS, (TOP ? 1280 : sizeof(T) == 2 ? 1536 : 1024) / THREADS) logprobs_kernel(const LogArgs a) {
   namespace cg = cooperative_groups;
   __shared__ __align__(16) RowShared<THREADS> sh;
   await_previous();
