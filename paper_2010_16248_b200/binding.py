@@ -534,7 +534,8 @@ class Context:
                     raise ValueError(f"{what}: expected a tensor [{n}, top]")
                 top = t.shape[1]
         _sized(logp, n, "logp"), _sized(norm, 2 * n, "norm"), _sized(entropy, n, "entropy")
-        self._call("acc_token_logprobs", at, lt, n, vocab, ld, (tokens, None if tokens is None else tokens.dtype, n, "tokens"), tt, float(scale), (logp, f32, n, "logp"),
+        given = None if tokens is None else (tokens, tokens.dtype, n, "tokens")
+        self._call("acc_token_logprobs", at, lt, n, vocab, ld, given, tt, float(scale), (logp, f32, n, "logp"),
                    (norm, f32, 2 * n, "norm"), (entropy, f32, n, "entropy"), top, (top_index, torch.int32, n * top, "top_index"),
                    (top_logp, f32, n * top, "top_logp"), stream=stream)
 
@@ -554,9 +555,10 @@ class Context:
                 raise ValueError(f"{what}: expected a tensor of {n} elements, or of one")
             counts.append(0 if t is None else t.numel())
         _sized(norm, 2 * n, "norm"), _sized(entropy, n, "entropy")
-        self._call("acc_token_logprobs_grad", at, lt, n, vocab, ld, (tokens, None if tokens is None else tokens.dtype, n, "tokens"),
-                   tt, float(scale), (norm, f32, 2 * n, "norm"), (g_logp, f32, 0, "g_logp"), counts[0],
-                   (g_entropy, f32, 0, "g_entropy"), counts[1], (entropy, f32, n, "entropy"), out, ot, ld_out, stream=stream)
+        given = None if tokens is None else (tokens, tokens.dtype, n, "tokens")
+        self._call("acc_token_logprobs_grad", at, lt, n, vocab, ld, given, tt, float(scale), (norm, f32, 2 * n, "norm"),
+                   (g_logp, f32, 0, "g_logp"), counts[0], (g_entropy, f32, 0, "g_entropy"), counts[1],
+                   (entropy, f32, n, "entropy"), out, ot, ld_out, stream=stream)
 
     def _checkpoint(self, code, scale, n, cols):
         """The ``_Arg`` items of a checkpoint of ``n`` rows, its size checked to the element."""
@@ -570,8 +572,8 @@ class Context:
         at, xt, (n, cols), (ld, _) = _rows(x, _VALUE_TYPES, "x", self.device)
         tt = self._row_tokens(tokens, n)
         c, s = self._checkpoint(code, scale, n, cols)
-        self._call("acc_checkpoint_store", at, xt, n, cols, ld, (tokens, None if tokens is None else tokens.dtype, n, "tokens"), tt,
-                   c, s, stream=stream)
+        given = None if tokens is None else (tokens, tokens.dtype, n, "tokens")
+        self._call("acc_checkpoint_store", at, xt, n, cols, ld, given, tt, c, s, stream=stream)
 
     def acc_checkpoint_load(self, code, scale, out, stream=None):
         """The values of a checkpoint into ``out`` ``[n, cols]`` (float32 / bfloat16; rows may lie apart)."""

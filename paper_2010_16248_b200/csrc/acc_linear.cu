@@ -36,7 +36,8 @@ template <DyPath P> struct LinCfg {
   static constexpr int threads = 32 * (P == DY_TMA ? kLoadWarp : kLoadWarp + kLoadWarps);
   static constexpr int smem = stages * stage + kEpiWarps * 32 * kEpiPitch * 4 + 1024;
   // Registers a thread: the sums' warps take what the others give back, within what the block was launched with.
-  static constexpr int launch_regs = P == DY_TMA ? 168 : 96, epi_regs = P == DY_TMA ? 216 : 128, mma_regs = P == DY_TMA ? 56 : 40, load_regs = 88;
+  static constexpr int launch_regs = P == DY_TMA ? 168 : 96, load_regs = 88;
+  static constexpr int epi_regs = P == DY_TMA ? 216 : 128, mma_regs = P == DY_TMA ? 56 : 40;
   static_assert(kEpiWarps * epi_regs + 4 * mma_regs + (threads / 32 - kLoadWarp) * load_regs <= threads / 32 * launch_regs, "");
   // Most steps whose sum stays in the tensor core.  It cuts its sums where fp32 adds round: 44 products of 16 tokens in one sum
   // are 8e-7 off, 1024 of them 1e-5.  So a sum ends after 24 products at most (as many of fp32's three terms) and is added to
@@ -121,7 +122,8 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, int 
       "{\n"
       "  .reg .b32 there;\n"
       "  mapa.shared::cluster.u32 there, %5, 0;\n"
-      "  cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [there];\n"
+      "  cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [there];\n"
       "}\n" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
       : "memory");
@@ -167,12 +169,13 @@ __device__ __forceinline__ bool lin_wait(uint64_t* bar, unsigned parity, int* st
   return false;
 }
 
-// A warp's 32 rows of finished sums, `cols` columns of each lane's row held[], times scale, to or onto rows of the layer.  Blocks of
-// 32 columns turn in shared memory.  A row may start at any element, and a store that ends inside 32 bytes of memory costs as
-// much as two: so a row's block begins up to seven columns early, where 32 bytes do, and the block before leaves those to it.
-// Rows eight apart start at the same place within 32 bytes and go together, one address for four of them.  (Rows of 650 columns,
-// the writing alone: 2.5 TB/s with blocks from the first column, 3.9 with an address each, 5.2 so.)
-// The code stays small -- one copy of the part that writes, for all blocks --: unrolled, it cost 30 us of 300 in instruction fetches.
+// A warp's 32 rows of finished sums, `cols` columns of each lane's row held[], times scale, to or onto rows of the layer.
+// Blocks of 32 columns turn in shared memory.  A row may start at any element, and a store that ends inside 32 bytes of memory
+// costs as much as two: so a row's block begins up to seven columns early, where 32 bytes do, and the block before leaves
+// those to it.  Rows eight apart start at the same place within 32 bytes and go together, one address for four of them.  (Rows
+// of 650 columns, the writing alone: 2.5 TB/s with blocks from the first column, 3.9 with an address each, 5.2 so.)
+// The code stays small -- one copy of the part that writes, for all blocks: unrolled, it cost 30 us of 300 in instruction
+// fetches.
 template <bool ADD, bool WHOLE>
 __device__ __forceinline__ void write_block(uint32_t at, float* out, int start, int ld, int c, int cols, int rows, int lane) {
   const long long step = 8ll * ld;
@@ -207,7 +210,8 @@ __device__ __forceinline__ void write_rows(const float (&held)[HELD], float scal
       if (b != c) continue;
 #pragma unroll
       for (int j = b > 0 ? 0 : 8; j < (b < HELD ? 40 : 8); ++j)
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * (lane * kEpiPitch + j)), "f"(held[b - 8 + j] * scale) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * (lane * kEpiPitch + j)), "f"(held[b - 8 + j] * scale)
+                     : "memory");
     }
     __syncwarp();
     if (rows == 32) {
@@ -249,7 +253,9 @@ struct DyShare {
     return box * kBoxBytes + token * 128 + (((lane >> 2) ^ (token & 7)) << 4) + (lane & 3) * 4;
   }
 };
-__device__ __forceinline__ void store4(uint32_t at, unsigned v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ void store4(uint32_t at, unsigned v) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
 
 // bf16 rows on 4 bytes: words copied asynchronously, two steps ahead of the step that is handed on.
 template <typename Wait, typename Done>
@@ -364,8 +370,12 @@ __device__ __forceinline__ void load_pairs(const LinArgs& a, StepWalk walk, cons
 }
 
 // The blocks of a pair walk over the tiles.  In each, warps 0-7 add up and write the sums of its 128 rows, two warps (half of
-// the columns each) for each quarter of them, warps 9 and 10 issue the copies of dy and of the checkpoint, and where dy cannot be copied eight more warps
-// load it; the first block's warp 8 issues the products of both.  Two sums in tensor memory: one is read while the other grows.
+// the columns each) for each quarter of them, warps 9 and 10 issue the copies of dy and of the checkpoint, and where dy cannot
+// be copied eight more warps load it; the first block's warp 8 issues the products of both.  Two sums in tensor memory: one is
+// read while the other grows.  8 x 700 tokens into 33278 x 650: 287 us (843 TFLOP/s, 37 % of the memory's rate); 187 us with the
+// sums left unwritten, 132 us for the same writing alone: the two meet in the L2 cache, which hands out 2.6 GB of operands
+// meanwhile.  8 x 16384 tokens into 4096 x 1024: 882 us, 1246 TFLOP/s; into 2600 x 650, whose tiles are 8 % and 3 % empty and fill
+// 3.6 waves of 4: 468 us, 945 TFLOP/s.
 template <DyPath P, bool WIDE>
 __global__ void __launch_bounds__(LinCfg<P>::threads, 1)
 linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map) {
@@ -421,7 +431,8 @@ linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, 
             tmem_load16(held_at + (sum & 1) * Cfg::n + c + 16, v + 16);
             tmem_wait_load();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) held[c + j] = decltype(add)::value ? held[c + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+            for (int j = 0; j < 32; ++j)
+              held[c + j] = decltype(add)::value ? held[c + j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
           }
         }
         tc_before_sync();
@@ -598,7 +609,8 @@ __global__ void __launch_bounds__(256) linear_grad_few_kernel(const LinArgs a, c
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float v = sum[k][j] * a.scale;
-      if (row0 + r + k < a.rows && col0 + lane + 32 * j < a.cols) out[(long long)k * a.cols + 32 * j] = a.accumulate ? old[k][j] + v : v;
+      if (row0 + r + k < a.rows && col0 + lane + 32 * j < a.cols)
+        out[(long long)k * a.cols + 32 * j] = a.accumulate ? old[k][j] + v : v;
     }
   }
 }
@@ -670,11 +682,12 @@ static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n, int most_n, 
   if (p.bytes < 256) p.bytes = 256;
   return p;
 }
-// Whether the kernel for few tokens takes the call: its sums cost 2 W n rows cols operations at the fp32 units' rate, and the
-// tensor cores' way some 8 us more of start.
+// Whether the kernel for few tokens takes the call: its sums cost 2 W n rows cols operations at the fp32 units' rate, the tensor
+// cores' way two launches and their start (columns: 650).  On the GPU, 35 tokens into 2600 rows: 7.9 us against 13.0; 64 tokens
+// into 1200: 6.6 and 9.4; into 2400: 9.2 and 8.0; 2 tokens into 33278: 34 and 37.
 static bool few_way(const acc_ctx* ctx, int layer, long long n) {
   const DevLayer& L = ctx->plan.layers[layer];
-  return n <= kFewTokens && (double)ctx->cfg.n_workers * n * L.rows * L.cols <= 1e8 && L.rows <= 65535 * kFewTile;
+  return n <= kFewTokens && (double)ctx->cfg.n_workers * n * L.rows * L.cols <= 7e7 && L.rows <= 65535 * kFewTile;
 }
 template <DyPath P> static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n) {
   return lin_plan(ctx, layer, n, LinCfg<P>::n, LinCfg<P>::parts);
@@ -769,7 +782,9 @@ cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf1
   cudaError_t e = launch_checkpoint(ctx, false, workspace, true, n * W, row, row, nullptr, false, const_cast<uint8_t*>(code),
                                     const_cast<uint8_t*>(scales), s);
   if (e != cudaSuccess) return e;
-  const LinPlan p = tma ? lin_plan<DY_TMA>(ctx, layer, n) : bf16 ? lin_plan<DY_BF16>(ctx, layer, n) : lin_plan<DY_F32>(ctx, layer, n);
+  const LinPlan p = tma    ? lin_plan<DY_TMA>(ctx, layer, n)
+                    : bf16 ? lin_plan<DY_BF16>(ctx, layer, n)
+                           : lin_plan<DY_F32>(ctx, layer, n);
   const bool split = p.splits > 1;
   float* const sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.x_bytes);
   LinArgs a{};
@@ -793,9 +808,10 @@ cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf1
     using Tma = std::integral_constant<DyPath, DY_TMA>;
     using Bf16 = std::integral_constant<DyPath, DY_BF16>;
     using F32 = std::integral_constant<DyPath, DY_F32>;
-    // words of two bf16, pairs of floats, where every row starts on one
-    const uintptr_t each = address | (uintptr_t)(n > 1 ? ld : 0) * (bf16 ? 2 : 4) | (uintptr_t)(W > 1 ? dy_stride : 0) * (bf16 ? 2 : 4);
-    const bool wide = each % (bf16 ? 4 : 8) == 0;
+    // pairs of values, where every row starts on one
+    const int size = bf16 ? 2 : 4;
+    const uintptr_t each = address | (uintptr_t)(n > 1 ? ld : 0) * size | (uintptr_t)(W > 1 ? dy_stride : 0) * size;
+    const bool wide = each % (2 * size) == 0;
     if (tma) e = go(Tma(), std::true_type());
     else if (bf16) e = wide ? go(Bf16(), std::true_type()) : go(Bf16(), std::false_type());
     else e = wide ? go(F32(), std::true_type()) : go(F32(), std::false_type());

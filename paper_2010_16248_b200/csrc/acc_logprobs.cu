@@ -72,7 +72,8 @@ template <> struct Eight<__nv_bfloat16> {
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
   }
   __device__ __forceinline__ void pairs(float2* v, float least) const {
-    const unsigned l = __float_as_uint(least) >> 16, l2 = l | l << 16, w[4] = {max2(a.x, l2), max2(a.y, l2), max2(a.z, l2), max2(a.w, l2)};
+    const unsigned l = __float_as_uint(least) >> 16, l2 = l | l << 16;
+    const unsigned w[4] = {max2(a.x, l2), max2(a.y, l2), max2(a.z, l2), max2(a.w, l2)};
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
   }
@@ -484,7 +485,12 @@ __device__ __forceinline__ void select_top(RowShared<THREADS>& sh, const T* row,
 }
 
 // A row per cluster of `parts` blocks: each takes a stretch of its groups, and the first joins them over the cluster's shared
-// memory.  One pass over the logits; the alternatives cost a second look at a tenth of them, which the L2 cache still holds.
+// memory.  One pass over the logits.  5600 rows of 33278, a tenth padding, fp32 85 % and bf16 82 % of the memory's rate (62 us,
+// 336 MB): the exponentials alone keep their unit busy half of that time, and a row's end (two joins, a logarithm) is not hidden
+// by other rows altogether.  The alternatives cost a second look at a tenth of the logits, in pieces of 16 bytes: 2048 rows of
+// 131071 with 20 take 117 us where 87 do without, and read 640 MB where 483 are there.  (Tried: a bar from a row's first quarter
+// and a list of what passes it afterwards, 134 us; the largest of every 2 KB kept and only those read again, 114 us but 5 us
+// more on rows of a few thousand.)
 template <typename T, bool ENT, bool TOP, int THREADS>
 __global__ void __launch_bounds__(THREADS, (TOP ? 1280 : sizeof(T) == 2 ? 1536 : 1024) / THREADS) logprobs_kernel(const LogArgs a) {
   namespace cg = cooperative_groups;
@@ -501,7 +507,8 @@ __global__ void __launch_bounds__(THREADS, (TOP ? 1280 : sizeof(T) == 2 ? 1536 :
   }
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   const RowSpan r = RowSpan::of(z, a.vocab);
-  const int first = (int)((long long)r.groups * part >> a.parts_log2), last = (int)((long long)r.groups * (part + 1) >> a.parts_log2);
+  const int first = (int)((long long)r.groups * part >> a.parts_log2);
+  const int last = (int)((long long)r.groups * (part + 1) >> a.parts_log2);
   // the singles before the groups belong to the first part, those behind them to the last
   const int single = tid < 7 ? (part == 0 ? tid : -1) : tid < 14 && part == parts - 1 ? tid : -1;
   const Scale& c = a.c;
@@ -628,14 +635,16 @@ __global__ void __launch_bounds__(256) logprobs_warp_kernel(const LogArgs a) {
   if (lane < a.top) write_top(a, row, lane, bests[warp][lane], all.m, log_s);
 }
 
-// Rows up to the first length take a warp each, and up to the second where that leaves every SM its warps (65536 rows of 2000 in
-// bf16: 105 us with a block of 128 threads each).
+// Rows up to the first length take a warp each, and up to the second where that leaves every SM its warps: 65536 rows of 2000 in
+// bf16 53 us, with a block of 128 threads each 105; 16384 of 8000 51 and 53.
 constexpr int kWarpVocab = 1024, kWarpVocabMany = 8192;
 static bool warp_rows(const acc_ctx* ctx, long long n, int vocab) {
   return vocab <= kWarpVocab || (vocab <= kWarpVocabMany && n >= 32ll * ctx->sm_count);
 }
 
-// Blocks per row: as many as keep the GPU busy when there are few rows, each with a stretch worth a block's start.
+// Blocks per row: as many as keep the GPU busy when there are few rows, each with a stretch worth a block's start.  One row of
+// 33278 in fp32 with five alternatives on the GPU: 7.0 us in eight parts, 11.2 in one; 64 rows 8.7 and 11.7; 150 rows 10.4 in two
+// and 12.0 in one; 600 rows of 131071 with 20: 48 us in one, 58 in eight.
 static int row_parts_log2(const acc_ctx* ctx, long long n, int vocab) {
   int p = 0;
   while (p < 3 && (n << (p + 1)) <= 4ll * ctx->sm_count && vocab >> (p + 1) >= 2048) ++p;
@@ -663,15 +672,16 @@ cudaError_t launch_token_logprobs(acc_ctx* ctx, const void* logits, bool bf16, l
                              : (ent ? logprobs_kernel<T, true, false, N> : logprobs_kernel<T, false, false, N>);
       return launch_early_as(kernel, (unsigned)(n << a.parts_log2), N, 0, 1 << a.parts_log2, s, a);
     };
-    // Rows of 33278 in bf16, 5040 of them: 64 us with 128 threads a row and 68 with 256 (more rows' ends overlap); 2048 rows of 131071:
-    // 99 us and 88 (fewer rows are left for the last wave).
+    // 5600 rows of 33278 in bf16: 70 us with 128 threads a row and 73 with 256 (more rows' ends overlap); 2048 rows of 131071:
+    // 101 us and 89 (fewer rows are left for the last wave).
     return vocab < 65536 ? block(std::integral_constant<int, 128>()) : block(std::integral_constant<int, 256>());
   };
   return bf16 ? go(__nv_bfloat16()) : go(0.f);
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------
-// dz_j = scale [ g (1[j = token] - p_j) - h p_j (log p_j + H) ]  with  log p_j = (z_j - max) scale - log S.
+// dz_j = scale [ g (1[j = token] - p_j) - h p_j (log p_j + H) ]  with  log p_j = (z_j - max) scale - log S.  5600 rows of 33278 in
+// bf16, a tenth padding: 112 us, 6.3 TB/s of reading and writing.
 
 struct LogGradArgs {
   const void* logits;
@@ -786,7 +796,8 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const LogGradArgs a)
   }
 }
 
-// Blocks of a row: one where there are rows enough (its start, a chain of loads, is then paid once), more where there are few.
+// Blocks of a row: one where there are rows enough (its start, a chain of loads, is then paid once: 5600 rows of 33278 took 149 us
+// in five blocks each and take 119 in one), more where there are few (64 rows of 131071 in fp32: 11.5 us in 37, 19.3 in one).
 static int grad_segments(const acc_ctx* ctx, long long n, int vocab) {
   const long long some = (16ll * ctx->sm_count + n - 1) / n, most = (vocab + 2047) / 2048;
   return (int)std::max<long long>(1, std::min(some, most));
