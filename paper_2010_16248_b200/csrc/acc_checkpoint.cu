@@ -12,8 +12,13 @@ namespace acc {
 constexpr int kBlock = ACC_CHECKPOINT_BLOCK;  // columns that share a scale
 static_assert(kBlock == 32, "two lanes of sixteen columns hold a block");
 
-__device__ __forceinline__ float as_float(float x) { return x; }
-__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+// The larger magnitudes of two pairs of bf16, NaN when one is (a of magnitudes); one instruction, where the integer maximum of
+// two halves takes several.
+__device__ __forceinline__ unsigned max_abs2(unsigned a, unsigned b) {
+  unsigned y;
+  asm("{\n  .reg .b32 m;\n  abs.bf16x2 m, %2;\n  max.NaN.bf16x2 %0, %1, m;\n}\n" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
 __device__ __forceinline__ unsigned as_bits(float x) { return __float_as_uint(x); }
 __device__ __forceinline__ unsigned as_bits(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
 
@@ -28,6 +33,7 @@ struct CkptArgs {
   int blocks;           // of a row
   int units;            // of a row
   float inv_units;
+  bool narrow;          // all units' numbers fit 32 bits (a division of 64 is a hundred instructions)
   const char *first, *end;  // the rows' bytes
 };
 
@@ -38,7 +44,7 @@ struct CkptPlace {
   int unit;
   template <int UNITS> __device__ __forceinline__ static CkptPlace of(const CkptArgs& a, int k) {
     const long long base = (long long)blockIdx.x * (blockDim.x * UNITS);
-    const long long row0 = base / a.units;
+    const long long row0 = a.narrow ? (long long)((unsigned)base / (unsigned)a.units) : base / a.units;
     const int from = (int)(base - row0 * a.units), way = k * (int)blockDim.x + (int)threadIdx.x;
     int at = from + way;
     CkptPlace p;
@@ -61,25 +67,27 @@ constexpr int kCkptThreads = 256;
 template <typename T> constexpr int kStoreUnits = 4 / (int)sizeof(T);
 constexpr int kLoadUnits = 4;
 
-// The bits of sixteen neighbouring values of a row, columns behind the row zeros.  ROWS16: every row starts on 16 bytes.
-// Otherwise the 16-byte pieces around the values are loaded -- inside the rows' bytes, so at their first and last the values come
-// one by one -- and moved by whole words, then by half of one.
+// The bits of sixteen neighbouring values of a row, columns behind the row zeros: the 16-byte pieces that hold them, moved (rows
+// that do not start on 16 bytes: !ROWS16) by whole words, then by half of one.  Pieces may hold bytes of a neighbouring row or
+// of what lies between, but none from outside the rows: at their first and last the values come one by one.
 template <typename T> constexpr int kWords = 16 * (int)sizeof(T) / 4;
 template <typename T, bool ROWS16>
 __device__ __forceinline__ void load_sixteen(const CkptArgs& a, long long row, int c, unsigned* w) {
   constexpr int N = kWords<T>;
   const T* const p = static_cast<const T*>(a.x) + row * a.ld + c;
+  const int live = min(16, a.cols - c);
+  if (live <= 0) return;  // (w holds zeros)
   const char* const at = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
-  const int by = ROWS16 ? 0 : (int)(reinterpret_cast<uintptr_t>(p) & 15);
-  if (c + 16 <= a.cols && (by == 0 || (at >= a.first && at + 4 * N + 16 <= a.end))) {
+  const int by = ROWS16 ? 0 : (int)(reinterpret_cast<uintptr_t>(p) & 15), pieces = (by + live * (int)sizeof(T) + 15) / 16;
+  if (at >= a.first && at + 16 * pieces <= a.end) {
     unsigned v[N + 4];
 #pragma unroll
-    for (int k = 0; k < N / 4 + 1; ++k) {
-      if (k == N / 4 && by == 0) break;
-      const uint4 x = __ldcs(reinterpret_cast<const uint4*>(at) + k);
+    for (int k = 0; k < N / 4 + !ROWS16; ++k) {
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (k < pieces) x = __ldcs(reinterpret_cast<const uint4*>(at) + k);
       v[4 * k] = x.x; v[4 * k + 1] = x.y; v[4 * k + 2] = x.z; v[4 * k + 3] = x.w;
     }
-    if (!ROWS16 && by != 0) {
+    if (!ROWS16) {
 #pragma unroll
       for (int k = 0; k < N + 3; ++k) v[k] = by & 4 ? v[k + 1] : v[k];
 #pragma unroll
@@ -91,12 +99,19 @@ __device__ __forceinline__ void load_sixteen(const CkptArgs& a, long long row, i
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) w[k] = v[k];
+    if (live < 16) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (sizeof(T) == 4) w[k] = k < live ? w[k] : 0u;
+        else w[k] = 2 * k + 1 < live ? w[k] : 2 * k < live ? w[k] & 0xffffu : 0u;
+      }
+    }
   } else {
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const unsigned b = c + k < a.cols ? as_bits(p[k]) : 0u;
-      if (sizeof(T) == 4) w[k] = b;
-      else w[k / 2] = k & 1 ? w[k / 2] | b << 16 : b;
+      if (k >= live) break;
+      if (sizeof(T) == 4) w[k % N] = as_bits(p[k]);
+      else w[k / 2] |= as_bits(p[k]) << (16 * (k & 1));
     }
   }
 }
@@ -138,7 +153,7 @@ __global__ void __launch_bounds__(kCkptThreads) checkpoint_store_kernel(const Ck
     unsigned top = 0;
     if (sizeof(T) == 2) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) top = __vmaxu2(top, w[u][k] & 0x7fff7fffu);
+      for (int k = 0; k < N; ++k) top = max_abs2(top, w[u][k]);
       top = max(top << 16, top & 0xffff0000u);
     } else {
 #pragma unroll
@@ -257,11 +272,12 @@ cudaError_t launch_checkpoint(acc_ctx* ctx, bool store, void* x, bool bf16, long
                               const void* tokens, bool tok64, uint8_t* code, uint8_t* scale, cudaStream_t s) {
   const int blocks = (cols + kBlock - 1) / kBlock, size = bf16 ? 2 : 4;
   const char* const first = static_cast<const char*>(x);
-  CkptArgs a{x, n, ld, cols, tokens, tok64, code, scale, blocks, 0, 0.f, first, first + ((n - 1) * ld + cols) * size};
+  CkptArgs a{x, n, ld, cols, tokens, tok64, code, scale, blocks, 0, 0.f, false, first, first + ((n - 1) * ld + cols) * size};
   const bool rows16 = (reinterpret_cast<uintptr_t>(x) | (n > 1 ? (uintptr_t)(ld * size) : 0)) % 16 == 0;
   // a row's pieces of 16 bytes of output are one more where it starts inside one
   a.units = store ? 2 * blocks : (cols + 16 / size - 1) / (16 / size) + !rows16;
   a.inv_units = 1.f / (float)a.units;
+  a.narrow = n * a.units < (1ll << 32) - (1 << 16);
   PhaseTimer pt(ctx, store ? PH_CKPT_STORE : PH_CKPT_LOAD, s);
   auto go = [&](auto t) {
     using T = decltype(t);
