@@ -118,9 +118,9 @@ __device__ __forceinline__ void load_sixteen(const CkptArgs& a, long long row, i
 
 // Codes and scales of a row, sixteen columns a thread.  The scale's byte is the exponent that brings the largest magnitude of the
 // block into [128, 256); the product with its inverse is exact (but below 2^-126, far below the least code), and rounding to
-// the nearest e4m3 is the only one.  131072 rows of 650 in bf16, a tenth padding: 53 us, 4.6 TB/s (issuing: 43 M warp
-// instructions, 60 % of the warps resident); eight columns a thread took 72 us, with a 64-bit division for each 115.  Rows that
-// start on 4 bytes: 75 us, and 167 with 4-byte loads.
+// the nearest e4m3 is the only one.  131072 rows of 650 in bf16, a tenth padding: 49 us, 5.0 TB/s (it issues in 78 % of the
+// cycles, 14 instructions a value; 53 us with the rows' last columns one by one, 72 with eight columns a thread, 115 with a 64-bit
+// division for each).  Rows that start on 4 bytes: 60 us, and 167 with 4-byte loads.
 template <typename T, bool ROWS16>
 __global__ void __launch_bounds__(kCkptThreads) checkpoint_store_kernel(const CkptArgs a) {
   await_previous();
