@@ -371,8 +371,8 @@ int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type
  *   with x read from a checkpoint [W][n] and G_w the layer in worker w's slice of grads [W][worker_stride].  accumulate = 0
  *   writes the layer, nothing outside it is touched; accumulate != 0 adds to it (micro-batches, shared weights).  dy holds
  *   rows of rows_l elements, ld apart, workers dy_stride apart (each >= rows_l where there is more than one), fp32 or bf16.
- *   Products are those of fp32 (fp32 values of dy count with all 24 bits), sums in fp32 on the tensor cores in an order that
- *   depends on the sizes and types alone: bit-reproducible.  Every token counts: a padded one's dy has to be zeros (as
+ *   Products are those of fp32 (fp32 values of dy count with all 24 bits), sums in fp32 in an order that depends on the
+ *   sizes, the types and dy's alignment alone: bit-reproducible.  Every token counts: a padded one's dy has to be zeros (as
  *   acc_token_logprobs_grad leaves it) and its checkpoint finite.  workspace: acc_linear_grad_workspace_bytes(layer, n)
  *   bytes of DEVICE memory, 256-byte aligned, caller-owned, for one call at a time; contents before and after do not matter.
  * Device pointers: x, out, dy (element-aligned), code [n][ceil(cols/32)*32] (16-byte aligned), code_scale
