@@ -661,7 +661,8 @@ static LinPlan lin_plan(const acc_ctx* ctx, int layer, long long n, int most_n, 
   const long long pairs = ctx->sm_count / 2;
   const int least = (L.cols + most_n - 1) / most_n;
   double best = -1.0;
-  for (int nt = least; nt <= 4 * least && (nt == least || L.cols / nt >= 32); ++nt) {
+  // (a wide layer has tiles enough: a few counts above the least are weighed, not all)
+  for (int nt = least; nt <= std::min(4 * least, least + 12) && (nt == least || L.cols / nt >= 32); ++nt) {
     const int tile_n = ((L.cols + nt - 1) / nt + 31) / 32 * 32, n_tiles = (L.cols + tile_n - 1) / tile_n;
     const long long tiles = (long long)W * p.m_tiles * n_tiles;
     const double each = tile_n / 256.0, step = std::max(each, most_n * 0.875 / 256.0);
