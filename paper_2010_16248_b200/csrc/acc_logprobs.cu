@@ -141,19 +141,21 @@ struct RowSpan {
 };
 
 // The running statistics of a set of logits z with largest m: s = sum 2^d, t = sum 2^d d.  d = z c2 - ref(m), one rounding, with
-// c2 = scale log2(e) and ref(m) = m c2 rounded, which the row's end puts right: 2^(m c2 - ref(m)) is known to all its bits.
-// Where m c2 nears fp32's range (a row of the type's lowest value) d = (z - m) c2 instead.  A distance below -200 counts as
-// -200, where 2^d is 0: -inf and the type's lowest value then add nothing, not 0 * inf.
+// c2 = scale log2(e) and ref(m) = m c2 rounded: the largest logit's own d is then what ref(m) left out, left(m), not 0, and the
+// row's end puts that right.  It is half a step of m c2, 2^-5 at most below the limit of 2^20; from there on, where it would grow
+// until 2^d is no number of use, d = (z - m) c2.  Sums that count from unlike references are brought together by their lefts.
+// A distance below -200 counts as -200, where 2^d is 0: -inf and masks of any size then add nothing, not 0 * inf.
 struct Scale {
   float c2, limit, least;  // |m| below limit has a ref; a logit below `least` counts as `least`: its 2^d is 0, and d finite
   static Scale of(float scale) {
     const float c2 = scale * kLog2e;
-    return {c2, 0x1p100f / c2, -0x1p120f / c2};
+    return {c2, 0x1p20f / c2, -0x1p120f / c2};
   }
   __device__ __forceinline__ bool near(float m) const { return fabsf(m) < limit; }
   __device__ __forceinline__ float ref(float m) const { return __fmul_rn(m, c2); }  // (never part of an fma)
+  __device__ __forceinline__ float left(float m) const { return near(m) ? fmaf(m, c2, -ref(m)) : 0.f; }
   __device__ __forceinline__ float distance(float z, float m) const {
-    return fmaxf(near(z) && near(m) ? ref(z) - ref(m) : (z - m) * c2, -200.f);
+    return fmaxf(near(z) && near(m) ? ref(z) - ref(m) : fmaf(z - m, c2, left(m) - left(z)), -200.f);
   }
 };
 struct Stats { float m, s, t; };
@@ -301,7 +303,7 @@ __device__ __forceinline__ float finish_row(const LogArgs& a, long long row, con
   const Scale& k = a.c;
   // (s and t count from ref(m): the distance of m from it enters log S, and cancels in the entropy)
   float log_s = logf(s.s), entropy = log_s - s.t / s.s * kLn2;
-  if (k.near(s.m)) log_s -= fmaf(s.m, k.c2, -k.ref(s.m)) * kLn2;
+  log_s -= k.left(s.m) * kLn2;
   if (s.m == kMinusInf) log_s = entropy = 0.f;  // nothing to choose from
   if (!(s.m < -kMinusInf)) log_s = entropy = not_a_number();
   if (a.norm != nullptr) a.norm[row] = make_float2(s.m, log_s);
