@@ -147,9 +147,11 @@ struct RowSpan {
 // A distance below -200 counts as -200, where 2^d is 0: -inf and masks of any size then add nothing, not 0 * inf.
 struct Scale {
   float c2, limit, least;  // |m| below limit has a ref; a logit below `least` counts as `least`: its 2^d is 0, and d finite
+  // (`least` is finite too.  At a scale so small that the type's lowest value may have a share of the row nothing is near: each d
+  // is bounded itself, and -inf alone has none.)
   static Scale of(float scale) {
     const float c2 = scale * kLog2e;
-    return {c2, 0x1p20f / c2, -0x1p120f / c2};
+    return {c2, c2 < 0x1p-100f ? 0.f : 0x1p20f / c2, std::max(-0x1p120f / c2, -0x1.fffffep127f)};
   }
   __device__ __forceinline__ bool near(float m) const { return fabsf(m) < limit; }
   __device__ __forceinline__ float ref(float m) const { return __fmul_rn(m, c2); }  // (never part of an fma)

@@ -112,3 +112,20 @@ def test_rows_around_the_references_limit(factor, center, vocab):
 def test_scales(scale, dtype, vocab):
     rng = np.random.default_rng(vocab)
     _check(rng.normal(0, 2.0, (5, vocab)), dtype, scale)
+
+
+@pytest.mark.parametrize("scale", [3e-3, 2e-3, 1e-3, 1e-4, 1e-6, 1e-20, 1e-30, 1e-36, 1e-37, 1e-38])
+@pytest.mark.parametrize("mask", ["-inf", "lowest", "both"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [9, 900, 9000])
+def test_masks_at_small_scales(scale, mask, dtype, vocab):
+    """A logit of -inf has no share of the row whatever the scale; a finite one does where the scale leaves it one."""
+    rng = np.random.default_rng(vocab)
+    z = rng.normal(0, 2.0, (4, vocab))
+    at = rng.random((4, vocab))
+    if mask != "-inf":
+        z[at < 0.3] = float(torch.finfo(dtype).min)
+    if mask != "lowest":
+        z[at > 0.7] = -np.inf
+    z[2] = -np.inf if mask == "-inf" else float(torch.finfo(dtype).min)
+    _check(z, dtype, scale)
