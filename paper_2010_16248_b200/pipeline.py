@@ -8,6 +8,7 @@ arithmetic happens in the library's kernels; nothing here reads results back to 
 """
 from __future__ import annotations
 
+import itertools
 from typing import Optional, Sequence
 
 import torch
@@ -92,10 +93,42 @@ class CheckpointedLinear:
         self.code, self.code_scale = ctx.new_checkpoint(ctx.n_workers * self.n, self.cols)
         self.workspace = ctx.new_linear_grad_workspace(self.layer, self.n)
 
+    def _runs(self, t, width):
+        """``t`` ``[W, n, width]`` as ``(first row, end, rows)``: one run where its rows lie at one distance from another, else one
+        for each worker.  Nothing is copied: a copy would be made on another stream than the call's."""
+        try:
+            runs = (t.view(-1, width),)
+        except RuntimeError:
+            runs = t.unbind(0)
+        ends = list(itertools.accumulate(r.shape[0] for r in runs))
+        if ends[-1:] != [self.ctx.n_workers * self.n] or runs[0].shape[-1] != width:
+            raise ValueError(f"expected {self.ctx.n_workers * self.n} rows of {width} elements, got {tuple(t.shape)}")
+        return [(end - r.shape[0], end, r) for end, r in zip(ends, runs)]
+
+    def _part(self, t, first, end, what):
+        """What belongs to the rows ``first`` to ``end`` of a tensor with one element for every row (or one for all, or None)."""
+        rows = self.ctx.n_workers * self.n
+        if end - first == rows or t is None:
+            return t
+        if not isinstance(t, torch.Tensor) or t.numel() not in (1, rows) or not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous tensor of {rows} elements")
+        return t.view(-1)[first:end] if t.numel() == rows else t
+
+    def _own(self, t, first, end):
+        """The same of a buffer ``[W * n, ...]`` or ``[W, n, ...]`` of this object."""
+        if t is None or end - first == self.ctx.n_workers * self.n:
+            return t
+        return (t if t.shape[0] == self.ctx.n_workers * self.n else t.flatten(0, 1))[first:end]
+
     def keep(self, x: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None) -> int:
-        """``x`` ``[W, n, cols]``; rows of negative ``tokens`` ``[W, n]`` are kept as zeros.  Returns the kernels launched."""
-        self.ctx.acc_checkpoint_store(x.reshape(-1, self.cols), self.code, self.code_scale, tokens, stream)
-        return self.ctx.last_launch_count()
+        """``x`` ``[W, n, cols]`` (workers and tokens may lie apart, in any order); rows of negative ``tokens`` ``[W, n]`` are kept as
+        zeros.  Returns the kernels launched: one, or one per worker."""
+        launches = 0
+        for first, end, rows in self._runs(x, self.cols):
+            self.ctx.acc_checkpoint_store(rows, self._own(self.code, first, end), self._own(self.code_scale, first, end),
+                                          self._part(tokens, first, end, "tokens"), stream)
+            launches += self.ctx.last_launch_count()
+        return launches
 
     def kept(self, out: torch.Tensor, stream=None) -> torch.Tensor:
         """The input as it was kept, into ``out`` ``[W, n, cols]``."""
@@ -130,20 +163,26 @@ class TokenHead(CheckpointedLinear):
         """A buffer ``[W, n, rows]`` for the logits, whose rows start on 16 bytes."""
         return self.dlogits.new_zeros(self.ctx.n_workers, self.n, self.dlogits.stride(1))[:, :, :self.rows]
 
-    def _flat(self, t):
-        return t.view(-1, self.rows) if t.is_contiguous() else t.flatten(0, 1)
-
     def forward(self, logits: torch.Tensor, tokens: torch.Tensor, stream=None) -> int:
-        """Fills ``logp``, ``entropy``, ``norm`` (and the alternatives) from ``logits`` ``[W, n, rows]`` and ``tokens``."""
-        self.ctx.acc_token_logprobs(self._flat(logits), tokens, self.logp, self.norm, self.entropy, self.top_index, self.top_logp,
-                                    self.logit_scale, stream)
-        return self.ctx.last_launch_count()
+        """Fills ``logp``, ``entropy``, ``norm`` (and the alternatives) from ``logits`` ``[W, n, rows]`` (workers and tokens may lie
+        apart, in any order) and ``tokens`` ``[W, n]``.  Returns the kernels launched: one, or one per worker."""
+        launches = 0
+        for first, end, rows in self._runs(logits, self.rows):
+            own = [self._own(t, first, end) for t in (self.logp, self.norm, self.entropy, self.top_index, self.top_logp)]
+            self.ctx.acc_token_logprobs(rows, self._part(tokens, first, end, "tokens"), *own, self.logit_scale, stream)
+            launches += self.ctx.last_launch_count()
+        return launches
 
     def backward_logits(self, logits: torch.Tensor, tokens: torch.Tensor, g_logp=None, g_entropy=None, stream=None) -> int:
         """``dlogits`` from the loss's derivatives by ``logp`` and ``entropy`` (``[W, n]``, or one element)."""
-        self.ctx.acc_token_logprobs_grad(self._flat(logits), tokens, self.norm, self._flat(self.dlogits), g_logp, g_entropy,
-                                         self.entropy, self.logit_scale, stream)
-        return self.ctx.last_launch_count()
+        launches, dlogits = 0, self.dlogits.flatten(0, 1)
+        for first, end, rows in self._runs(logits, self.rows):
+            given, g, h = (self._part(t, first, end, what) for t, what in
+                           ((tokens, "tokens"), (g_logp, "g_logp"), (g_entropy, "g_entropy")))
+            self.ctx.acc_token_logprobs_grad(rows, given, self._own(self.norm, first, end), self._own(dlogits, first, end), g, h,
+                                             self._own(self.entropy, first, end), self.logit_scale, stream)
+            launches += self.ctx.last_launch_count()
+        return launches
 
 
 def _make_optimizer(optimizer, ctx, stride, dev):
