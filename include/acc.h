@@ -375,6 +375,7 @@ int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type
  *   sizes, the types and dy's alignment alone: bit-reproducible.  Every token counts: a padded one's dy has to be zeros (as
  *   acc_token_logprobs_grad leaves it) and its checkpoint finite.  workspace: acc_linear_grad_workspace_bytes(layer, n)
  *   bytes of DEVICE memory, 256-byte aligned, caller-owned, for one call at a time; contents before and after do not matter.
+ *   (Host threads may ask for sizes at the same time.)
  * Device pointers: x, out, dy (element-aligned), code [n][ceil(cols/32)*32] (16-byte aligned), code_scale
  * [n][ceil(cols/32)] (no alignment), tokens [n], grads (16-byte aligned).  n = 0 is allowed; n (gradient: W * n) is at most
  * ACC_MAX_TOKENS, cols at most 2^30, otherwise ACC_EINVAL.  bf16 rows of dy that start on 16 bytes (ld and dy_stride multiples of 8) are the

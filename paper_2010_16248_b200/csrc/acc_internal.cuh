@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
 #include <vector>
 
 #include "acc.h"
@@ -80,8 +81,14 @@ enum Phase {
 
 struct ProfSlot { int phase; cudaEvent_t a, b; };
 
-// What acc_linear_grad's workspace came to for the last layer and number of tokens that were asked about.
-struct LinWorkspace { int layer; long long n; size_t bytes; };
+// What acc_linear_grad's workspace came to for the last layer and number of tokens that were asked about; host threads may ask at
+// the same time.
+struct LinWorkspace {
+  int layer = -1;
+  long long n = -1;
+  size_t bytes = 0;
+  std::mutex lock;
+};
 
 struct Plan {
   std::vector<DevLayer> layers;
@@ -115,7 +122,7 @@ struct acc_ctx {
   int occ_topk_first_pass = 3;       // resident blocks per SM of topk_ef_hist1_kernel (queried at creation)
   int occ_adamw = 1, occ_adamw_8bit = 1;  // resident blocks per SM of the AdamW kernels, likewise
   int last_launches = 0;
-  mutable acc::LinWorkspace linear_workspace{-1, -1, 0};
+  mutable acc::LinWorkspace linear_workspace;
   bool prof = false;                 // per-kernel event timing on
   std::vector<acc::ProfSlot> prof_slots;
   size_t prof_used = 0;

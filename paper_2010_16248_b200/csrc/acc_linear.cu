@@ -695,11 +695,18 @@ template <DyPath P> static LinPlan lin_plan(const acc_ctx* ctx, int layer, long 
 }
 size_t linear_grad_workspace(const acc_ctx* ctx, int layer, long long n) {
   LinWorkspace& last = ctx->linear_workspace;  // (the same question from call to call: 400 plans to weigh for many tokens)
-  if (last.layer != layer || last.n != n)
-    last = {layer, n, few_way(ctx, layer, n) ? 256 :
-            std::max(lin_plan<DY_TMA>(ctx, layer, n).bytes,
-                     std::max(lin_plan<DY_BF16>(ctx, layer, n).bytes, lin_plan<DY_F32>(ctx, layer, n).bytes))};
-  return last.bytes;
+  {
+    std::lock_guard<std::mutex> hold(last.lock);
+    if (last.layer == layer && last.n == n) return last.bytes;
+  }
+  const size_t bytes = few_way(ctx, layer, n) ? 256 :
+      std::max(lin_plan<DY_TMA>(ctx, layer, n).bytes,
+               std::max(lin_plan<DY_BF16>(ctx, layer, n).bytes, lin_plan<DY_F32>(ctx, layer, n).bytes));
+  std::lock_guard<std::mutex> hold(last.lock);
+  last.layer = layer;
+  last.n = n;
+  last.bytes = bytes;
+  return bytes;
 }
 
 template <DyPath P, bool WIDE> static cudaError_t lin_prepare() {
