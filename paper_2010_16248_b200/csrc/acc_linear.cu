@@ -464,7 +464,7 @@ linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, 
         const int chunks = lin_chunks<Cfg::chunk>(x);
         int begin = x.from, end = begin, chunk = 0;
         for (int k = x.from; k < x.to; ++k, ++step) {
-          if (k == end) begin = k, end = x.from + (x.to - x.from) * ++chunk / chunks;
+          if (k == end) begin = k, end = x.from + (int)((long long)(x.to - x.from) * ++chunk / chunks);
           const unsigned s = step % S, acc = sum & 1;
           const bool first = k == begin, last = k + 1 == end;
           if (first && !(ok = lin_wait(&sh.acc_empty[acc], ((sum >> 1) & 1) ^ 1, a.status))) break;
