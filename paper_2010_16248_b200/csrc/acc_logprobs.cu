@@ -760,8 +760,10 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const LogGradArgs a)
     else out[i] = v;
   };
   if (!SAME) {
-    const int from = segment * a.stretch, to = ROW_THREADS == 256 ? min(a.vocab, from + a.stretch) : a.vocab;
-    for (int i = from + lane; i < to; i += ROW_THREADS) single(i);
+    // (unsigned: a step past the last element of the longest rows is beyond 2^31)
+    const unsigned from = (unsigned)segment * a.stretch, vocab = a.vocab;
+    const unsigned to = ROW_THREADS == 256 ? min(vocab, from + a.stretch) : vocab;
+    for (unsigned i = from + lane; i < to; i += ROW_THREADS) single((int)i);
     return;
   }
   const int first = segment * a.stretch, last = ROW_THREADS == 256 ? min(r.groups, first + a.stretch) : r.groups;
@@ -803,7 +805,7 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const LogGradArgs a)
 // Blocks of a row: one where there are rows enough (its start, a chain of loads, is then paid once: 5600 rows of 33278 took 149 us
 // in five blocks each and take 119 in one), more where there are few (64 rows of 131071 in fp32: 11.5 us in 37, 19.3 in one).
 static int grad_segments(const acc_ctx* ctx, long long n, int vocab) {
-  const long long some = (16ll * ctx->sm_count + n - 1) / n, most = (vocab + 2047) / 2048;
+  const long long some = (16ll * ctx->sm_count + n - 1) / n, most = (vocab + 2047ll) / 2048;
   return (int)std::max<long long>(1, std::min(some, most));
 }
 static bool grad_warp_rows(const acc_ctx* ctx, long long n, int vocab) { return warp_rows(ctx, n, vocab); }
@@ -823,7 +825,7 @@ cudaError_t launch_token_logprobs_grad(acc_ctx* ctx, const void* logits, bool bf
   const bool warp = grad_warp_rows(ctx, n, vocab);
   if (!warp) {
     a.segments = grad_segments(ctx, n, vocab);
-    a.stretch = ((same ? vocab / 8 : vocab) + a.segments - 1) / a.segments;
+    a.stretch = (int)(((same ? vocab / 8 : vocab) + a.segments - 1ll) / a.segments);
   }
   PhaseTimer pt(ctx, PH_LOGPROBS_GRAD, s);
   auto go = [&](auto in, auto o, auto ent) {
