@@ -231,7 +231,8 @@ int acc_create(const acc_config* cfg, void* workspace, size_t workspace_bytes, a
   if (e == cudaSuccess) e = prepare_powersgd();
   if (e == cudaSuccess) e = prepare_topk(ctx);
   if (e == cudaSuccess) e = prepare_adamw(ctx);
-  if (e == cudaSuccess) e = prepare_linear();
+  if (e == cudaSuccess) ctx->linear_ready = prepare_linear();  // (acc_linear_grad's to report: nothing else needs these kernels)
+  if (ctx->linear_ready != cudaSuccess) cudaGetLastError();    // (taken back: the next call would find it otherwise)
   int dev = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, dev);

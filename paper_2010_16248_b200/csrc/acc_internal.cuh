@@ -122,6 +122,7 @@ struct acc_ctx {
   int occ_topk_first_pass = 3;       // resident blocks per SM of topk_ef_hist1_kernel (queried at creation)
   int occ_adamw = 1, occ_adamw_8bit = 1;  // resident blocks per SM of the AdamW kernels, likewise
   int last_launches = 0;
+  cudaError_t linear_ready = cudaSuccess;  // what preparing the linear gradient's kernels came to
   mutable acc::LinWorkspace linear_workspace;
   bool prof = false;                 // per-kernel event timing on
   std::vector<acc::ProfSlot> prof_slots;

@@ -778,6 +778,7 @@ cudaError_t launch_linear_grad(acc_ctx* ctx, int layer, const void* dy, bool bf1
     return launch_early(bf16 ? linear_grad_few_kernel<__nv_bfloat16> : linear_grad_few_kernel<float>,
                         dim3((L.cols + kFewTile - 1) / kFewTile, (L.rows + kFewTile - 1) / kFewTile, W), 256, s, a, code, scales);
   }
+  if (ctx->linear_ready != cudaSuccess) return ctx->linear_ready;
   if (encode_tiled() == nullptr) return cudaErrorNotSupported;
   // The checkpoint as bf16, exactly, once for all tiles: a tile's own decoding costs the SM more than its products do (64 tokens
   // x 224 columns: 2400 warp instructions for 448 cycles of the tensor core).
