@@ -327,7 +327,7 @@ int acc_embedding_grad(acc_ctx* ctx, int32_t layer, const void* tokens, int32_t 
  * gradient is half of what the step compresses) --------------------------------------------------------------------
  * Rows of logits, fp32 or bf16 (logit_type ACC_F32 / ACC_BF16), `vocab` elements each and `ld` elements apart (ld >= vocab:
  * what lies between the rows is neither read nor written); any start that suits the type.  scale > 0 multiplies the logits
- * (1 / temperature).  Row i, with m = max_j z_j and S = sum_j exp(scale (z_j - m)):
+ * (1 / temperature); scale log2(e) has to be finite in fp32 (any scale up to 2^127).  Row i, with m = max_j z_j and S = sum_j exp(scale (z_j - m)):
  *   norm[2i] = m, norm[2i + 1] = log S;  log p_j = scale (z_j - m) - log S;  logp[i] = log p_tokens[i];
  *   entropy[i] = -sum_j p_j log p_j (a p_j of 0 adds nothing);
  *   top_index[i][k], top_logp[i][k], k < top: the tokens of the `top` largest logits, equal ones by rising index, and their

@@ -575,6 +575,8 @@ static size_t value_size(int type) { return type == ACC_BF16 ? 2 : 4; }
 static size_t token_size(int type) { return type == ACC_I64 ? 8 : 4; }
 static bool known_value(int type) { return type == ACC_F32 || type == ACC_BF16; }
 static bool known_token(int type) { return type == ACC_I32 || type == ACC_I64; }
+// Of logits, which the kernels take in units of log 2.
+static bool known_scale(float scale) { return scale > 0.f && std::isfinite(scale * 1.4426950408889634f); }
 // Rows of `width` elements, `ld` apart, of which a call takes n.
 static bool rows_fit(int64_t n, int64_t width, int64_t ld) {
   return n >= 0 && n <= ACC_MAX_TOKENS && width >= 1 && width <= 0x7fffffff - 16 && (n <= 1 || ld >= width);
@@ -585,7 +587,7 @@ int acc_token_logprobs(acc_ctx* ctx, const void* logits, int32_t logit_type, int
                        const void* tokens, int32_t token_type, float scale, float* logp, float* norm, float* entropy,
                        int32_t top, int32_t* top_index, float* top_logp, void* stream) {
   if (!ctx || !known_value(logit_type) || !known_token(token_type) || !rows_fit(n, vocab, ld)) return ACC_EINVAL;
-  if (!(scale > 0.f) || !std::isfinite(scale) || top < 0 || top > ACC_LOGPROBS_MAX_TOP) return ACC_EINVAL;
+  if (!known_scale(scale) || top < 0 || top > ACC_LOGPROBS_MAX_TOP) return ACC_EINVAL;
   ctx->last_launches = 0;
   if (n == 0) return ACC_OK;
   if ((top > 0) != (top_index != nullptr || top_logp != nullptr)) return ACC_EINVAL;
@@ -604,7 +606,7 @@ int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type
   if (!ctx || !known_value(logit_type) || !known_value(out_type) || !known_token(token_type) || !rows_fit(n, vocab, ld) ||
       !rows_fit(n, vocab, ld_out))
     return ACC_EINVAL;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return ACC_EINVAL;
+  if (!known_scale(scale)) return ACC_EINVAL;
   ctx->last_launches = 0;
   if (n == 0) return ACC_OK;
   if (!logits || !norm || !dlogits || (!g_logp && !g_entropy) || (g_logp && !tokens) || (g_entropy && !entropy))

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from oracle import head_oracle as hor
+from paper_2010_16248_b200 import binding
 from tests.test_gpu_logprobs import _bounds, _ctx, _near, _outputs, _rows
 
 pytestmark = pytest.mark.gpu
@@ -129,3 +130,22 @@ def test_masks_at_small_scales(scale, mask, dtype, vocab):
         z[at > 0.7] = -np.inf
     z[2] = -np.inf if mask == "-inf" else float(torch.finfo(dtype).min)
     _check(z, dtype, scale)
+
+
+def test_largest_scale():
+    """Up to 2^127; where scale log2(e) is beyond fp32 the calls refuse."""
+    rng = np.random.default_rng(7)
+    for vocab in (900, 9000):
+        for peak in (0.0, 3.0, -2.0 ** -100):
+            z = np.minimum(rng.normal(0, 2.0, (3, vocab)), 0.0) + peak
+            z[:, ::17] = peak
+            _check(z, torch.float32, 2.0 ** 127)
+    ctx, z, t = _ctx(), torch.zeros(2, 50, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    logp, norm, one = torch.zeros(2, device="cuda"), torch.zeros(2, 2, device="cuda"), torch.ones(1, device="cuda")
+    for scale in (2.4e38, 3e38):
+        with pytest.raises(binding.AccError) as e:
+            ctx.acc_token_logprobs(z, t, logp=logp, scale=scale)
+        assert e.value.status == 1
+        with pytest.raises(binding.AccError) as e:
+            ctx.acc_token_logprobs_grad(z, t, norm, z.clone(), g_logp=one, scale=scale)
+        assert e.value.status == 1
