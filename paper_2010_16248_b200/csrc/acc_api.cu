@@ -582,6 +582,7 @@ static bool rows_fit(int64_t n, int64_t width, int64_t ld) {
   return n >= 0 && n <= ACC_MAX_TOKENS && width >= 1 && width <= 0x7fffffff - 16 && (n <= 1 || ld >= width);
 }
 constexpr int64_t kMostBlocks = 0x7fffffff;
+constexpr int kMostColumns = 1 << 30;  // of a checkpoint's row
 
 int acc_token_logprobs(acc_ctx* ctx, const void* logits, int32_t logit_type, int64_t n, int32_t vocab, int64_t ld,
                        const void* tokens, int32_t token_type, float scale, float* logp, float* norm, float* entropy,
@@ -629,7 +630,7 @@ static int checkpoint(acc_ctx* ctx, bool store, void* x, int type, int64_t n, in
                       int token_type, uint8_t* code, uint8_t* scale, void* stream) {
   if (!ctx || !known_value(type) || !known_token(token_type) || !rows_fit(n, cols, ld)) return ACC_EINVAL;
   if (n > 0 && (!x || !code || !scale)) return ACC_EINVAL;
-  if (cols > (1 << 30) || n * ((cols + 31ll) / 32 * 8 + 1) / 1024 >= kMostBlocks - 1) return ACC_EINVAL;
+  if (cols > kMostColumns || n * ((cols + 31ll) / 32 * 8 + 1) / 1024 >= kMostBlocks - 1) return ACC_EINVAL;
   if (!aligned_to(x, value_size(type)) || !aligned_to(tokens, token_size(token_type)) || !aligned16(code)) return ACC_EALIGN;
   ctx->last_launches = 0;
   if (n == 0) return ACC_OK;
@@ -648,6 +649,7 @@ int acc_checkpoint_load(acc_ctx* ctx, const uint8_t* code, const uint8_t* code_s
 
 static int check_linear(const acc_ctx* ctx, int layer, int64_t n) {
   if (!ctx || layer < 0 || layer >= ctx->cfg.n_layers || ctx->plan.layers[layer].kind != ACC_MATRIX) return ACC_EINVAL;
+  if (ctx->plan.layers[layer].cols > kMostColumns) return ACC_EINVAL;
   return n < 0 || n > ACC_MAX_TOKENS || n * ctx->cfg.n_workers > ACC_MAX_TOKENS ? ACC_EINVAL : ACC_OK;
 }
 int acc_linear_grad_workspace_bytes(const acc_ctx* ctx, int32_t layer, int64_t n, size_t* bytes) {

@@ -14,7 +14,25 @@ PROGRAM = r"""
 
 #include "acc_internal.cuh"
 
-int main() {
+// A checkpoint's rows have 2^30 columns at most, and so have the layers of a gradient from one.
+static int columns() {
+  static acc_ctx ctx;
+  ctx.cfg.n_workers = ctx.cfg.n_layers = 1;
+  ctx.plan.layers.emplace_back();
+  acc::DevLayer& l = ctx.plan.layers[0];
+  l.rows = 1; l.kind = ACC_MATRIX;
+  size_t bytes = 0;
+  l.cols = 1 << 30;
+  if (acc_linear_grad_workspace_bytes(&ctx, 0, 1, &bytes) != ACC_OK || bytes < (2ull << 30)) return 3;
+  l.cols = (1 << 30) + 1;
+  if (acc_linear_grad_workspace_bytes(&ctx, 0, 1, &bytes) != ACC_EINVAL) return 4;
+  alignas(256) static float here[64];  // (an address; the call is refused before anything is read)
+  uint8_t* const code = reinterpret_cast<uint8_t*>(here);
+  return acc_linear_grad(&ctx, 0, here, ACC_BF16, 1, 1, 1, 1.f, code, code, here, 0, here, ~(size_t)0, nullptr) == ACC_EINVAL ? 0 : 5;
+}
+
+int main(int argc, char**) {
+  if (argc > 1) return columns();
   static acc_ctx ctx;
   ctx.cfg.n_workers = 4;
   const int shapes[][2] = {{33278, 650}, {2600, 650}, {40, 24}, {70000, 33}};
@@ -61,3 +79,7 @@ def program(tmp_path_factory):
 def test_threads_that_ask_at_once_get_their_own_answers(program):
     done = subprocess.run([program], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stdout + done.stderr
+
+
+def test_most_columns(program):
+    assert subprocess.run([program, "columns"], timeout=60).returncode == 0
