@@ -327,7 +327,8 @@ int acc_embedding_grad(acc_ctx* ctx, int32_t layer, const void* tokens, int32_t 
  * gradient is half of what the step compresses) --------------------------------------------------------------------
  * Rows of logits, fp32 or bf16 (logit_type ACC_F32 / ACC_BF16), `vocab` elements each and `ld` elements apart (ld >= vocab:
  * what lies between the rows is neither read nor written); any start that suits the type.  scale > 0 multiplies the logits
- * (1 / temperature); scale log2(e) has to be finite in fp32 (any scale up to 2^127).  Row i, with m = max_j z_j and S = sum_j exp(scale (z_j - m)):
+ * (1 / temperature); scale log2(e) has to be finite in fp32 (any scale up to 2^127).  z_j - m is taken in fp32.
+ * Row i, with m = max_j z_j and S = sum_j exp(scale (z_j - m)):
  *   norm[2i] = m, norm[2i + 1] = log S;  log p_j = scale (z_j - m) - log S;  logp[i] = log p_tokens[i];
  *   entropy[i] = -sum_j p_j log p_j (a p_j of 0 adds nothing);
  *   top_index[i][k], top_logp[i][k], k < top: the tokens of the `top` largest logits, equal ones by rising index, and their
@@ -358,12 +359,12 @@ int acc_token_logprobs_grad(acc_ctx* ctx, const void* logits, int32_t logit_type
                             void* dlogits, int32_t out_type, int64_t ld_out, void* stream);
 
 /* ---- Activation checkpoints in 8 bits, and linear layers' gradients from them (no counterpart in the paper) --------
- * A checkpoint of a row of `cols` values: ceil(cols / 32) * 32 e4m3 codes (those behind the columns are zeros) and one power of
+ * A checkpoint of a row of `cols` values: ceil(cols / 32) * 32 e4m3 codes (those behind the columns count as zeros) and one power of
  * two for each block of ACC_CHECKPOINT_BLOCK = 32 columns, an e8m0 byte (2^(byte - 127)), ceil(cols / 32) bytes a row.
  * acc_checkpoint_store: x [n] rows, ld elements apart, fp32 or bf16.  A block's scale brings its largest magnitude into
  *   [128, 256) -- not below 2^-126 --, and every value is rounded to the nearest code (ties to even): half a step is 2^-4 of
  *   a value, or 2^-17 of the block's largest where that is more.  A block of zeros has the byte 0; one that holds a NaN or an
- *   infinity the byte 255: it reads as NaN.  tokens: NULL, or one per row: rows of negative tokens are not read and stored as
+ *   infinity the byte 255 and NaN for all its codes: it reads as NaN.  tokens: NULL, or one per row: rows of negative tokens are not read and stored as
  *   zeros (padding then adds nothing to a gradient).
  * acc_checkpoint_load: the values, out [n] rows, ld elements apart, in fp32 (exact) or bf16 (exact but below 2^-126).
  * acc_linear_grad: for a MATRIX layer y = x W^T (W: rows x cols) and each of the W workers w,

@@ -372,10 +372,13 @@ __device__ __forceinline__ void load_pairs(const LinArgs& a, StepWalk walk, cons
 // The blocks of a pair walk over the tiles.  In each, warps 0-7 add up and write the sums of its 128 rows, two warps (half of
 // the columns each) for each quarter of them, warps 9 and 10 issue the copies of dy and of the checkpoint, and where dy cannot
 // be copied eight more warps load it; the first block's warp 8 issues the products of both.  Two sums in tensor memory: one is
-// read while the other grows.  8 x 700 tokens into 33278 x 650: 287 us (843 TFLOP/s, 37 % of the memory's rate); 187 us with the
+// read while the other grows.  All by this kernel alone, a few launches:
+// 8 x 700 tokens into 33278 x 650: 287 us (843 TFLOP/s, 37 % of the memory's rate); 187 us with the
 // sums left unwritten, 132 us for the same writing alone: the two meet in the L2 cache, which hands out 2.6 GB of operands
 // meanwhile.  8 x 16384 tokens into 4096 x 1024: 882 us, 1246 TFLOP/s; into 2600 x 650, whose tiles are 8 % and 3 % empty and fill
-// 3.6 waves of 4: 468 us, 945 TFLOP/s.
+// 3.6 waves of 4: 468 us, 945 TFLOP/s.  Whole calls (decoding too), a thousand behind one another at the power cap: 337-365 us
+// and 557-600 us for the first and the last of these.  dy by loads, 33278 x 650: bf16 rows on 4 bytes 835-1070 us, on 2 bytes
+// 1010 us, fp32 1880 us.
 template <DyPath P, bool WIDE>
 __global__ void __launch_bounds__(LinCfg<P>::threads, 1)
 linear_grad_kernel(const LinArgs a, const __grid_constant__ CUtensorMap dy_map, const __grid_constant__ CUtensorMap x_map) {
